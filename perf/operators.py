@@ -291,7 +291,7 @@ def _handle(st):
         if st.case["kind"] == "decode":
             room = ctx.ds_decode_quant_workspace_bytes(st.b, st.longest + 1)
         elif st.case["kind"] == "shared":
-            room = ctx.ds_decode_shared_workspace_bytes(st.b, st.case["groups"], st.longest_prefix, max(1, st.longest))
+            room = ctx.ds_decode_shared_workspace_bytes(st.b, st.longest_prefix, max(1, st.longest))
         st.handle = ctx, torch.empty(max(256, room), dtype=torch.uint8, device="cuda")
     return st.handle
 
