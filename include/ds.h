@@ -261,6 +261,90 @@ ds_status ds_decode_attention(ds_ctx *ctx, const void *q, const int32_t *kv_lens
                               int32_t num_blocks, void *o,
                               void *workspace, size_t workspace_bytes, void *stream);
 
+/* ---- a paged cache of 8 bits, and prefixes that sequences share ----
+ * The cache of a decoding instance bounds its batch (its size) and its step (its bytes are read once per token).  These
+ * calls stand beside ds_kv_migrate, ds_decode_attention and ds_decode_step for a cache that holds each number in 8 bits,
+ * and for sequences that start with the same tokens (one system prompt, several continuations of one prompt), whose K
+ * and V are kept and read once for all of them.
+ *
+ * A row is the s numbers x_d of one token and key/value head, a = max |x_d|.  It is held as 8-bit values and one scale c:
+ *   DS_KV_E4M3  c = 2^e, e the least integer >= -100 with a <= 448 2^e;  values: x_d / c to the nearest e4m3 (OCP), ties to even
+ *   DS_KV_INT8  c = the least bf16 >= a / 127 and >= 2^-100;             values: x_d / c to the nearest integer, ties to even
+ * a = 0: c = 1.  A row that holds an infinity or a NaN: c = NaN, values 0; all of it then stands for NaN.  What a row
+ * stands for, value times c, is exact in fp32.
+ *   k_cache [num_blocks, n_kv, 16, s] bytes; v_cache [num_blocks, n_kv, s, 16] bytes - a feature's 16 tokens together, unlike
+ *   the bf16 cache; k_scale, v_scale [num_blocks, n_kv, 16] bf16.  Block tables are those of the bf16 cache.
+ * With DS_KV_BF16, where a call takes it, k_cache and v_cache are the bf16 cache and the scales NULL. */
+enum { DS_KV_BF16 = 0, DS_KV_E4M3 = 1, DS_KV_INT8 = 2 };
+
+/* ds_kv_migrate into such a cache: every row quantised as it is written.  Slots that no token maps to keep their bytes. */
+ds_status ds_kv_migrate_quant(ds_ctx *ctx, const void *k_src, const void *v_src, const int32_t *cu_seqlens,
+                              int32_t B, int32_t t, int32_t max_seqlen, const int32_t *block_tables,
+                              int32_t max_blocks_per_seq, void *k_cache, void *v_cache, void *k_scale, void *v_scale,
+                              int32_t num_blocks, int32_t kv_type, void *stream);
+
+/* The reverse: what the first cu_seqlens[i+1] - cu_seqlens[i] tokens of each sequence's pages stand for, as contiguous
+ * rows k_dst, v_dst [t, n_kv, s] bf16, rounded to nearest even (e4m3: exact; what would round to infinity is the largest
+ * finite bf16).  Quantising these rows again need not give the same bytes; e4m3 stands for the same numbers. */
+ds_status ds_kv_read_quant(ds_ctx *ctx, const int32_t *cu_seqlens, int32_t B, int32_t t, int32_t max_seqlen,
+                           const int32_t *block_tables, int32_t max_blocks_per_seq, const void *k_cache,
+                           const void *v_cache, const void *k_scale, const void *v_scale, int32_t num_blocks,
+                           int32_t kv_type, void *k_dst, void *v_dst, void *stream);
+
+/* One new row of K and V for each of B sequences, written at position ctx_lens[i] (tokens before it; its page must be in
+ * block_tables).  Row i starts row_stride * i elements (a multiple of 8, at least n_kv s) behind k_new / v_new: they may
+ * point into the rows of a QKV product.  ctx_lens[i] = -1 marks a row that only pads the batch: nothing is written for
+ * it.  No two rows may name the same slot. */
+ds_status ds_kv_append_quant(ds_ctx *ctx, const void *k_new, const void *v_new, int32_t row_stride,
+                             const int32_t *ctx_lens, const int32_t *block_tables, int32_t B,
+                             int32_t max_blocks_per_seq, void *k_cache, void *v_cache, void *k_scale, void *v_scale,
+                             int32_t num_blocks, int32_t kv_type, void *stream);
+
+/* ds_decode_attention over such a cache; kv_lens[i] = 0: output 0.  Workspace: ds_decode_quant_workspace_bytes(B,
+ * max_kv_len), which serves every smaller batch and length too, and ds_decode_step_quant with max_ctx for max_kv_len.
+ * The result does not depend on the workspace's size. */
+size_t ds_decode_quant_workspace_bytes(const ds_ctx *ctx, int32_t max_batch, int32_t max_ctx);
+ds_status ds_decode_attention_quant(ds_ctx *ctx, const void *q, const int32_t *kv_lens, const int32_t *block_tables,
+                                    int32_t B, int32_t max_blocks_per_seq, int32_t max_kv_len, const void *k_cache,
+                                    const void *v_cache, const void *k_scale, const void *v_scale, int32_t num_blocks,
+                                    int32_t kv_type, void *o, void *workspace, size_t workspace_bytes, void *stream);
+
+/* ds_decode_step on such a cache: the new token's rows are quantised, appended, and attended over as they then stand.
+ * ctx_lens[i] = -1: a row that pads the batch (nothing is appended, its attention is 0, its y is the layer's of that).
+ * A workspace below what ds_decode_quant_workspace_bytes reports may serve with plans of the products that split less. */
+ds_status ds_decode_step_quant(ds_ctx *ctx, const ds_layer_weights *w, const void *x, const int32_t *ctx_lens,
+                               const int32_t *block_tables, int32_t B, int32_t max_blocks_per_seq, int32_t max_ctx,
+                               void *k_cache, void *v_cache, void *k_scale, void *v_scale, int32_t num_blocks,
+                               int32_t kv_type, void *y, void *workspace, size_t workspace_bytes, void *stream);
+
+/* ds_decode_attention for rows in groups that share a prefix: row r of group i attends over the prefix_lens[i] tokens in
+ * the pages prefix_tables[i * max_prefix_blocks + ..] and then over its own kv_lens[r] tokens in those of block_tables,
+ * as over one sequence.  A prefix's K and V are read once for its group.  The prefix may end inside a page; a row's own
+ * tokens start at slot 0 of its first own page.  Either length may be 0; both: output 0.
+ *   cu_groups      device [n_groups+1] int32: group i is rows cu_groups[i] .. cu_groups[i+1]-1; starts at 0, ends at B
+ *   max_group_rows, max_prefix_len, max_kv_len   host upper bounds (> 0) of what the arrays hold
+ *   prefix_tables  device [n_groups, max_prefix_blocks] int32
+ * kv_type: any.  Workspace: ds_decode_shared_workspace_bytes(B, max_prefix_len, max_kv_len), which serves smaller calls
+ * and ds_decode_step_shared too. */
+size_t ds_decode_shared_workspace_bytes(const ds_ctx *ctx, int32_t max_batch, int32_t max_prefix_len, int32_t max_ctx);
+ds_status ds_decode_attention_shared(ds_ctx *ctx, const void *q, const int32_t *cu_groups, int32_t n_groups,
+                                     int32_t max_group_rows, const int32_t *prefix_lens, const int32_t *prefix_tables,
+                                     int32_t max_prefix_blocks, int32_t max_prefix_len, const int32_t *kv_lens,
+                                     const int32_t *block_tables, int32_t B, int32_t max_blocks_per_seq,
+                                     int32_t max_kv_len, const void *k_cache, const void *v_cache, const void *k_scale,
+                                     const void *v_scale, int32_t num_blocks, int32_t kv_type, void *o, void *workspace,
+                                     size_t workspace_bytes, void *stream);
+
+/* ds_decode_step for such rows, on a cache of any kv_type: ctx_lens[i] own tokens before this step (the prefix not
+ * counted), the new one appended behind them. */
+ds_status ds_decode_step_shared(ds_ctx *ctx, const ds_layer_weights *w, const void *x, const int32_t *cu_groups,
+                                int32_t n_groups, int32_t max_group_rows, const int32_t *prefix_lens,
+                                const int32_t *prefix_tables, int32_t max_prefix_blocks, int32_t max_prefix_len,
+                                const int32_t *ctx_lens, const int32_t *block_tables, int32_t B,
+                                int32_t max_blocks_per_seq, int32_t max_ctx, void *k_cache, void *v_cache, void *k_scale,
+                                void *v_scale, int32_t num_blocks, int32_t kv_type, void *y, void *workspace,
+                                size_t workspace_bytes, void *stream);
+
 /* ---- per-kernel timing (HIP events around every launch; off by default) ---- */
 enum {
   DS_K_LAYERNORM = 0, DS_K_GEMM = 1, DS_K_PREFILL_ATTN = 2, DS_K_KV_MIGRATE = 3,

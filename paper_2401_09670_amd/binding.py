@@ -24,6 +24,7 @@ DS_OK = 0
 STATIC_SCRATCH_BYTES = 32 << 20   # DS_STATIC_SCRATCH_BYTES of include/ds.h
 STATUS_NAMES = {0: "DS_OK", 1: "DS_ERR_INVALID_ARG", 2: "DS_ERR_UNSUPPORTED", 3: "DS_ERR_WORKSPACE",
                 4: "DS_ERR_HIP", 5: "DS_ERR_BOUNDS"}
+KV_BF16, KV_E4M3, KV_INT8 = 0, 1, 2   # DS_KV_*: what a paged cache holds
 KERNEL_CLASSES = ("layernorm", "gemm", "prefill_attn", "kv_migrate", "skinny_gemm", "decode_attn", "kv_append",
                   "token_io")
 
@@ -32,7 +33,10 @@ EXPORTS = ("ds_create", "ds_destroy", "ds_last_error", "ds_set_validate", "ds_pr
            "ds_decode_workspace_bytes", "ds_prefill", "ds_kv_migrate", "ds_decode_step", "ds_decode_step_static",
            "ds_layernorm",
            "ds_linear_workspace_bytes", "ds_linear_plan", "ds_layer_plan", "ds_linear", "ds_prefill_attention", "ds_decode_attention",
-           "ds_embed", "ds_next_token_workspace_bytes", "ds_next_token", "ds_profile_enable", "ds_profile_collect")
+           "ds_embed", "ds_next_token_workspace_bytes", "ds_next_token", "ds_profile_enable", "ds_profile_collect",
+           "ds_decode_quant_workspace_bytes", "ds_decode_shared_workspace_bytes", "ds_kv_migrate_quant",
+           "ds_kv_read_quant", "ds_kv_append_quant", "ds_decode_attention_quant", "ds_decode_attention_shared",
+           "ds_decode_step_quant", "ds_decode_step_shared")
 
 
 class DsError(RuntimeError):
@@ -55,7 +59,9 @@ class LayerWeights(ctypes.Structure):
 
 # the entry points that take tensors: their library functions are called through the module _calls
 TENSOR_CALLS = ("ds_prefill", "ds_kv_migrate", "ds_decode_step", "ds_decode_step_static", "ds_layernorm", "ds_linear",
-                "ds_prefill_attention", "ds_decode_attention", "ds_embed", "ds_next_token")
+                "ds_prefill_attention", "ds_decode_attention", "ds_embed", "ds_next_token", "ds_kv_migrate_quant",
+                "ds_kv_read_quant", "ds_kv_append_quant", "ds_decode_attention_quant", "ds_decode_attention_shared",
+                "ds_decode_step_quant", "ds_decode_step_shared")
 
 _lib = None
 
@@ -122,6 +128,23 @@ def load_library() -> ctypes.CDLL:
     lib.ds_next_token_workspace_bytes.restype = sz
     lib.ds_next_token.argtypes = [vp, vp, vp, i32, vp, vp, vp, i32, vp, vp, vp, sz, vp]
     lib.ds_next_token.restype = ctypes.c_int
+    cache = [vp, vp, vp, vp, i32, i32]          # pages, scales, number of pages, what they hold
+    groups = [vp, i32, i32, vp, vp, i32, i32]
+    lib.ds_decode_quant_workspace_bytes.argtypes = [vp, i32, i32]
+    lib.ds_decode_quant_workspace_bytes.restype = sz
+    lib.ds_decode_shared_workspace_bytes.argtypes = [vp, i32, i32, i32]
+    lib.ds_decode_shared_workspace_bytes.restype = sz
+    for name, args in (
+            ("ds_kv_migrate_quant", [vp, vp, vp, i32, i32, i32, vp, i32, *cache]),
+            ("ds_kv_read_quant", [vp, i32, i32, i32, vp, i32, *cache, vp, vp]),
+            ("ds_kv_append_quant", [vp, vp, i32, vp, vp, i32, i32, *cache]),
+            ("ds_decode_attention_quant", [vp, vp, vp, i32, i32, i32, *cache, vp, vp, sz]),
+            ("ds_decode_attention_shared", [vp, *groups, vp, vp, i32, i32, i32, *cache, vp, vp, sz]),
+            ("ds_decode_step_quant", [ctypes.POINTER(LayerWeights), vp, vp, vp, i32, i32, i32, *cache, vp, vp, sz]),
+            ("ds_decode_step_shared", [ctypes.POINTER(LayerWeights), vp, *groups, vp, vp, i32, i32, i32, *cache, vp, vp,
+                                       sz])):
+        getattr(lib, name).argtypes = [vp, *args, vp]
+        getattr(lib, name).restype = ctypes.c_int
     lib.ds_profile_enable.argtypes = [vp, i32]
     lib.ds_profile_enable.restype = ctypes.c_int
     lib.ds_profile_collect.argtypes = [vp, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_int64)]
@@ -250,6 +273,63 @@ class Context:
         self._check(self.calls.ds_decode_attention(self.handle.value, q, kv_lens, block_tables, B,
                                                    max_blocks_per_seq, max_kv_len, k_cache, v_cache, num_blocks, o,
                                                    workspace, workspace, _stream()))
+
+    # ---- pages of 8 bits, prefixes that rows share ----
+    def ds_decode_quant_workspace_bytes(self, max_batch: int, max_ctx: int) -> int:
+        return self.lib.ds_decode_quant_workspace_bytes(self.handle, max_batch, max_ctx)
+
+    def ds_decode_shared_workspace_bytes(self, max_batch: int, max_prefix_len: int, max_ctx: int) -> int:
+        return self.lib.ds_decode_shared_workspace_bytes(self.handle, max_batch, max_prefix_len, max_ctx)
+
+    def ds_kv_migrate_quant(self, k_src, v_src, cu_seqlens, B: int, t: int, max_seqlen: int, block_tables,
+                            max_blocks_per_seq: int, k_cache, v_cache, k_scale, v_scale, num_blocks: int, kv_type: int):
+        self._check(self.calls.ds_kv_migrate_quant(self.handle.value, k_src, v_src, cu_seqlens, B, t, max_seqlen,
+                                                   block_tables, max_blocks_per_seq, k_cache, v_cache, k_scale, v_scale,
+                                                   num_blocks, kv_type, _stream()))
+
+    def ds_kv_read_quant(self, cu_seqlens, B: int, t: int, max_seqlen: int, block_tables, max_blocks_per_seq: int, k_cache,
+                         v_cache, k_scale, v_scale, num_blocks: int, kv_type: int, k_dst, v_dst):
+        self._check(self.calls.ds_kv_read_quant(self.handle.value, cu_seqlens, B, t, max_seqlen, block_tables,
+                                                max_blocks_per_seq, k_cache, v_cache, k_scale, v_scale, num_blocks,
+                                                kv_type, k_dst, v_dst, _stream()))
+
+    def ds_kv_append_quant(self, k_new, v_new, row_stride: int, ctx_lens, block_tables, B: int, max_blocks_per_seq: int,
+                           k_cache, v_cache, k_scale, v_scale, num_blocks: int, kv_type: int):
+        self._check(self.calls.ds_kv_append_quant(self.handle.value, k_new, v_new, row_stride, ctx_lens, block_tables, B,
+                                                  max_blocks_per_seq, k_cache, v_cache, k_scale, v_scale, num_blocks,
+                                                  kv_type, _stream()))
+
+    def ds_decode_attention_quant(self, q, kv_lens, block_tables, B: int, max_blocks_per_seq: int, max_kv_len: int,
+                                  k_cache, v_cache, k_scale, v_scale, num_blocks: int, kv_type: int, o, workspace=None):
+        self._check(self.calls.ds_decode_attention_quant(self.handle.value, q, kv_lens, block_tables, B,
+                                                         max_blocks_per_seq, max_kv_len, k_cache, v_cache, k_scale,
+                                                         v_scale, num_blocks, kv_type, o, workspace, workspace,
+                                                         _stream()))
+
+    def ds_decode_attention_shared(self, q, cu_groups, n_groups: int, max_group_rows: int, prefix_lens, prefix_tables,
+                                   max_prefix_blocks: int, max_prefix_len: int, kv_lens, block_tables, B: int,
+                                   max_blocks_per_seq: int, max_kv_len: int, k_cache, v_cache, k_scale, v_scale,
+                                   num_blocks: int, kv_type: int, o, workspace):
+        self._check(self.calls.ds_decode_attention_shared(
+            self.handle.value, q, cu_groups, n_groups, max_group_rows, prefix_lens, prefix_tables, max_prefix_blocks,
+            max_prefix_len, kv_lens, block_tables, B, max_blocks_per_seq, max_kv_len, k_cache, v_cache, k_scale, v_scale,
+            num_blocks, kv_type, o, workspace, workspace, _stream()))
+
+    def ds_decode_step_quant(self, weights: LayerWeights, x, ctx_lens, block_tables, B: int, max_blocks_per_seq: int,
+                             max_ctx: int, k_cache, v_cache, k_scale, v_scale, num_blocks: int, kv_type: int, y,
+                             workspace):
+        self._check(self.calls.ds_decode_step_quant(self.handle.value, weights, x, ctx_lens, block_tables, B,
+                                                    max_blocks_per_seq, max_ctx, k_cache, v_cache, k_scale, v_scale,
+                                                    num_blocks, kv_type, y, workspace, workspace, _stream()))
+
+    def ds_decode_step_shared(self, weights: LayerWeights, x, cu_groups, n_groups: int, max_group_rows: int, prefix_lens,
+                              prefix_tables, max_prefix_blocks: int, max_prefix_len: int, ctx_lens, block_tables, B: int,
+                              max_blocks_per_seq: int, max_ctx: int, k_cache, v_cache, k_scale, v_scale, num_blocks: int,
+                              kv_type: int, y, workspace):
+        self._check(self.calls.ds_decode_step_shared(
+            self.handle.value, weights, x, cu_groups, n_groups, max_group_rows, prefix_lens, prefix_tables,
+            max_prefix_blocks, max_prefix_len, ctx_lens, block_tables, B, max_blocks_per_seq, max_ctx, k_cache, v_cache,
+            k_scale, v_scale, num_blocks, kv_type, y, workspace, workspace, _stream()))
 
     # ---- the two ends of the token loop ----
     def ds_embed(self, token_ids, positions, tok_emb, vocab: int, pos_emb, n_pos: int, rows: int, x):

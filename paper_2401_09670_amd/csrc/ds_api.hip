@@ -11,6 +11,7 @@
 #include <map>
 #include <mutex>
 #include <new>
+#include <tuple>
 #include <utility>
 #include <vector>
 
@@ -49,6 +50,7 @@ struct ds_ctx {
   };
   mutable std::map<int, Least> prefill_least;
   mutable std::map<std::pair<int, int>, Least> decode_least;
+  mutable std::map<std::tuple<int, int, int>, size_t> tile_states;
 };
 
 // ---- per-device set-up: kernel attributes, address of the static scratch array ----
@@ -480,6 +482,34 @@ ds_ctx::Least decode_least(const ds_ctx* ctx, int max_batch, int max_ctx) {
   return need;
 }
 
+// The states of the attention over pages of 8 bits or behind a shared prefix, for any batch up to max_batch (fewer
+// sequences can mean more splits).  max_prefix = 0: there is no prefix.
+size_t tile_states(const ds_ctx* ctx, int max_batch, int max_ctx, int max_prefix) {
+  const ds_model_cfg& c = ctx->cfg;
+  const std::tuple<int, int, int> key(max_batch, (max_ctx + 15) / 16, (max_prefix + 15) / 16);
+  const auto hit = ctx->tile_states.find(key);
+  if (hit != ctx->tile_states.end()) return hit->second;
+  size_t most = 0;
+  for (int b = 1; b <= max_batch; ++b) {
+    const ds::TilePlan p = ds::tile_plan(b, c.n_heads, c.n_kv_heads, max_ctx, max_prefix);
+    most = std::max(most, ds::tile_states_bytes(b, c.n_heads, c.head_dim, p.own + p.prefix));
+  }
+  most = align_up(most, 256);
+  if (ctx->tile_states.size() < 4096) ctx->tile_states[key] = most;
+  return most;
+}
+
+// The same step with that attention: its states take the place of the FFN intermediate and of the products' partial sums,
+// neither of which is live meanwhile.
+ds_ctx::Least tile_step_least(const ds_ctx* ctx, int max_batch, int max_ctx, int max_prefix) {
+  const ds_model_cfg& c = ctx->cfg;
+  const size_t bh = align_up((size_t)max_batch * c.hidden * 2, 256);
+  const size_t b3h = align_up((size_t)max_batch * qkv_width(c) * 2, 256);
+  const size_t bm = align_up((size_t)max_batch * c.ffn * 2, 256);
+  const size_t partials = least_gemm_ws(ctx, max_batch);
+  return {3 * bh + b3h + std::max(bm + partials, tile_states(ctx, max_batch, max_ctx, max_prefix)), partials};
+}
+
 // Bytes for the partial states of a decode step's attention: those of the least number of splits lie between the FFN
 // intermediate and the partial sums of the products.  Neither of these is live while the attention runs, so the states
 // of more splits may take the place of all three.  A matter of B and max_ctx, not of the workspace that a call brings:
@@ -861,26 +891,123 @@ ds_status ds_decode_attention(ds_ctx* ctx, const void* q, const int32_t* kv_lens
   return DS_OK;
 }
 
-// Both decode-step entry points: `workspace` is the caller's buffer, or null for the static scratch array
+// Pages that a call is given: of 8 bits with their scales, or, where a call takes either, bf16 without.
+static ds_status check_cache(ds_ctx* ctx, const char* who, const void* k, const void* v, const void* k_scale,
+                             const void* v_scale, int32_t num_blocks, int32_t kv_type, bool bf16_too) {
+  const bool quant = kv_type == DS_KV_E4M3 || kv_type == DS_KV_INT8;
+  if (!quant && !(bf16_too && kv_type == DS_KV_BF16))
+    return fail(ctx, DS_ERR_UNSUPPORTED, "%s: kv_type %d is not one that this call takes", who, kv_type);
+  if (!k || !v || (quant && (!k_scale || !v_scale))) return fail(ctx, DS_ERR_INVALID_ARG, "%s: NULL pointer", who);
+  if (!quant && (k_scale || v_scale)) return fail(ctx, DS_ERR_INVALID_ARG, "%s: bf16 pages have no scales", who);
+  if (num_blocks <= 0) return fail(ctx, DS_ERR_INVALID_ARG, "%s: non-positive size", who);
+  if (!aligned16(k) || !aligned16(v) || !aligned16(k_scale) || !aligned16(v_scale))
+    return fail(ctx, DS_ERR_INVALID_ARG, "%s: pointers must be 16-byte aligned", who);
+  return DS_OK;
+}
+
+// Packed rows and the pages of their sequences.
+static ds_status check_rows(ds_ctx* ctx, const char* who, const void* k_rows, const void* v_rows, const int32_t* cu_seqlens,
+                            int32_t B, int32_t t, int32_t max_seqlen, const int32_t* block_tables, int32_t max_blocks) {
+  if (!k_rows || !v_rows || !cu_seqlens || !block_tables) return fail(ctx, DS_ERR_INVALID_ARG, "%s: NULL pointer", who);
+  if (B <= 0 || t <= 0 || max_seqlen <= 0 || max_seqlen > t || max_blocks <= 0)
+    return fail(ctx, DS_ERR_INVALID_ARG, "%s: non-positive or inconsistent size", who);
+  if ((int64_t)max_blocks * ctx->cfg.block_size < max_seqlen)
+    return fail(ctx, DS_ERR_INVALID_ARG, "%s: max_seqlen %d does not fit %d blocks per sequence", who, max_seqlen, max_blocks);
+  if (!aligned16(k_rows) || !aligned16(v_rows))
+    return fail(ctx, DS_ERR_INVALID_ARG, "%s: pointers must be 16-byte aligned", who);
+  return DS_OK;
+}
+
+static ds_status validate_rows(ds_ctx* ctx, const char* who, const int32_t* cu_seqlens, int32_t B, int32_t t,
+                               int32_t max_seqlen, const int32_t* block_tables, int32_t max_blocks, int32_t num_blocks,
+                               hipStream_t s) {
+  std::vector<int32_t> cu, lens((size_t)B);
+  if (ds_status st = validate_cu(ctx, who, cu_seqlens, B, t, max_seqlen, s, cu)) return st;
+  for (int i = 0; i < B; ++i) lens[i] = cu[i + 1] - cu[i];
+  return validate_tables(ctx, who, block_tables, B, max_blocks, num_blocks, lens, s);
+}
+
+// The groups of rows that share a prefix.
+static ds_status check_groups(ds_ctx* ctx, const char* who, const int32_t* cu_groups, int32_t n_groups,
+                              int32_t max_group_rows, const int32_t* prefix_lens, const int32_t* prefix_tables,
+                              int32_t max_prefix_blocks, int32_t max_prefix_len, int32_t B) {
+  if (!cu_groups || !prefix_lens || !prefix_tables) return fail(ctx, DS_ERR_INVALID_ARG, "%s: NULL pointer", who);
+  if (n_groups <= 0 || max_group_rows <= 0 || max_prefix_blocks <= 0 || max_prefix_len <= 0 ||
+      (int64_t)n_groups * max_group_rows < B)
+    return fail(ctx, DS_ERR_INVALID_ARG, "%s: non-positive size, or groups that cannot hold %d rows", who, B);
+  if ((int64_t)max_prefix_blocks * ctx->cfg.block_size < max_prefix_len)
+    return fail(ctx, DS_ERR_INVALID_ARG, "%s: max_prefix_len %d does not fit %d blocks per prefix", who, max_prefix_len,
+                max_prefix_blocks);
+  return DS_OK;
+}
+
+static ds_status validate_groups(ds_ctx* ctx, const char* who, const int32_t* cu_groups, int32_t n_groups,
+                                 int32_t max_group_rows, int32_t B, const int32_t* prefix_lens, const int32_t* prefix_tables,
+                                 int32_t max_prefix_blocks, int32_t max_prefix_len, int32_t num_blocks, hipStream_t s) {
+  std::vector<int32_t> cu, lens;
+  if (ds_status st = fetch_i32(ctx, cu_groups, (size_t)n_groups + 1, s, cu)) return st;
+  if (cu[0] != 0 || cu[n_groups] != B)
+    return fail(ctx, DS_ERR_BOUNDS, "%s: cu_groups goes from %d to %d, must go from 0 to B = %d", who, cu[0], cu[n_groups], B);
+  for (int i = 0; i < n_groups; ++i) {
+    const long rows = (long)cu[i + 1] - cu[i];
+    if (rows < 0 || rows > max_group_rows)
+      return fail(ctx, DS_ERR_BOUNDS, "%s: group %d has %ld rows, outside [0, %d]", who, i, rows, max_group_rows);
+  }
+  if (ds_status st = fetch_i32(ctx, prefix_lens, (size_t)n_groups, s, lens)) return st;
+  for (int i = 0; i < n_groups; ++i)
+    if (lens[i] < 0 || lens[i] > max_prefix_len)
+      return fail(ctx, DS_ERR_BOUNDS, "%s: prefix %d has %d tokens, outside [0, %d]", who, i, lens[i], max_prefix_len);
+  return validate_tables(ctx, who, prefix_tables, n_groups, max_prefix_blocks, num_blocks, lens, s);
+}
+
+// Where a step's keys and values are: in the bf16 cache alone, or (`tiles`) in pages of 8 bits, behind a prefix that rows
+// share, or both; then the attention runs on the tile kernel.
+struct StepCache {
+  ds::KvCache kv;
+  bool tiles;
+  const int32_t *cu_groups = nullptr, *prefix_lens = nullptr, *prefix_tables = nullptr;
+  int n_groups = 0, max_group_rows = 0, max_prefix_blocks = 0, max_prefix = 0;
+};
+
+static ds::TileAttention tile_attention(const ds_ctx* ctx, const StepCache& cache, const void* q, int q_stride,
+                                        const int32_t* kv_lens, int kv_len_add, const int32_t* block_tables, int B,
+                                        int max_blocks, int max_kv_len, void* o, void* states) {
+  const ds_model_cfg& c = ctx->cfg;
+  ds::TileAttention t{};
+  t.q = q; t.q_stride = q_stride;
+  t.cu_groups = cache.cu_groups; t.prefix_lens = cache.prefix_lens; t.prefix_tables = cache.prefix_tables;
+  t.n_groups = cache.n_groups; t.max_rows = std::min(cache.max_group_rows, B);
+  t.max_prefix_pages = cache.max_prefix_blocks; t.max_prefix = cache.max_prefix;
+  t.kv_lens = kv_lens; t.block_tables = block_tables;
+  t.kv_len_add = kv_len_add; t.B = B; t.max_blocks = max_blocks; t.max_kv_len = max_kv_len;
+  t.cache = cache.kv;
+  t.n_heads = c.n_heads; t.n_kv_heads = c.n_kv_heads; t.head_dim = c.head_dim;
+  t.plan = ds::tile_plan(B, c.n_heads, c.n_kv_heads, max_kv_len, cache.max_prefix);
+  t.o = o; t.states = states;
+  return t;
+}
+
+// Every decode-step entry point: `workspace` is the caller's buffer, or null for the static scratch array
 // of the current device (then the step must fit DS_STATIC_SCRATCH_BYTES).
 static ds_status decode_step(ds_ctx* ctx, const ds_layer_weights* w, const void* x, const int32_t* ctx_lens,
                              const int32_t* block_tables, int32_t B, int32_t max_blocks_per_seq, int32_t max_ctx,
-                             void* k_cache, void* v_cache, int32_t num_blocks, void* y, void* workspace,
-                             size_t workspace_bytes, bool use_static, void* stream) {
+                             const StepCache& cache, int32_t num_blocks, void* y, void* workspace,
+                             size_t workspace_bytes, bool use_static, void* stream, const char* who = "ds_decode_step") {
   if (!ctx) return DS_ERR_INVALID_ARG;
   ds_status st = check_weights(ctx, w);
   if (st != DS_OK) return st;
+  void *k_cache = cache.kv.k, *v_cache = cache.kv.v;
   if (!x || !ctx_lens || !block_tables || !k_cache || !v_cache || !y)
-    return fail(ctx, DS_ERR_INVALID_ARG, "ds_decode_step: NULL pointer");
+    return fail(ctx, DS_ERR_INVALID_ARG, "%s: NULL pointer", who);
   if (B <= 0 || max_ctx <= 0 || num_blocks <= 0 || max_blocks_per_seq <= 0)
-    return fail(ctx, DS_ERR_INVALID_ARG, "ds_decode_step: non-positive size");
+    return fail(ctx, DS_ERR_INVALID_ARG, "%s: non-positive size", who);
   if ((int64_t)max_blocks_per_seq * ctx->cfg.block_size < max_ctx)
-    return fail(ctx, DS_ERR_INVALID_ARG, "ds_decode_step: max_ctx %d does not fit %d blocks per sequence", max_ctx,
+    return fail(ctx, DS_ERR_INVALID_ARG, "%s: max_ctx %d does not fit %d blocks per sequence", who, max_ctx,
                 max_blocks_per_seq);
-  if (x == y) return fail(ctx, DS_ERR_INVALID_ARG, "ds_decode_step: y must not alias x");
+  if (x == y) return fail(ctx, DS_ERR_INVALID_ARG, "%s: y must not alias x", who);
   if (!aligned16(x) || !aligned16(y) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(workspace))
-    return fail(ctx, DS_ERR_INVALID_ARG, "ds_decode_step: pointers must be 16-byte aligned");
-  const size_t need = decode_least(ctx, B, max_ctx).all;
+    return fail(ctx, DS_ERR_INVALID_ARG, "%s: pointers must be 16-byte aligned", who);
+  const size_t need = cache.tiles ? tile_step_least(ctx, B, max_ctx, cache.max_prefix).all : decode_least(ctx, B, max_ctx).all;
   const DeviceState* dev = nullptr;
   if (use_static) {
     if (need > (size_t)DS_STATIC_SCRATCH_BYTES)
@@ -892,10 +1019,10 @@ static ds_status decode_step(ds_ctx* ctx, const ds_layer_weights* w, const void*
     workspace_bytes = (size_t)DS_STATIC_SCRATCH_BYTES;
   } else {
     if (!workspace || workspace_bytes < need)
-      return fail(ctx, DS_ERR_WORKSPACE, "ds_decode_step: workspace %zu < %zu", workspace_bytes, need);
+      return fail(ctx, DS_ERR_WORKSPACE, "%s: workspace %zu < %zu", who, workspace_bytes, need);
     if ((st = ensure_device(ctx)) != DS_OK) return st;
-    // Both entry points plan a step that either can run against the same size, and so give the same bits.
-    if (need <= (size_t)DS_STATIC_SCRATCH_BYTES && workspace_bytes > (size_t)DS_STATIC_SCRATCH_BYTES)
+    // ds_decode_step and ds_decode_step_static plan a step that either can run against the same size, and so give the same bits.
+    if (!cache.tiles && need <= (size_t)DS_STATIC_SCRATCH_BYTES && workspace_bytes > (size_t)DS_STATIC_SCRATCH_BYTES)
       workspace_bytes = (size_t)DS_STATIC_SCRATCH_BYTES;
   }
 
@@ -904,9 +1031,11 @@ static ds_status decode_step(ds_ctx* ctx, const ds_layer_weights* w, const void*
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (ctx->validate) {
     std::vector<int32_t> lens;
-    if ((st = validate_lens(ctx, "ds_decode_step", ctx_lens, B, 1, 1, max_ctx, s, lens)) != DS_OK) return st;
-    if ((st = validate_tables(ctx, "ds_decode_step", block_tables, B, max_blocks_per_seq, num_blocks, lens, s)) !=
-        DS_OK)
+    if ((st = validate_lens(ctx, who, ctx_lens, B, 1, cache.kv.type == ds::kKvBf16 ? 1 : 0, max_ctx, s, lens)) != DS_OK) return st;
+    if ((st = validate_tables(ctx, who, block_tables, B, max_blocks_per_seq, num_blocks, lens, s)) != DS_OK) return st;
+    if (cache.n_groups > 0 &&
+        (st = validate_groups(ctx, who, cache.cu_groups, cache.n_groups, cache.max_group_rows, B, cache.prefix_lens,
+                              cache.prefix_tables, cache.max_prefix_blocks, cache.max_prefix, num_blocks, s)) != DS_OK)
       return st;
   }
   Carver ws(workspace);
@@ -916,17 +1045,18 @@ static ds_status decode_step(ds_ctx* ctx, const ds_layer_weights* w, const void*
   const int hkv = kv_width(c), wqkv = qkv_width(c);
   void* qkv = ws.take((size_t)B * wqkv * 2);
   void* u = ws.take((size_t)B * m * 2);
-  const AttentionRoom att = attention_room(ctx, B, max_ctx);
+  const AttentionRoom att = cache.tiles ? AttentionRoom{0, 0} : attention_room(ctx, B, max_ctx);
   ws.take(att.least);
   void* sk = ws.take(0);
-  const int splits = ds::decode_attention_splits(B, c.n_heads, c.n_kv_heads, c.head_dim, max_ctx, att.all);
+  const int splits =
+      cache.tiles ? 1 : ds::decode_attention_splits(B, c.n_heads, c.n_kv_heads, c.head_dim, max_ctx, att.all);
   const size_t sk_bytes = workspace_bytes - ws.off;
 
   // The attention starts its longest sequences first; their order lies in x1 until the out-projection writes there.  It
   // is made beside LayerNorm's rows, so not where that is no launch of its own: a step of 64 sequences of 256 features
   // 25.7 -> 23.4 us at lengths of 300, 35.1 -> 33.0 at ragged ones, 32 of 512 features 37.7 -> 36.0.
   ds::LengthOrder by_length;
-  if (!norms_input(B, h, wqkv) &&
+  if (!cache.tiles && !norms_input(B, h, wqkv) &&
       ds::decode_attention_wants_order(B, c.n_heads, c.n_kv_heads, c.head_dim, splits))
     by_length = ds::LengthOrder{ctx_lens, static_cast<int32_t*>(x1), B};
   const uint16_t* qkv16 = static_cast<const uint16_t*>(qkv);
@@ -941,18 +1071,29 @@ static ds_status decode_step(ds_ctx* ctx, const ds_layer_weights* w, const void*
     fu.k_cache = k_cache; fu.v_cache = v_cache;
     fu.n_heads = c.n_heads; fu.n_kv_heads = c.n_kv_heads; fu.head_dim = c.head_dim;
     bool appended = false;
-    st = norm_and_linear(ctx, x, w->ln1_g, w->ln1_b, a, w->w_qkv, B, h, wqkv, ep, sk, sk_bytes, s, by_length, &fu,
-                         &appended);
+    const bool quant = cache.kv.type != ds::kKvBf16;  // (a row's scale needs the whole row: a launch of its own)
+    st = norm_and_linear(ctx, x, w->ln1_g, w->ln1_b, a, w->w_qkv, B, h, wqkv, ep, sk, sk_bytes, s, by_length,
+                         quant ? nullptr : &fu, quant ? nullptr : &appended);
     if (st != DS_OK) return st;
-    if (!appended)
+    if (quant)
+      DS_LAUNCH(ctx, s, DS_K_KV_APPEND,
+                ds::launch_kv_append_quant(qkv16 + h, qkv16 + h + hkv, wqkv, ctx_lens, block_tables, B, max_blocks_per_seq,
+                                           cache.kv, c.n_kv_heads, c.head_dim, s));
+    else if (!appended)
       DS_LAUNCH(ctx, s, DS_K_KV_APPEND,
                 ds::launch_kv_append(qkv16 + h, qkv16 + h + hkv, wqkv, ctx_lens, block_tables, B, max_blocks_per_seq,
                                      k_cache, v_cache, c.n_kv_heads, c.head_dim, s));
   }
-  DS_LAUNCH(ctx, s, DS_K_DECODE_ATTN,
+  if (cache.tiles) {
+    const ds::TileAttention t = tile_attention(ctx, cache, qkv, wqkv, ctx_lens, 1, block_tables, B, max_blocks_per_seq,
+                                               max_ctx, o, u);
+    DS_LAUNCH(ctx, s, DS_K_DECODE_ATTN, ds::launch_tile_attention(t, s));
+  } else {
+    DS_LAUNCH(ctx, s, DS_K_DECODE_ATTN,
             ds::launch_decode_attention(qkv, wqkv, ctx_lens, 1, block_tables, B, max_blocks_per_seq, max_ctx,
                                         k_cache, v_cache, c.n_heads, c.n_kv_heads, c.head_dim, splits, o, u, s,
                                         by_length.order));
+  }
   const bool fc1_norms = norms_input(B, h, m);
   {
     // x1 = x + o W_o^T + b_o, f = LN2(x1)
@@ -985,16 +1126,195 @@ ds_status ds_decode_step(ds_ctx* ctx, const ds_layer_weights* w, const void* x, 
                          const int32_t* block_tables, int32_t B, int32_t max_blocks_per_seq, int32_t max_ctx,
                          void* k_cache, void* v_cache, int32_t num_blocks, void* y, void* workspace,
                          size_t workspace_bytes, void* stream) {
-  return decode_step(ctx, w, x, ctx_lens, block_tables, B, max_blocks_per_seq, max_ctx, k_cache, v_cache,
-                     num_blocks, y, workspace, workspace_bytes, false, stream);
+  const StepCache cache{{k_cache, v_cache, nullptr, nullptr, ds::kKvBf16}, false};
+  return decode_step(ctx, w, x, ctx_lens, block_tables, B, max_blocks_per_seq, max_ctx, cache, num_blocks, y, workspace,
+                     workspace_bytes, false, stream);
 }
 
 ds_status ds_decode_step_static(ds_ctx* ctx, const ds_layer_weights* w, const void* x, const int32_t* ctx_lens,
                                 const int32_t* block_tables, int32_t B, int32_t max_blocks_per_seq,
                                 int32_t max_ctx, void* k_cache, void* v_cache, int32_t num_blocks, void* y,
                                 void* stream) {
-  return decode_step(ctx, w, x, ctx_lens, block_tables, B, max_blocks_per_seq, max_ctx, k_cache, v_cache,
-                     num_blocks, y, nullptr, 0, true, stream);
+  const StepCache cache{{k_cache, v_cache, nullptr, nullptr, ds::kKvBf16}, false};
+  return decode_step(ctx, w, x, ctx_lens, block_tables, B, max_blocks_per_seq, max_ctx, cache, num_blocks, y, nullptr, 0,
+                     true, stream);
+}
+
+// ---- pages of 8 bits, prefixes that rows share ----
+
+// From these sizes on every product of such a step has its fastest plan.
+size_t ds_decode_quant_workspace_bytes(const ds_ctx* ctx, int32_t max_batch, int32_t max_ctx) {
+  if (!ctx || max_batch <= 0 || max_ctx <= 0) return 0;
+  return full_ws(ctx, max_batch, tile_step_least(ctx, max_batch, max_ctx, 0));
+}
+
+size_t ds_decode_shared_workspace_bytes(const ds_ctx* ctx, int32_t max_batch, int32_t max_prefix_len, int32_t max_ctx) {
+  if (!ctx || max_batch <= 0 || max_ctx <= 0 || max_prefix_len <= 0) return 0;
+  return full_ws(ctx, max_batch, tile_step_least(ctx, max_batch, max_ctx, max_prefix_len));
+}
+
+ds_status ds_kv_migrate_quant(ds_ctx* ctx, const void* k_src, const void* v_src, const int32_t* cu_seqlens, int32_t B,
+                              int32_t t, int32_t max_seqlen, const int32_t* block_tables, int32_t max_blocks_per_seq,
+                              void* k_cache, void* v_cache, void* k_scale, void* v_scale, int32_t num_blocks,
+                              int32_t kv_type, void* stream) {
+  const char* who = "ds_kv_migrate_quant";
+  if (!ctx) return DS_ERR_INVALID_ARG;
+  if (ds_status st = check_rows(ctx, who, k_src, v_src, cu_seqlens, B, t, max_seqlen, block_tables, max_blocks_per_seq)) return st;
+  if (ds_status st = check_cache(ctx, who, k_cache, v_cache, k_scale, v_scale, num_blocks, kv_type, false)) return st;
+  if (ds_status st = ensure_device(ctx)) return st;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (ctx->validate)
+    if (ds_status st = validate_rows(ctx, who, cu_seqlens, B, t, max_seqlen, block_tables, max_blocks_per_seq, num_blocks, s))
+      return st;
+  const ds::KvCache cache{k_cache, v_cache, k_scale, v_scale, kv_type};
+  DS_LAUNCH(ctx, s, DS_K_KV_MIGRATE,
+            ds::launch_kv_migrate_quant(k_src, v_src, cu_seqlens, B, max_seqlen, block_tables, max_blocks_per_seq, cache,
+                                        ctx->cfg.n_kv_heads, ctx->cfg.head_dim, s));
+  return DS_OK;
+}
+
+ds_status ds_kv_read_quant(ds_ctx* ctx, const int32_t* cu_seqlens, int32_t B, int32_t t, int32_t max_seqlen,
+                           const int32_t* block_tables, int32_t max_blocks_per_seq, const void* k_cache,
+                           const void* v_cache, const void* k_scale, const void* v_scale, int32_t num_blocks,
+                           int32_t kv_type, void* k_dst, void* v_dst, void* stream) {
+  const char* who = "ds_kv_read_quant";
+  if (!ctx) return DS_ERR_INVALID_ARG;
+  if (ds_status st = check_rows(ctx, who, k_dst, v_dst, cu_seqlens, B, t, max_seqlen, block_tables, max_blocks_per_seq)) return st;
+  if (ds_status st = check_cache(ctx, who, k_cache, v_cache, k_scale, v_scale, num_blocks, kv_type, false)) return st;
+  if (ds_status st = ensure_device(ctx)) return st;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (ctx->validate)
+    if (ds_status st = validate_rows(ctx, who, cu_seqlens, B, t, max_seqlen, block_tables, max_blocks_per_seq, num_blocks, s))
+      return st;
+  const ds::KvCache cache{const_cast<void*>(k_cache), const_cast<void*>(v_cache), const_cast<void*>(k_scale),
+                          const_cast<void*>(v_scale), kv_type};
+  DS_LAUNCH(ctx, s, DS_K_KV_MIGRATE,
+            ds::launch_kv_read_quant(cu_seqlens, B, max_seqlen, block_tables, max_blocks_per_seq, cache,
+                                     ctx->cfg.n_kv_heads, ctx->cfg.head_dim, k_dst, v_dst, s));
+  return DS_OK;
+}
+
+ds_status ds_kv_append_quant(ds_ctx* ctx, const void* k_new, const void* v_new, int32_t row_stride,
+                             const int32_t* ctx_lens, const int32_t* block_tables, int32_t B, int32_t max_blocks_per_seq,
+                             void* k_cache, void* v_cache, void* k_scale, void* v_scale, int32_t num_blocks,
+                             int32_t kv_type, void* stream) {
+  const char* who = "ds_kv_append_quant";
+  if (!ctx) return DS_ERR_INVALID_ARG;
+  if (!k_new || !v_new || !ctx_lens || !block_tables) return fail(ctx, DS_ERR_INVALID_ARG, "%s: NULL pointer", who);
+  if (B <= 0 || max_blocks_per_seq <= 0 || row_stride < kv_width(ctx->cfg) || row_stride % 8 != 0)
+    return fail(ctx, DS_ERR_INVALID_ARG, "%s: non-positive size, or a row stride that is below n_kv s or no multiple of 8", who);
+  if (!aligned16(k_new) || !aligned16(v_new))
+    return fail(ctx, DS_ERR_INVALID_ARG, "%s: pointers must be 16-byte aligned", who);
+  if (ds_status st = check_cache(ctx, who, k_cache, v_cache, k_scale, v_scale, num_blocks, kv_type, false)) return st;
+  if (ds_status st = ensure_device(ctx)) return st;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (ctx->validate) {
+    std::vector<int32_t> lens;
+    const int most = (int)std::min<int64_t>((int64_t)max_blocks_per_seq * ctx->cfg.block_size, INT32_MAX);
+    if (ds_status st = validate_lens(ctx, who, ctx_lens, B, 1, 0, most, s, lens)) return st;
+    if (ds_status st = validate_tables(ctx, who, block_tables, B, max_blocks_per_seq, num_blocks, lens, s)) return st;
+  }
+  const ds::KvCache cache{k_cache, v_cache, k_scale, v_scale, kv_type};
+  DS_LAUNCH(ctx, s, DS_K_KV_APPEND,
+            ds::launch_kv_append_quant(k_new, v_new, row_stride, ctx_lens, block_tables, B, max_blocks_per_seq, cache,
+                                       ctx->cfg.n_kv_heads, ctx->cfg.head_dim, s));
+  return DS_OK;
+}
+
+// ds_decode_attention_quant and ds_decode_attention_shared
+static ds_status paged_attention(ds_ctx* ctx, const char* who, const void* q, const StepCache& cache, const int32_t* kv_lens,
+                                 const int32_t* block_tables, int32_t B, int32_t max_blocks_per_seq, int32_t max_kv_len,
+                                 int32_t num_blocks, void* o, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!q || !kv_lens || !block_tables || !o) return fail(ctx, DS_ERR_INVALID_ARG, "%s: NULL pointer", who);
+  if (B <= 0 || max_kv_len <= 0 || max_blocks_per_seq <= 0 ||
+      (int64_t)max_blocks_per_seq * ctx->cfg.block_size < max_kv_len)
+    return fail(ctx, DS_ERR_INVALID_ARG, "%s: non-positive or inconsistent size", who);
+  if (!aligned16(q) || !aligned16(o) || !aligned16(workspace))
+    return fail(ctx, DS_ERR_INVALID_ARG, "%s: pointers must be 16-byte aligned", who);
+  const ds_model_cfg& c = ctx->cfg;
+  const ds::TileAttention t = tile_attention(ctx, cache, q, c.hidden, kv_lens, 0, block_tables, B, max_blocks_per_seq,
+                                             max_kv_len, o, workspace);
+  const size_t need = ds::tile_states_bytes(B, c.n_heads, c.head_dim, t.plan.own + t.plan.prefix);
+  if (need > 0 && (!workspace || workspace_bytes < need))
+    return fail(ctx, DS_ERR_WORKSPACE, "%s: workspace %zu < %zu", who, workspace_bytes, need);
+  if (ds_status st = ensure_device(ctx)) return st;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (ctx->validate) {
+    std::vector<int32_t> lens;
+    if (ds_status st = validate_lens(ctx, who, kv_lens, B, 0, 0, max_kv_len, s, lens)) return st;
+    if (ds_status st = validate_tables(ctx, who, block_tables, B, max_blocks_per_seq, num_blocks, lens, s)) return st;
+    if (cache.n_groups > 0)
+      if (ds_status st = validate_groups(ctx, who, cache.cu_groups, cache.n_groups, cache.max_group_rows, B,
+                                         cache.prefix_lens, cache.prefix_tables, cache.max_prefix_blocks, cache.max_prefix,
+                                         num_blocks, s))
+        return st;
+  }
+  DS_LAUNCH(ctx, s, DS_K_DECODE_ATTN, ds::launch_tile_attention(t, s));
+  return DS_OK;
+}
+
+ds_status ds_decode_attention_quant(ds_ctx* ctx, const void* q, const int32_t* kv_lens, const int32_t* block_tables,
+                                    int32_t B, int32_t max_blocks_per_seq, int32_t max_kv_len, const void* k_cache,
+                                    const void* v_cache, const void* k_scale, const void* v_scale, int32_t num_blocks,
+                                    int32_t kv_type, void* o, void* workspace, size_t workspace_bytes, void* stream) {
+  const char* who = "ds_decode_attention_quant";
+  if (!ctx) return DS_ERR_INVALID_ARG;
+  if (ds_status st = check_cache(ctx, who, k_cache, v_cache, k_scale, v_scale, num_blocks, kv_type, false)) return st;
+  const StepCache cache{{const_cast<void*>(k_cache), const_cast<void*>(v_cache), const_cast<void*>(k_scale),
+                         const_cast<void*>(v_scale), kv_type}, true};
+  return paged_attention(ctx, who, q, cache, kv_lens, block_tables, B, max_blocks_per_seq, max_kv_len, num_blocks, o,
+                         workspace, workspace_bytes, stream);
+}
+
+ds_status ds_decode_attention_shared(ds_ctx* ctx, const void* q, const int32_t* cu_groups, int32_t n_groups,
+                                     int32_t max_group_rows, const int32_t* prefix_lens, const int32_t* prefix_tables,
+                                     int32_t max_prefix_blocks, int32_t max_prefix_len, const int32_t* kv_lens,
+                                     const int32_t* block_tables, int32_t B, int32_t max_blocks_per_seq,
+                                     int32_t max_kv_len, const void* k_cache, const void* v_cache, const void* k_scale,
+                                     const void* v_scale, int32_t num_blocks, int32_t kv_type, void* o, void* workspace,
+                                     size_t workspace_bytes, void* stream) {
+  const char* who = "ds_decode_attention_shared";
+  if (!ctx) return DS_ERR_INVALID_ARG;
+  if (ds_status st = check_cache(ctx, who, k_cache, v_cache, k_scale, v_scale, num_blocks, kv_type, true)) return st;
+  if (ds_status st = check_groups(ctx, who, cu_groups, n_groups, max_group_rows, prefix_lens, prefix_tables,
+                                  max_prefix_blocks, max_prefix_len, B))
+    return st;
+  const StepCache cache{{const_cast<void*>(k_cache), const_cast<void*>(v_cache), const_cast<void*>(k_scale),
+                         const_cast<void*>(v_scale), kv_type}, true, cu_groups, prefix_lens, prefix_tables, n_groups,
+                        max_group_rows, max_prefix_blocks, max_prefix_len};
+  return paged_attention(ctx, who, q, cache, kv_lens, block_tables, B, max_blocks_per_seq, max_kv_len, num_blocks, o,
+                         workspace, workspace_bytes, stream);
+}
+
+ds_status ds_decode_step_quant(ds_ctx* ctx, const ds_layer_weights* w, const void* x, const int32_t* ctx_lens,
+                               const int32_t* block_tables, int32_t B, int32_t max_blocks_per_seq, int32_t max_ctx,
+                               void* k_cache, void* v_cache, void* k_scale, void* v_scale, int32_t num_blocks,
+                               int32_t kv_type, void* y, void* workspace, size_t workspace_bytes, void* stream) {
+  const char* who = "ds_decode_step_quant";
+  if (!ctx) return DS_ERR_INVALID_ARG;
+  if (ds_status st = check_cache(ctx, who, k_cache, v_cache, k_scale, v_scale, num_blocks, kv_type, false)) return st;
+  const StepCache cache{{k_cache, v_cache, k_scale, v_scale, kv_type}, true};
+  return decode_step(ctx, w, x, ctx_lens, block_tables, B, max_blocks_per_seq, max_ctx, cache, num_blocks, y, workspace,
+                     workspace_bytes, false, stream, who);
+}
+
+ds_status ds_decode_step_shared(ds_ctx* ctx, const ds_layer_weights* w, const void* x, const int32_t* cu_groups,
+                                int32_t n_groups, int32_t max_group_rows, const int32_t* prefix_lens,
+                                const int32_t* prefix_tables, int32_t max_prefix_blocks, int32_t max_prefix_len,
+                                const int32_t* ctx_lens, const int32_t* block_tables, int32_t B,
+                                int32_t max_blocks_per_seq, int32_t max_ctx, void* k_cache, void* v_cache, void* k_scale,
+                                void* v_scale, int32_t num_blocks, int32_t kv_type, void* y, void* workspace,
+                                size_t workspace_bytes, void* stream) {
+  const char* who = "ds_decode_step_shared";
+  if (!ctx) return DS_ERR_INVALID_ARG;
+  if (ds_status st = check_cache(ctx, who, k_cache, v_cache, k_scale, v_scale, num_blocks, kv_type, true)) return st;
+  if (ds_status st = check_groups(ctx, who, cu_groups, n_groups, max_group_rows, prefix_lens, prefix_tables,
+                                  max_prefix_blocks, max_prefix_len, B))
+    return st;
+  const StepCache cache{{k_cache, v_cache, k_scale, v_scale, kv_type}, true, cu_groups, prefix_lens, prefix_tables,
+                        n_groups, max_group_rows, max_prefix_blocks, max_prefix_len};
+  return decode_step(ctx, w, x, ctx_lens, block_tables, B, max_blocks_per_seq, max_ctx, cache, num_blocks, y, workspace,
+                     workspace_bytes, false, stream, who);
 }
 
 ds_status ds_profile_enable(ds_ctx* ctx, int32_t on) {

@@ -173,4 +173,45 @@ hipError_t launch_decode_attention(const void* q, int q_stride, const int32_t* k
                                    int head_dim, int splits, void* o, void* workspace, hipStream_t stream,
                                    const int32_t* order = nullptr);
 
+// A layer's paged cache: bf16 (no scales), or one of the 8-bit forms of kv_quant.h.
+enum KvType { kKvBf16 = 0, kKvE4m3 = 1, kKvInt8 = 2 };
+struct KvCache {
+  void *k, *v;
+  void *k_scale, *v_scale;
+  int type;  // KvType
+};
+
+// contiguous [t, n, s] -> pages of 8 bits; pages -> contiguous rows; new rows (row stride `row_stride` elements) of B
+// sequences -> slot ctx_lens[i] (negative: none).
+hipError_t launch_kv_migrate_quant(const void* k_src, const void* v_src, const int32_t* cu_seqlens, int B, int max_seqlen,
+                                   const int32_t* block_tables, int max_blocks, const KvCache& cache, int n_heads,
+                                   int head_dim, hipStream_t stream);
+hipError_t launch_kv_read_quant(const int32_t* cu_seqlens, int B, int max_seqlen, const int32_t* block_tables,
+                                int max_blocks, const KvCache& cache, int n_heads, int head_dim, void* k_dst, void* v_dst,
+                                hipStream_t stream);
+hipError_t launch_kv_append_quant(const void* k_new, const void* v_new, int row_stride, const int32_t* ctx_lens,
+                                  const int32_t* block_tables, int B, int max_blocks, const KvCache& cache, int n_heads,
+                                  int head_dim, hipStream_t stream);
+
+// One query per (sequence, head) over pages, on the matrix cores whatever the number of heads: over the sequence's own
+// pages, and before them, where n_groups > 0, over the prefix of its group (rows [cu_groups[i], cu_groups[i + 1])).
+struct TilePlan {
+  int prefix = 0, own = 1;  // splits of the prefixes' (up to max_prefix tokens; 0: there are none) and of the own pages
+};
+TilePlan tile_plan(int B, int n_heads, int n_kv_heads, int max_len, int max_prefix);
+size_t tile_states_bytes(int B, int n_heads, int head_dim, int states);
+struct TileAttention {
+  const void* q;
+  int q_stride;
+  const int32_t *cu_groups, *prefix_lens, *prefix_tables;
+  int n_groups, max_rows, max_prefix_pages, max_prefix;
+  const int32_t *kv_lens, *block_tables;
+  int kv_len_add, B, max_blocks, max_kv_len;
+  KvCache cache;
+  int n_heads, n_kv_heads, head_dim;
+  TilePlan plan;
+  void *o, *states;
+};
+hipError_t launch_tile_attention(const TileAttention& t, hipStream_t stream);
+
 }  // namespace ds

@@ -122,7 +122,10 @@ struct Entry<ds_status(A...)> {
 PyMethodDef entries[] = {DS_ENTRY(ds_prefill),          DS_ENTRY(ds_kv_migrate),        DS_ENTRY(ds_decode_step),
                          DS_ENTRY(ds_decode_step_static), DS_ENTRY(ds_layernorm),      DS_ENTRY(ds_linear),
                          DS_ENTRY(ds_prefill_attention), DS_ENTRY(ds_decode_attention), DS_ENTRY(ds_embed),
-                         DS_ENTRY(ds_next_token)};
+                         DS_ENTRY(ds_next_token),       DS_ENTRY(ds_kv_migrate_quant),  DS_ENTRY(ds_kv_read_quant),
+                         DS_ENTRY(ds_kv_append_quant),  DS_ENTRY(ds_decode_attention_quant),
+                         DS_ENTRY(ds_decode_attention_shared), DS_ENTRY(ds_decode_step_quant),
+                         DS_ENTRY(ds_decode_step_shared)};
 
 // bind(name, address, LayerWeights) -> the entry point of that name whose code lies at `address`
 PyObject* bind(PyObject*, PyObject* args) {
