@@ -1,23 +1,23 @@
 // Attention of single queries over pages in tiles of the matrix cores: over the paged cache of 8 bits, and over a prefix
-// whose pages several sequences share (in any of the three forms of the cache).
+// whose pages several sequences share (in any of the three forms of the cache) together with the sequences' own pages.
 //
-// The 16 columns of a tile are queries of one key/value head: the query heads that share it, of one sequence or, for a
+// The columns of a tile are queries of one key/value head: the query heads that share it, of one sequence or, for a
 // prefix, of all rows of the group that shares the pages.  Per 16 x 16 x 32 instruction
 //   scores  S[key, column]  = K[key, :] . Q[column, :]        operand A = 16 keys, operand B = 16 columns
 //   output  O^T[d, column] += V^T[d, key] . P[key, column]    operand A = 16 features, operand B = P
 // In the result of the first a lane has one column (lane % 16) and 4 keys, so the softmax's running maximum and sum are
 // scalars of a lane; with the keys dealt out as below the probabilities are already the second product's operand B.
-//
-// A workgroup of 4 waves takes one (group, key/value head, NC tiles of columns, split of the pages); its waves take turns
-// by chunks of 64 (8 bits) or 32 keys (bf16), and their states (maximum, sum, output) are merged through LDS.
-//   8 bits: a chunk is 4 pages, g = lane / 16 is the lane's page.  Row i of score tile t is key 4 t + i % 4 of page i / 4, so
-// the lane's results are all 16 keys of page g.  V is kept with a feature's 16 tokens together: 16 bytes are the lane's
-// operand for 16 keys of page g.  Values go to bf16 exactly; the scales of K multiply the scores, those of V the
-// probabilities (in fp32, by a DPP operand: lane 16 g + j has the scale of key j).
-//   bf16: a chunk is 2 pages, row i of score tile t is key i of page t; V goes through LDS, where the transposing read
-// makes the operand.
-// Probabilities are rounded to bf16 for the second product (at most 2^-9 of each, in no one direction); the sum is that of
+// Values of 8 bits go to bf16 exactly; the scales of K multiply the scores, those of V the probabilities, in fp32.
+// Probabilities are rounded to bf16 for the second product (at most 2^-8 of each, in no one direction); the sum is that of
 // the unrounded ones.
+//
+// A launch has up to two parts, the groups' prefixes and the rows' own pages, and a workgroup of 4 waves takes one
+// (group, key/value head, block of columns, split of the pages) of either part:
+//  * narrow, up to 16 columns: the waves take turns by chunks of 32 keys, from global memory straight to registers, and
+//    their states (maximum, sum, output) are merged through LDS.  HBM bounds it.
+//  * wide, 64 columns: each wave has 16 of them, and all see the same tiles of 32 keys, which the workgroup brings to bf16
+//    and into LDS once.
+// Where a (row, head) has more than one state, they are written out in fp32 and a second launch merges them in order.
 #include <algorithm>
 #include <type_traits>
 
@@ -26,23 +26,33 @@
 namespace ds {
 
 constexpr int kTileThreads = 256, kTileWaves = 4;
+constexpr int kWideCols = 64, kNarrowCols = 16;
 
-struct TileArgs {
-  const uint16_t* q;
-  int q_stride;
+struct TilePart {
   const int32_t* cu_rows;  // group i has the rows [cu_rows[i], cu_rows[i + 1]); null: row i
   const int32_t* lens;
-  int len_add;
   const int32_t* tables;
-  int max_pages;
+  int len_add, max_pages, groups;
+  int blocks_x;            // key/value heads x blocks of columns
+  int pages_per_split;
+  int first_state;         // states of this part's splits
+  int wide, rank;          // rank: longest groups first
+};
+
+struct TileArgs {
+  TilePart part[2];
+  int first_blocks;  // workgroups of part 0
+  const uint16_t* q;
+  int q_stride;
   const void *k, *v;
   const uint16_t *k_scale, *v_scale;
-  int n_heads, n_kv_heads, pages_per_split;
-  int first_state, n_states;  // a (row, head) has n_states states, this launch's from first_state on; 1: o is written
+  int n_heads, n_kv_heads;
+  int n_states;      // of a (row, head); 1: o is written
   float scale_log2e;
   uint16_t* o;
-  float* partial;  // [row][head][state][max, sum, output[HD]]
+  float* partial;    // [row][head][state][output[HD], max, sum, -, -]
 };
+constexpr int kStatePad = 4;
 
 // v of lane 16 (lane / 16) + J
 template <int J>
@@ -57,330 +67,660 @@ __device__ __forceinline__ void each(std::integer_sequence<int, J...>, F&& f) {
 __device__ __forceinline__ floatx4 mfma(u32x4 a, u32x4 b, floatx4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
+template <bool ONCE>
+__device__ __forceinline__ u32x4 ld16_kv(const void* p) {
+  if constexpr (ONCE) return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
+  else return ld16(p);
+}
 
-template <int HD, int T>
-struct Tiles {
-  static constexpr bool kQuant = T != kKvBf16;
-  static constexpr int kPages = kQuant ? 4 : 2;       // of a chunk
-  static constexpr int kTilesS = kPages;              // score tiles of 16 keys
-  static constexpr int kSteps = HD / 32;              // instructions per score tile
-  static constexpr int kVRow = HD + 16;               // LDS row of a staged V page (bf16): 8 banks further than the last
-  static constexpr int kStage = kQuant ? 0 : 2 * kKvPage * kVRow * 2;  // bytes of a wave
-  static constexpr int kMerge = kTileWaves * 16 * (HD + 2) * 4;
-  static constexpr int kLds = kTileWaves * kStage > kMerge ? kTileWaves * kStage : kMerge;
+// One workgroup's share: a group's pages [lo, hi) of a key/value head, for some of the group's columns.
+struct TileWork {
+  int kv, row0, c0, cols, state, len, lo, hi;
+  const int32_t* bt;
 };
 
-template <int HD, int T, int NC>
-__global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(2))) void tile_attention_kernel(
-    const TileArgs a) {
-  using C = Tiles<HD, T>;
-  constexpr int DB = HD / 16;
-  __shared__ __attribute__((aligned(16))) unsigned char smem[C::kLds];
-  const int G = a.n_heads / a.n_kv_heads;
-  const int kv = blockIdx.x % a.n_kv_heads, c0 = blockIdx.x / a.n_kv_heads * (16 * NC);
-  const int group = blockIdx.y, split = blockIdx.z;
-  const int row0 = a.cu_rows ? a.cu_rows[group] : group;
-  const int cols = (a.cu_rows ? a.cu_rows[group + 1] - row0 : 1) * G;
-  if (c0 >= cols) return;
-  const int tid = threadIdx.x, lane = tid & 63, hl = lane & 15, g = lane >> 4;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int len = a.lens[group] + a.len_add;
-  const int n_pages = (len + kKvPage - 1) / kKvPage;
-  const int page_lo = split * a.pages_per_split, page_hi = min(n_pages, page_lo + a.pages_per_split);
-  const int32_t* bt = a.tables + (size_t)group * a.max_pages;
-
-  // operand B of the scores.  8 bits: instruction 2 c + h takes features 64 c + 16 g + 8 h .. + 8 of lane group g (16 bytes of
-  // K are two operands); bf16: instruction s features 32 s + 8 g .. + 8.
-  u32x4 qf[NC][C::kSteps];
-#pragma unroll
-  for (int t = 0; t < NC; ++t) {
-    const int col = c0 + 16 * t + hl;
-    const uint16_t* qp = a.q + (size_t)(row0 + col / G) * a.q_stride + (size_t)(kv * G + col % G) * HD;
-#pragma unroll
-    for (int s = 0; s < C::kSteps; ++s) {
-      qf[t][s] = u32x4{0, 0, 0, 0};
-      const int at = C::kQuant ? 64 * (s / 2) + 16 * g + 8 * (s % 2) : 32 * s + 8 * g;
-      if (col < cols) qf[t][s] = ld16(qp + at);
+// The r-th longest (by pages, then by number) of up to 64 sequences, one a lane (pages < 0: none): a lane's number.
+__device__ __forceinline__ int ranked(int pages, int r, int bits) {
+  uint64_t left = __builtin_amdgcn_ballot_w64(pages >= 0);
+  for (int b = bits - 1; b >= 0; --b) {
+    const uint64_t with = __builtin_amdgcn_ballot_w64((pages >> b) & 1) & left;
+    const int n = __builtin_popcountll(with);
+    if (r < n) left = with;
+    else {
+      r -= n;
+      left &= ~with;
     }
   }
-  floatx4 acc[NC][DB];
-  float m_run[NC], l_run[NC];  // l_run: this lane's share of the sum
-#pragma unroll
-  for (int t = 0; t < NC; ++t) {
-    m_run[t] = -INFINITY;
-    l_run[t] = 0.f;
-#pragma unroll
-    for (int db = 0; db < DB; ++db) acc[t][db] = floatx4{0.f, 0.f, 0.f, 0.f};
-  }
+  const int before = __builtin_amdgcn_mbcnt_hi((uint32_t)(left >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)left, 0));
+  const int lane = threadIdx.x & 63;
+  return __builtin_ctzll(__builtin_amdgcn_ballot_w64(((left >> lane) & 1) && before == r));
+}
 
-  // Softmax over a chunk's scores (scaled, -inf where there is no key): new maximum, old results rescaled, p in place of s.
-  auto softmax = [&](int t, auto& s) {
-    float top = -INFINITY;
+// Running softmax over two score tiles (scaled by log2 e, -inf where there is no key): p in place of s.
+template <int DB>
+__device__ __forceinline__ void online_softmax(floatx4 (&s)[2], floatx4 (&acc)[DB], float& m_run, float& l_run) {
+  float top = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < C::kTilesS; ++i)
+  for (int i = 0; i < 2; ++i)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) top = fmaxf(top, s[i][r]);
-    top = across_groups<16>(top, MaxOp());
-    const float m_new = fmaxf(m_run[t], top);
-    const float alpha = __builtin_amdgcn_exp2f(m_run[t] - m_new);
-    float sum = 0.f;
+    for (int r = 0; r < 4; ++r) top = fmaxf(top, s[i][r]);
+  top = across_groups<16>(top, MaxOp());
+  if (__builtin_amdgcn_ballot_w64(top > m_run) != 0) {  // (rare from the first few tiles on)
+    const float m_new = fmaxf(m_run, top);
+    const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+    l_run *= alpha;
+    m_run = m_new;
 #pragma unroll
-    for (int i = 0; i < C::kTilesS; ++i)
+    for (int db = 0; db < DB; ++db) acc[db] *= alpha;
+  }
+  float sum = 0.f;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        s[i][r] = __builtin_amdgcn_exp2f(s[i][r] - m_new);
-        sum += s[i][r];
-      }
-    l_run[t] = l_run[t] * alpha + sum;
-    m_run[t] = m_new;
+  for (int i = 0; i < 2; ++i)
 #pragma unroll
-    for (int db = 0; db < DB; ++db) acc[t][db] *= alpha;
+    for (int r = 0; r < 4; ++r) {
+      s[i][r] = __builtin_amdgcn_exp2f(s[i][r] - m_run);
+      sum += s[i][r];
+    }
+  l_run += sum;
+}
+__device__ __forceinline__ u32x4 probabilities(const floatx4 (&s)[2]) {
+  u32x4 p;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) p[w] = pack_bf16(s[w / 2][2 * (w % 2)], s[w / 2][2 * (w % 2) + 1]);
+  return p;
+}
+template <int T>
+__device__ __forceinline__ u32x4 values8(uint32_t a, uint32_t b) {
+  const u32x2 lo = values4<T>(a), hi = values4<T>(b);
+  return u32x4{lo[0], lo[1], hi[0], hi[1]};
+}
+
+// V of bf16 in LDS as it lies in the page: rows 8 banks apart (mod 64) and 16 elements longer than a row, so that the
+// transposing reads of half a wave (4 rows of 32 bytes for each of two lane groups, 4 rows apart) meet in no bank.
+template <int HD>
+constexpr int kVRow = HD + 16;
+// Operand A of the second product out of it: lane i of a group of 16 hands in 4 features of key i / 4 and is handed the 4
+// keys of feature i; keys 4 g .. 4 g + 3 of two pages.
+template <int HD>
+__device__ __forceinline__ u32x4 turned(const uint16_t* vfrag, int db) {
+  typedef short short4v __attribute__((ext_vector_type(4)));
+  typedef __attribute__((address_space(3))) short4v* lds_short4_ptr;
+  const u32x2 p0 = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_ptr)(vfrag + 16 * db)));
+  const u32x2 p1 = __builtin_bit_cast(
+      u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_ptr)(vfrag + kKvPage * kVRow<HD> + 16 * db)));
+  return u32x4{p0[0], p0[1], p1[0], p1[1]};
+}
+
+// bytes of LDS: a tile of K and of V, twice (wide); the staging areas of the waves (narrow, bf16); the merge (narrow)
+template <int HD, int T, bool WIDE>
+struct TileLds {
+  static constexpr int kK = 32 * HD * 2, kV = T == kKvBf16 ? 32 * kVRow<HD> * 2 : 32 * HD * 2;
+  static constexpr int kTile = kK + kV + (T == kKvBf16 ? 0 : 2 * 32 * 4);
+  static constexpr int kStage = T == kKvBf16 ? 32 * kVRow<HD> * 2 : 0;
+  static constexpr int kMerge = kTileWaves * 16 * (HD + kStatePad) * 4;
+  static constexpr int most(int a, int b) { return a > b ? a : b; }
+  static constexpr int kBytes = most(WIDE ? 2 * kTile : 0, most(kTileWaves * kStage, kMerge));
+};
+
+// ---- narrow ----
+// 8 bits: of a chunk's 32 keys lane group g has keys 8 (g & 1) .. + 8 of page g / 2: row i of score tile t is key
+// 8 (i / 4 & 1) + 4 t + i % 4 of page i / 8.  V is kept with a feature's 16 tokens together: a 16-byte load and two row
+// swaps give 8 keys of two blocks of features, operand A as it is wanted.
+//   K is asked for one chunk ahead when this one's scores are made, V when its output is: 16 registers each.  (A chunk of 64
+// keys has twice those and half the waves: 40 heads, 64 sequences of 545 tokens 76 -> 71 us.)  Loads that no cache keeps,
+// where the caches could not keep them: 71 -> 66.
+template <int HD, int T, bool ONCE>
+__device__ __forceinline__ void narrow_quant(const TileArgs& a, const TileWork& w, const u32x4 (&qf)[HD / 32],
+                                             floatx4 (&acc)[HD / 16], float& m_run, float& l_run) {
+  constexpr int KL = HD / 64, VL = HD / 32;  // 16-byte loads of a key, of a chunk's V, per lane
+  constexpr int kStep = 2 * kTileWaves;
+  const int lane = threadIdx.x & 63, hl = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint8_t* kc = static_cast<const uint8_t*>(a.k);
+  const uint8_t* vc = static_cast<const uint8_t*>(a.v);
+  int kid = 0, vid = 0;
+  auto ids = [&](int p) {  // pages of the lane as a row of K and as a column of V (behind the last: the last, without keys)
+    kid = w.bt[min(p + (hl >> 3), w.hi - 1)];
+    vid = w.bt[min(p + (g >> 1), w.hi - 1)];
   };
-
-  if constexpr (C::kQuant) {
-    const uint8_t* kc = static_cast<const uint8_t*>(a.k);
-    const uint8_t* vc = static_cast<const uint8_t*>(a.v);
-    constexpr int KL = HD / 64;  // 16-byte loads of a key per lane
-    for (int pg = page_lo + 4 * wave; pg < page_hi; pg += 4 * kTileWaves) {
-      // pages of the lane: hl / 4 as a row of K, g as a column of V (behind the last: the last again, without keys)
-      const size_t kp = (size_t)bt[min(pg + (hl >> 2), page_hi - 1)] * a.n_kv_heads + kv;
-      const size_t vp = (size_t)bt[min(pg + g, page_hi - 1)] * a.n_kv_heads + kv;
-      const int there = pg + g < page_hi ? min(len - (pg + g) * kKvPage, kKvPage) : 0;  // keys of the lane's page
-      u32x4 kr[4][KL], vr[DB];
+  u32x4 kr[2][KL], vr[VL];
+  uint16_t ksr, vsr;
+  const uint8_t* vsrc;
+  auto fetch_k = [&] {
+    const size_t kp = (size_t)kid * a.n_kv_heads + w.kv, vp = (size_t)vid * a.n_kv_heads + w.kv;
+    const uint8_t* src = kc + kp * (kKvPage * HD) + (8 * ((hl >> 2) & 1) + (hl & 3)) * HD + 16 * g;
 #pragma unroll
-      for (int t = 0; t < 4; ++t)
+    for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int c = 0; c < KL; ++c) kr[t][c] = ld16(kc + (kp * kKvPage + 4 * t + (hl & 3)) * HD + 64 * c + 16 * g);
+      for (int c = 0; c < KL; ++c) kr[t][c] = ld16_kv<ONCE>(src + 4 * t * HD + 64 * c);
+    const size_t sc = vp * kKvPage + 8 * (g & 1) + (hl & 7);
+    ksr = a.k_scale[sc];
+    vsr = a.v_scale[sc];
+    vsrc = vc + vp * (kKvPage * HD) + (16 * (g & 1) + hl) * kKvPage;
+  };
+  auto fetch_v = [&] {
 #pragma unroll
-      for (int db = 0; db < DB; ++db) vr[db] = ld16(vc + (vp * HD + 16 * db + hl) * kKvPage);
-      const float ks = bf16_lo(a.k_scale[vp * kKvPage + hl]) * a.scale_log2e;
-      const float vs = hl < there ? bf16_lo(a.v_scale[vp * kKvPage + hl]) : 0.f;
-
-      floatx4 s[NC][4];
-#pragma unroll
-      for (int t = 0; t < 4; ++t) {
-#pragma unroll
-        for (int n = 0; n < NC; ++n) s[n][t] = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int c = 0; c < KL; ++c)
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const u32x2 lo = values4<T>(kr[t][c][2 * h]), hi = values4<T>(kr[t][c][2 * h + 1]);
-            const u32x4 kf = {lo[0], lo[1], hi[0], hi[1]};
-#pragma unroll
-            for (int n = 0; n < NC; ++n) s[n][t] = mfma(kf, qf[n][2 * c + h], s[n][t]);
-          }
-      }
-      u32x4 pf[NC][2];
-#pragma unroll
-      for (int n = 0; n < NC; ++n) {
-        each(std::make_integer_sequence<int, 16>{}, [&](auto j) {
-          const float x = s[n][j() / 4][j() % 4] * row_lane<j()>(ks);
-          s[n][j() / 4][j() % 4] = j() < there ? x : -INFINITY;  // (whatever the slot holds)
-        });
-        softmax(n, s[n]);
-        each(std::make_integer_sequence<int, 16>{}, [&](auto j) { s[n][j() / 4][j() % 4] *= row_lane<j()>(vs); });
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int w = 0; w < 4; ++w)
-            pf[n][h][w] = pack_bf16(s[n][2 * h + w / 2][2 * (w % 2)], s[n][2 * h + w / 2][2 * (w % 2) + 1]);
-      }
-      // slots behind the end may hold NaN, and 0 * NaN is NaN
-      u32x4 keep;
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        const int n = min(max(there - 4 * w, 0), 4);
-        keep[w] = n == 4 ? 0xffffffffu : (1u << (8 * n)) - 1u;
-      }
-#pragma unroll
-      for (int db = 0; db < DB; ++db) {
-        const u32x4 v = vr[db] & keep;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const u32x2 lo = values4<T>(v[2 * h]), hi = values4<T>(v[2 * h + 1]);
-          const u32x4 vf = {lo[0], lo[1], hi[0], hi[1]};
-#pragma unroll
-          for (int n = 0; n < NC; ++n) acc[n][db] = mfma(vf, pf[n][h], acc[n][db]);
-        }
-      }
-    }
-  } else {
-    const uint16_t* kc = static_cast<const uint16_t*>(a.k);
-    const uint16_t* vc = static_cast<const uint16_t*>(a.v);
-    uint16_t* vst = reinterpret_cast<uint16_t*>(smem + wave * C::kStage);
-    constexpr int CPR = HD / 8, RPL = 64 / CPR;  // 16-byte pieces of a row, rows of a load
-    constexpr int NL = kKvPage / RPL;            // loads of a page
-    const int vrow = lane / CPR, vcol = lane % CPR * 8;
-    for (int pg = page_lo + 2 * wave; pg < page_hi; pg += 2 * kTileWaves) {
-      u32x4 kr[2][C::kSteps], vr[2][NL];
-      int there[2];
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const size_t p = ((size_t)bt[min(pg + u, page_hi - 1)] * a.n_kv_heads + kv) * (kKvPage * HD);
-        there[u] = pg + u < page_hi ? min(len - (pg + u) * kKvPage, kKvPage) : 0;
-#pragma unroll
-        for (int s = 0; s < C::kSteps; ++s) kr[u][s] = ld16(kc + p + hl * HD + 32 * s + 8 * g);
-#pragma unroll
-        for (int i = 0; i < NL; ++i) vr[u][i] = ld16(vc + p + (size_t)(RPL * i + vrow) * HD + vcol);
-      }
-      floatx4 s[NC][2];
-#pragma unroll
-      for (int n = 0; n < NC; ++n)
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          s[n][u] = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int st = 0; st < C::kSteps; ++st) s[n][u] = mfma(kr[u][st], qf[n][st], s[n][u]);
-        }
-      // (rows behind the end as zeros: what is there may be NaN, and 0 * NaN is NaN)
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int i = 0; i < NL; ++i) {
-          const int row = RPL * i + vrow;
-          *reinterpret_cast<u32x4*>(vst + (u * kKvPage + row) * C::kVRow + vcol) = row < there[u] ? vr[u][i] : u32x4{0, 0, 0, 0};
-        }
-      u32x4 pf[NC];
-#pragma unroll
-      for (int n = 0; n < NC; ++n) {
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) s[n][u][r] = 4 * g + r < there[u] ? s[n][u][r] * a.scale_log2e : -INFINITY;
-        softmax(n, s[n]);
-#pragma unroll
-        for (int w = 0; w < 4; ++w) pf[n][w] = pack_bf16(s[n][w / 2][2 * (w % 2)], s[n][w / 2][2 * (w % 2) + 1]);
-      }
-      __builtin_amdgcn_wave_barrier();  // (a wave's LDS accesses keep their order; the compiler has to keep it too)
-      // lane i of a group of 16 hands in 4 features of key 4 g + i / 4 and is handed 4 keys of feature i
-      typedef short short4v __attribute__((ext_vector_type(4)));
-      typedef __attribute__((address_space(3))) short4v* lds_short4_ptr;
-      const uint16_t* vfrag = vst + (4 * g + (hl >> 2)) * C::kVRow + (hl & 3) * 4;
-#pragma unroll
-      for (int db = 0; db < DB; ++db) {
-        const u32x2 p0 = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_ptr)(vfrag + 16 * db)));
-        const u32x2 p1 = __builtin_bit_cast(
-            u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_ptr)(vfrag + kKvPage * C::kVRow + 16 * db)));
-        const u32x4 vf = {p0[0], p0[1], p1[0], p1[1]};
-#pragma unroll
-        for (int n = 0; n < NC; ++n) acc[n][db] = mfma(vf, pf[n], acc[n][db]);
-      }
-      __builtin_amdgcn_wave_barrier();
-    }
+    for (int i = 0; i < VL; ++i) vr[i] = ld16_kv<ONCE>(vsrc + 32 * i * kKvPage);
+  };
+  int pg = w.lo + 2 * wave;
+  if (pg < w.hi) {
+    ids(pg);
+    fetch_k();
+    fetch_v();
+    ids(pg + kStep);
   }
-
-  // Merge the waves, a tile of columns at a time.  A wave without keys has maximum -inf and weight 0.
-  float* mg = reinterpret_cast<float*>(smem);  // [wave][column][max, sum, output[HD]]
+  for (; pg < w.hi; pg += kStep) {
+    // keys of the lane's half page
+    const int there = pg + (g >> 1) < w.hi ? min(w.len - (pg + (g >> 1)) * kKvPage - 8 * (g & 1), 8) : 0;
+    floatx4 s[2] = {floatx4{0.f, 0.f, 0.f, 0.f}, floatx4{0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-  for (int t = 0; t < NC; ++t) {
-    const float l = across_groups<16>(l_run[t], AddOp());
-    __syncthreads();  // the staging areas, or the tile before, are done with
-    float* dst = mg + (size_t)(wave * 16 + hl) * (HD + 2);
-    if (g == 0) {
-      dst[0] = m_run[t];
-      dst[1] = l;
+    for (int c = 0; c < KL; ++c)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+          s[t] = mfma(values8<T>(kr[t][c][2 * h], kr[t][c][2 * h + 1]), qf[2 * c + h], s[t]);
+    const float ks = bf16_lo(ksr) * a.scale_log2e, vs = (hl & 7) < there ? bf16_lo(vsr) : 0.f;
+    const bool more = pg + kStep < w.hi;
+    if (more) fetch_k();
+    each(std::make_integer_sequence<int, 8>{}, [&](auto j) {
+      const float x = s[j() / 4][j() % 4] * row_lane<j()>(ks);
+      s[j() / 4][j() % 4] = j() < there ? x : -INFINITY;  // (whatever the slot holds)
+    });
+    online_softmax(s, acc, m_run, l_run);
+    each(std::make_integer_sequence<int, 8>{}, [&](auto j) { s[j() / 4][j() % 4] *= row_lane<j()>(vs); });
+    const u32x4 pf = probabilities(s);
+    // A load gave the lane 16 keys of one feature, g & 1 choosing between two blocks of 16 features: words 2, 3 of the
+    // even rows of lanes against words 0, 1 of the odd ones, and words 0, 1 are 8 keys of the first block in every lane,
+    // words 2, 3 of the second.
+#pragma unroll
+    for (int i = 0; i < VL; ++i) {
+      uint32_t x[4] = {vr[i][0], vr[i][1], vr[i][2], vr[i][3]};
+      swap16(x[0], x[2]);
+      swap16(x[1], x[3]);
+      vr[i] = u32x4{x[0], x[1], x[2], x[3]};
+    }
+    // slots behind the end may hold NaN, and 0 * NaN is NaN
+    if (__builtin_amdgcn_ballot_w64(there < 8) != 0) {
+      const uint32_t keep0 = there >= 4 ? 0xffffffffu : (1u << (8 * max(there, 0))) - 1u;
+      const uint32_t keep1 = there >= 8 ? 0xffffffffu : (1u << (8 * max(there - 4, 0))) - 1u;
+#pragma unroll
+      for (int i = 0; i < VL; ++i) vr[i] &= u32x4{keep0, keep1, keep0, keep1};
     }
 #pragma unroll
-    for (int db = 0; db < DB; ++db)
+    for (int i = 0; i < VL; ++i)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) dst[2 + 16 * db + 4 * g + r] = acc[t][db][r];
-    __syncthreads();
-    constexpr int ND = HD / 16;
-    const int col = c0 + 16 * t + (tid >> 4), d0 = (tid & 15) * ND;
-    if (col < cols) {
-      float m = -INFINITY, sum = 0.f, out[ND];
-#pragma unroll
-      for (int w = 0; w < kTileWaves; ++w) m = fmaxf(m, mg[(size_t)(w * 16 + (tid >> 4)) * (HD + 2)]);
-#pragma unroll
-      for (int j = 0; j < ND; ++j) out[j] = 0.f;
-#pragma unroll
-      for (int w = 0; w < kTileWaves; ++w) {
-        const float* src = mg + (size_t)(w * 16 + (tid >> 4)) * (HD + 2);
-        const float f = src[0] > -INFINITY ? __builtin_amdgcn_exp2f(src[0] - m) : 0.f;  // (NaN: its sum and output are NaN, times anything)
-        sum += src[1] * f;
-#pragma unroll
-        for (int j = 0; j < ND; ++j) out[j] += src[2 + d0 + j] * f;
-      }
-      const size_t item = (size_t)(row0 + col / G) * a.n_heads + kv * G + col % G;
-      if (a.n_states == 1) {
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;  // no key at all: 0
-        uint32_t w[ND / 2];
-#pragma unroll
-        for (int j = 0; j < ND / 2; ++j) w[j] = pack_bf16(out[2 * j] * inv, out[2 * j + 1] * inv);
-        uint16_t* op = a.o + item * HD + d0;
-        if constexpr (ND == 8) st16(op, u32x4{w[0], w[1], w[2], w[3]});
-        else *reinterpret_cast<u32x2*>(op) = u32x2{w[0], w[1]};
-      } else {
-        float* st = a.partial + (item * a.n_states + a.first_state + split) * (HD + 2);
-        if ((tid & 15) == 0) {
-          st[0] = m;
-          st[1] = sum;
-        }
-#pragma unroll
-        for (int j = 0; j < ND; ++j) st[2 + d0 + j] = out[j];
-      }
+      for (int h = 0; h < 2; ++h) acc[2 * i + h] = mfma(values8<T>(vr[i][2 * h], vr[i][2 * h + 1]), pf, acc[2 * i + h]);
+    if (more) {
+      fetch_v();
+      ids(pg + 2 * kStep);
     }
   }
 }
 
-// The states of a (row, head) as one, in their order: the same bits whenever.
-template <int HD>
-__global__ __launch_bounds__(HD) void tile_combine_kernel(const float* __restrict__ partial, int n_states,
-                                                          uint16_t* __restrict__ o) {
-  const size_t item = blockIdx.x;
-  const float* src = partial + item * n_states * (HD + 2);
-  float m = -INFINITY, sum = 0.f, out = 0.f;
-  for (int s = 0; s < n_states; ++s) m = fmaxf(m, src[(size_t)s * (HD + 2)]);
-  for (int s = 0; s < n_states; ++s) {
-    const float* st = src + (size_t)s * (HD + 2);
-    const float f = st[0] > -INFINITY ? __builtin_amdgcn_exp2f(st[0] - m) : 0.f;
-    sum += st[1] * f;
-    out += st[2 + threadIdx.x] * f;
+// bf16: row i of score tile t is key i of page t; V goes through the wave's own LDS.
+template <int HD, bool ONCE>
+__device__ __forceinline__ void narrow_bf16(const TileArgs& a, const TileWork& w, const u32x4 (&qf)[HD / 32],
+                                            floatx4 (&acc)[HD / 16], float& m_run, float& l_run, unsigned char* smem) {
+  constexpr int CPR = HD / 8, RPL = 64 / CPR;  // 16-byte pieces of a row, rows of a load
+  constexpr int NL = kKvPage / RPL;            // loads of a page
+  constexpr int kStep = 2 * kTileWaves;
+  const int lane = threadIdx.x & 63, hl = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint16_t* kc = static_cast<const uint16_t*>(a.k);
+  const uint16_t* vc = static_cast<const uint16_t*>(a.v);
+  uint16_t* vst = reinterpret_cast<uint16_t*>(smem) + wave * 32 * kVRow<HD>;
+  const int vrow = lane / CPR, vcol = lane % CPR * 8;
+  int id[2] = {0, 0};
+  auto ids = [&](int p) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) id[u] = w.bt[min(p + u, w.hi - 1)];
+  };
+  u32x4 kr[2][HD / 32], vr[2][NL];
+  size_t at[2];
+  auto fetch_k = [&] {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      at[u] = ((size_t)id[u] * a.n_kv_heads + w.kv) * (kKvPage * HD);
+#pragma unroll
+      for (int s = 0; s < HD / 32; ++s) kr[u][s] = ld16_kv<ONCE>(kc + at[u] + hl * HD + 32 * s + 8 * g);
+    }
+  };
+  auto fetch_v = [&] {
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int i = 0; i < NL; ++i) vr[u][i] = ld16_kv<ONCE>(vc + at[u] + (size_t)(RPL * i + vrow) * HD + vcol);
+  };
+  int pg = w.lo + 2 * wave;
+  if (pg < w.hi) {
+    ids(pg);
+    fetch_k();
+    fetch_v();
+    ids(pg + kStep);
   }
-  reinterpret_cast<__bf16*>(o)[item * HD + threadIdx.x] = (__bf16)(sum == 0.f ? 0.f : out / sum);
+  for (; pg < w.hi; pg += kStep) {
+    int there[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) there[u] = pg + u < w.hi ? min(w.len - (pg + u) * kKvPage, kKvPage) : 0;
+    floatx4 s[2] = {floatx4{0.f, 0.f, 0.f, 0.f}, floatx4{0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+    for (int st = 0; st < HD / 32; ++st)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) s[u] = mfma(kr[u][st], qf[st], s[u]);
+    const bool more = pg + kStep < w.hi;
+    if (more) fetch_k();
+    // (rows behind the end as zeros: what is there may be NaN, and 0 * NaN is NaN)
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int i = 0; i < NL; ++i) {
+        const int row = RPL * i + vrow;
+        *reinterpret_cast<u32x4*>(vst + (u * kKvPage + row) * kVRow<HD> + vcol) =
+            row < there[u] ? vr[u][i] : u32x4{0, 0, 0, 0};
+      }
+    if (more) {
+      fetch_v();
+      ids(pg + 2 * kStep);
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) s[u][r] = 4 * g + r < there[u] ? s[u][r] * a.scale_log2e : -INFINITY;
+    online_softmax(s, acc, m_run, l_run);
+    const u32x4 pf = probabilities(s);
+    __builtin_amdgcn_wave_barrier();  // (a wave's LDS accesses keep their order; the compiler has to keep it too)
+    const uint16_t* vfrag = vst + (4 * g + (hl >> 2)) * kVRow<HD> + (hl & 3) * 4;
+#pragma unroll
+    for (int db = 0; db < HD / 16; ++db) acc[db] = mfma(turned<HD>(vfrag, db), pf, acc[db]);
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+// ---- wide ----
+// A tile's K in LDS as bf16 rows, chunk c of 16 bytes at c ^ swizzle: the 16 rows that an operand read takes at one chunk
+// number then lie in 16 different places of the 256 bytes of all banks.  bf16: row i of score tile t is key 16 t + i, and V
+// is as for the narrow form.  8 bits: row i of score tile t is key 8 (i / 4) + 4 t + i % 4, so that lane group g has keys
+// 8 g .. + 8, and V^T rows of 32 keys hold operand A in their chunk g (at g ^ (d / 4 & 3)).
+template <int HD, int T>
+__device__ __forceinline__ int k_swizzle(int row) {
+  if constexpr (T == kKvBf16) return HD == 128 ? row & 15 : (row >> 1) & 7;
+  else return HD == 128 ? (row & 3) | ((row >> 3) & 3) << 2 : ((row >> 1) & 1) | ((row >> 3) & 3) << 1;
+}
+
+template <int HD, int T>
+__device__ __forceinline__ void wide_tiles(const TileArgs& a, const TileWork& w, const u32x4 (&qf)[HD / 32],
+                                           floatx4 (&acc)[HD / 16], float& m_run, float& l_run, bool idle,
+                                           unsigned char* smem) {
+  using L = TileLds<HD, T, true>;
+  constexpr bool kQuant = T != kKvBf16;
+  constexpr int B8 = HD / 8;                     // numbers of K, and tokens x features of V, of a thread: 16 or 8
+  constexpr int RW = kQuant ? B8 / 4 : B8 / 2;   // words of a thread
+  const int tid = threadIdx.x, lane = tid & 63, hl = lane & 15, g = lane >> 4;
+  const int half = __builtin_amdgcn_readfirstlane(tid >> 7), at = tid & 127;  // page of the tile, place in it
+  const int key = at >> 3, piece = at & 7;       // of K (and of V where it is bf16): B8 numbers from B8 piece on
+  uint32_t kr[RW], vr[RW];
+  uint16_t scale = 0;
+  int id = 0, pg;
+  auto ids = [&](int p) { id = w.bt[min(p + half, w.hi - 1)]; };
+  auto words = [&](uint32_t (&r)[RW], const void* p) {
+    if constexpr (RW == 8) {
+      const u32x4 x = ld16(p), y = ld16(static_cast<const char*>(p) + 16);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        r[i] = x[i];
+        r[4 + i] = y[i];
+      }
+    } else if constexpr (RW == 4) {
+      const u32x4 x = ld16(p);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) r[i] = x[i];
+    } else {
+      const u32x2 x = *static_cast<const u32x2*>(p);
+      r[0] = x[0];
+      r[1] = x[1];
+    }
+  };
+  auto fetch = [&] {
+    const size_t page = (size_t)id * a.n_kv_heads + w.kv;
+    const size_t first = page * (kKvPage * HD) + (size_t)at * B8;
+    if constexpr (kQuant) {
+      words(kr, static_cast<const uint8_t*>(a.k) + first);
+      words(vr, static_cast<const uint8_t*>(a.v) + first);
+      if (at < 32) scale = (at < 16 ? a.k_scale : a.v_scale)[page * kKvPage + (at & 15)];
+    } else {
+      words(kr, static_cast<const uint16_t*>(a.k) + first);
+      words(vr, static_cast<const uint16_t*>(a.v) + first);
+    }
+  };
+  auto stage = [&](unsigned char* buf) {
+    const int row = half * kKvPage + key;
+    const int there = pg + half < w.hi ? min(w.len - (pg + half) * kKvPage, kKvPage) : 0;  // keys of the thread's page
+    uint16_t* kt = reinterpret_cast<uint16_t*>(buf);
+    uint16_t* vt = reinterpret_cast<uint16_t*>(buf + L::kK);
+    constexpr int NCH = B8 / 8;  // 16-byte chunks of bf16
+    if constexpr (kQuant) {
+#pragma unroll
+      for (int c = 0; c < NCH; ++c)
+        *reinterpret_cast<u32x4*>(kt + row * HD + ((NCH * piece + c) ^ k_swizzle<HD, T>(row)) * 8) =
+            values8<T>(kr[2 * c], kr[2 * c + 1]);
+      // the thread's V: feature `at` of its page, all tokens (HD 128), or feature at / 2, half of them
+      const int d = HD == 128 ? at : at >> 1, t0 = HD == 128 ? 0 : 8 * (at & 1);
+#pragma unroll
+      for (int c = 0; c < NCH; ++c) {
+        const int n = there - t0 - 8 * c;  // (slots behind the end may hold NaN)
+        const uint32_t x = n >= 4 ? vr[2 * c] : n > 0 ? vr[2 * c] & ((1u << (8 * n)) - 1u) : 0;
+        const uint32_t y = n >= 8 ? vr[2 * c + 1] : n > 4 ? vr[2 * c + 1] & ((1u << (8 * (n - 4))) - 1u) : 0;
+        *reinterpret_cast<u32x4*>(vt + d * 32 + ((2 * half + t0 / 8 + c) ^ ((d >> 2) & 3)) * 8) = values8<T>(x, y);
+      }
+      if (at < 32) {
+        float* sc = reinterpret_cast<float*>(buf + L::kK + L::kV) + (at < 16 ? 0 : 32);
+        const float f = bf16_lo(scale);
+        sc[half * kKvPage + (at & 15)] = at < 16 ? f * a.scale_log2e : ((at & 15) < there ? f : 0.f);
+      }
+    } else {
+#pragma unroll
+      for (int c = 0; c < NCH; ++c) {
+        *reinterpret_cast<u32x4*>(kt + row * HD + ((NCH * piece + c) ^ k_swizzle<HD, T>(row)) * 8) =
+            u32x4{kr[4 * c], kr[4 * c + 1], kr[4 * c + 2], kr[4 * c + 3]};
+        *reinterpret_cast<u32x4*>(vt + row * kVRow<HD> + (NCH * piece + c) * 8) =
+            key < there ? u32x4{vr[4 * c], vr[4 * c + 1], vr[4 * c + 2], vr[4 * c + 3]} : u32x4{0, 0, 0, 0};
+      }
+    }
+  };
+  pg = w.lo;
+  if (pg >= w.hi) return;
+  ids(pg);
+  fetch();
+  ids(pg + 2);
+  for (int buf = 0; pg < w.hi; pg += 2, buf ^= 1) {
+    unsigned char* tile = smem + buf * L::kTile;
+    stage(tile);  // (last read two tiles ago, before the barrier of the tile before this)
+    if (pg + 2 < w.hi) {
+      fetch();
+      ids(pg + 4);
+    }
+    __syncthreads();
+    if (idle) continue;
+    const uint16_t* kt = reinterpret_cast<const uint16_t*>(tile);
+    const uint16_t* vt = reinterpret_cast<const uint16_t*>(tile + L::kK);
+    floatx4 s[2] = {floatx4{0.f, 0.f, 0.f, 0.f}, floatx4{0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+    for (int st = 0; st < HD / 32; ++st)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const int row = kQuant ? 8 * (hl >> 2) + 4 * t + (hl & 3) : 16 * t + hl;
+        s[t] = mfma(ld16(kt + row * HD + ((4 * st + g) ^ k_swizzle<HD, T>(row)) * 8), qf[st], s[t]);
+      }
+    const int left = w.len - pg * kKvPage;  // keys from this tile on, of this sequence; and of this split
+    const int here = min(left, (w.hi - pg) * kKvPage);
+    if constexpr (kQuant) {
+      const floatx4* sc = reinterpret_cast<const floatx4*>(tile + L::kK + L::kV);
+#pragma unroll
+      for (int t = 0; t < 2; ++t) s[t] *= sc[2 * g + t];
+    } else {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) s[t] *= a.scale_log2e;
+    }
+    if (here < 32) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if ((kQuant ? 8 * g + 4 * t : 16 * t + 4 * g) + r >= here) s[t][r] = -INFINITY;
+    }
+    online_softmax(s, acc, m_run, l_run);
+    if constexpr (kQuant) {
+      const floatx4* sc = reinterpret_cast<const floatx4*>(tile + L::kK + L::kV) + 8;
+#pragma unroll
+      for (int t = 0; t < 2; ++t) s[t] *= sc[2 * g + t];
+    }
+    const u32x4 pf = probabilities(s);
+    if constexpr (kQuant) {
+#pragma unroll
+      for (int db = 0; db < HD / 16; ++db) {
+        const int d = 16 * db + hl;
+        acc[db] = mfma(ld16(vt + d * 32 + (g ^ ((d >> 2) & 3)) * 8), pf, acc[db]);
+      }
+    } else {
+      const uint16_t* vfrag = vt + (4 * g + (hl >> 2)) * kVRow<HD> + (hl & 3) * 4;
+#pragma unroll
+      for (int db = 0; db < HD / 16; ++db) acc[db] = mfma(turned<HD>(vfrag, db), pf, acc[db]);
+    }
+  }
+}
+
+// WIDE: either part may be wide (a part of up to 16 columns is narrow all the same).  ONCE: the rows' own pages are read
+// with loads that no cache keeps.
+template <int HD, int T, bool WIDE, bool ONCE>
+__global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(T == kKvBf16 ? 3 : 4))) void tile_attention_kernel(const TileArgs a) {
+  constexpr int DB = HD / 16, kSteps = HD / 32, kState = HD + kStatePad;
+  constexpr bool kQuant = T != kKvBf16;
+  __shared__ __attribute__((aligned(16))) unsigned char smem[TileLds<HD, T, WIDE>::kBytes];
+  const int tid = threadIdx.x, lane = tid & 63, hl = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const bool second = (int)blockIdx.x >= a.first_blocks;
+  const TilePart& p = a.part[second ? 1 : 0];
+  const bool wide = WIDE && p.wide;
+  const int G = a.n_heads / a.n_kv_heads;
+
+  // workgroup -> key/value head (fastest), block of columns, group, split
+  int id = (int)blockIdx.x - (second ? a.first_blocks : 0);
+  const int x = id % p.blocks_x;
+  id /= p.blocks_x;
+  int group = id % p.groups;
+  const int split = id / p.groups;
+  TileWork w;
+  w.kv = x % a.n_kv_heads;
+  // Workgroups reach the chip's eight partitions in turn: heads that share 128 bytes of scales meet in one of them.
+  if (kQuant && a.n_kv_heads % 8 == 0) w.kv = w.kv % 8 * (a.n_kv_heads / 8) + w.kv / 8;
+  w.c0 = x / a.n_kv_heads * (wide ? kWideCols : kNarrowCols);
+  if (p.rank) {
+    // Longest first among every n-th sequence, so that no long one starts among the last and ends the launch by itself.
+    const int n = (p.groups + 63) / 64, other = group % n + n * lane;
+    const int pages = other < p.groups ? max(p.lens[other] + p.len_add + kKvPage - 1, 0) / kKvPage : -1;
+    group = group % n + n * ranked(min(pages, p.max_pages), group / n, 32 - __builtin_clz(p.max_pages));
+  }
+  w.row0 = p.cu_rows ? p.cu_rows[group] : group;
+  w.cols = (p.cu_rows ? p.cu_rows[group + 1] - w.row0 : 1) * G;
+  if (w.c0 >= w.cols) return;
+  w.len = p.lens[group] + p.len_add;
+  w.lo = split * p.pages_per_split;
+  w.hi = min((w.len + kKvPage - 1) / kKvPage, w.lo + p.pages_per_split);
+  w.bt = p.tables + (size_t)group * p.max_pages;
+  w.state = p.first_state + split;
+
+  // Operand B of the scores.  8 bits, narrow: instruction 2 c + h takes features 64 c + 16 g + 8 h .. + 8 of lane group g (16
+  // bytes of K are two operands); else instruction s features 32 s + 8 g .. + 8.
+  const int my_c0 = w.c0 + (wide ? 16 * wave : 0), col = my_c0 + hl;
+  u32x4 qf[kSteps];
+  {
+    const uint16_t* qp = a.q + (size_t)(w.row0 + col / G) * a.q_stride + (size_t)(w.kv * G + col % G) * HD;
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+      qf[s] = u32x4{0, 0, 0, 0};
+      const int at = kQuant && !wide ? 64 * (s / 2) + 16 * g + 8 * (s % 2) : 32 * s + 8 * g;
+      if (col < w.cols) qf[s] = ld16(qp + at);
+    }
+  }
+  floatx4 acc[DB];
+  float m_run = -INFINITY, l_run = 0.f;  // l_run: this lane's share of the sum
+#pragma unroll
+  for (int db = 0; db < DB; ++db) acc[db] = floatx4{0.f, 0.f, 0.f, 0.f};
+
+  const size_t item = (size_t)(w.row0 + col / G) * a.n_heads + w.kv * G + col % G;
+  if constexpr (WIDE) {
+    if (wide) {
+      wide_tiles<HD, T>(a, w, qf, acc, m_run, l_run, my_c0 >= w.cols, smem);
+      const float l = across_groups<16>(l_run, AddOp());
+      if (col >= w.cols) return;
+      if (a.n_states == 1) {
+        const float inv = l == 0.f ? 0.f : 1.f / l;  // no key at all: 0
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+          *reinterpret_cast<u32x2*>(a.o + item * HD + 16 * db + 4 * g) =
+              u32x2{pack_bf16(acc[db][0] * inv, acc[db][1] * inv), pack_bf16(acc[db][2] * inv, acc[db][3] * inv)};
+      } else {
+        float* st = a.partial + (item * a.n_states + w.state) * kState;
+#pragma unroll
+        for (int db = 0; db < DB; ++db) *reinterpret_cast<floatx4*>(st + 16 * db + 4 * g) = acc[db];
+        if (g == 0) {
+          st[HD] = m_run;
+          st[HD + 1] = l;
+        }
+      }
+      return;
+    }
+  }
+  if constexpr (kQuant) narrow_quant<HD, T, ONCE>(a, w, qf, acc, m_run, l_run);
+  else narrow_bf16<HD, ONCE>(a, w, qf, acc, m_run, l_run, smem);
+
+  // Merge the waves.  A wave without keys has maximum -inf and weight 0.
+  const float l = across_groups<16>(l_run, AddOp());
+  float* mg = reinterpret_cast<float*>(smem);  // [wave][column][output[HD], max, sum, -, -]
+  __syncthreads();                             // the staging areas are done with
+  float* dst = mg + (wave * 16 + hl) * kState;
+#pragma unroll
+  for (int db = 0; db < DB; ++db) *reinterpret_cast<floatx4*>(dst + 16 * db + 4 * g) = acc[db];
+  if (g == 0) {
+    dst[HD] = m_run;
+    dst[HD + 1] = l;
+  }
+  __syncthreads();
+  constexpr int ND = HD / 16;
+  const int c = tid >> 4, d0 = (tid & 15) * ND;
+  if (w.c0 + c >= w.cols) return;
+  float m = -INFINITY, sum = 0.f, out[ND];
+#pragma unroll
+  for (int i = 0; i < kTileWaves; ++i) m = fmaxf(m, mg[(i * 16 + c) * kState + HD]);
+#pragma unroll
+  for (int j = 0; j < ND; ++j) out[j] = 0.f;
+#pragma unroll
+  for (int i = 0; i < kTileWaves; ++i) {
+    const float* src = mg + (i * 16 + c) * kState;
+    const float f = src[HD] > -INFINITY ? __builtin_amdgcn_exp2f(src[HD] - m) : 0.f;  // (NaN: its sum is NaN, times anything)
+    sum += src[HD + 1] * f;
+#pragma unroll
+    for (int j = 0; j < ND; ++j) out[j] += src[d0 + j] * f;
+  }
+  const int mine = w.c0 + c;
+  const size_t to = (size_t)(w.row0 + mine / G) * a.n_heads + w.kv * G + mine % G;
+  if (a.n_states == 1) {
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;  // no key at all: 0
+    uint32_t v[ND / 2];
+#pragma unroll
+    for (int j = 0; j < ND / 2; ++j) v[j] = pack_bf16(out[2 * j] * inv, out[2 * j + 1] * inv);
+    uint16_t* op = a.o + to * HD + d0;
+    if constexpr (ND == 8) st16(op, u32x4{v[0], v[1], v[2], v[3]});
+    else *reinterpret_cast<u32x2*>(op) = u32x2{v[0], v[1]};
+  } else {
+    float* st = a.partial + (to * a.n_states + w.state) * kState;
+#pragma unroll
+    for (int j = 0; j < ND; j += 4) *reinterpret_cast<floatx4*>(st + d0 + j) = floatx4{out[j], out[j + 1], out[j + 2], out[j + 3]};
+    if ((tid & 15) == 0) {
+      st[HD] = m;
+      st[HD + 1] = sum;
+    }
+  }
+}
+
+// The states of a (row, head) as one, in a fixed order: the same bits whenever.  Wave w takes states w, w + 4, ...: its lanes
+// have the maxima and sums of 64 of them at once, and then HD / 64 features each, the states asked for 8 at a time.
+template <int HD>
+__global__ __launch_bounds__(kTileThreads) void tile_combine_kernel(const float* __restrict__ partial, int n_states,
+                                                                    uint16_t* __restrict__ o) {
+  constexpr int ND = HD / 64, kState = HD + kStatePad, U = 8;
+  __shared__ float merge[kTileWaves][HD + 2];
+  const size_t item = blockIdx.x;
+  const float* src = partial + item * n_states * kState;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  float m_run = -INFINITY, l_run = 0.f, out[ND] = {};
+  for (int s0 = wave; s0 < n_states; s0 += 64 * kTileWaves) {
+    const int n = min((n_states - s0 + kTileWaves - 1) / kTileWaves, 64);  // of them in this turn
+    float m = -INFINITY, l = 0.f;
+    if (lane < n) {
+      m = src[(size_t)(s0 + kTileWaves * lane) * kState + HD];
+      l = src[(size_t)(s0 + kTileWaves * lane) * kState + HD + 1];
+    }
+    float top = lane_op<1>(m, MaxOp());
+    top = lane_op<2>(top, MaxOp());
+    top = lane_op<kMirror4>(top, MaxOp());
+    top = across_groups<8>(top, MaxOp());
+    const float m_new = fmaxf(m_run, top), alpha = m_run > -INFINITY ? __builtin_amdgcn_exp2f(m_run - m_new) : 0.f;
+    const float f = m > -INFINITY ? __builtin_amdgcn_exp2f(m - m_new) : 0.f;
+    l_run = l_run * alpha + wave_sum(l * f);
+#pragma unroll
+    for (int j = 0; j < ND; ++j) out[j] *= alpha;
+    m_run = m_new;
+    for (int i0 = 0; i0 < n; i0 += U) {
+      float v[U][ND];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {  // (behind the last: the last again, not used)
+        const float* st = src + (size_t)(s0 + kTileWaves * min(i0 + u, n - 1)) * kState + ND * lane;
+#pragma unroll
+        for (int j = 0; j < ND; ++j) v[u][j] = st[j];
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const float fu = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), min(i0 + u, n - 1)));
+        if (i0 + u < n)
+#pragma unroll
+          for (int j = 0; j < ND; ++j) out[j] += v[u][j] * fu;
+      }
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < ND; ++j) merge[wave][ND * lane + j] = out[j];
+  if (lane == 0) {
+    merge[wave][HD] = m_run;
+    merge[wave][HD + 1] = l_run;
+  }
+  __syncthreads();
+  const int d = threadIdx.x;
+  if (d >= HD) return;
+  float m = -INFINITY, sum = 0.f, r = 0.f;
+#pragma unroll
+  for (int i = 0; i < kTileWaves; ++i) m = fmaxf(m, merge[i][HD]);
+#pragma unroll
+  for (int i = 0; i < kTileWaves; ++i) {
+    const float f = merge[i][HD] > -INFINITY ? __builtin_amdgcn_exp2f(merge[i][HD] - m) : 0.f;
+    sum += merge[i][HD + 1] * f;
+    r += merge[i][d] * f;
+  }
+  reinterpret_cast<__bf16*>(o)[item * HD + d] = (__bf16)(sum == 0.f ? 0.f : r / sum);
 }
 
 // ---- plans ----
-// Column tiles of a workgroup.
-static int column_tiles(long cols) { return cols <= 16 ? 1 : 2; }
+DS_SWITCH(g_tile_own, 0);
+DS_SWITCH(g_tile_prefix, 0);
+DS_SWITCH(g_tile_rank, 1);
 
-// Splits of up to max_len tokens for `columns` queries of each key/value head in all: enough for two workgroups per compute
-// unit, of 16 pages or more.  (Of a prefix: as though one group had all rows.)
-static int tile_splits(long columns, int n_kv_heads, int max_len) {
-  const int nc = column_tiles(columns);
-  const long items = n_kv_heads * ((columns + 16 * nc - 1) / (16 * nc));
+static int blocks_of(long cols) { return (int)(cols <= kNarrowCols ? 1 : (cols + kWideCols - 1) / kWideCols); }
+
+// Splits of up to max_len tokens for `items` workgroups that there are anyway: enough for two workgroups per compute unit,
+// of 16 pages or more.
+static int tile_splits(long items, int max_len) {
   const int pages = (max_len + kKvPage - 1) / kKvPage;
-  const long wanted = (512 + items - 1) / items;
-  return (int)std::max(1l, std::min(wanted, (long)pages / 16));
+  return (int)std::max(1l, std::min((512 + items - 1) / items, (long)pages / 16));
 }
 
 TilePlan tile_plan(int B, int n_heads, int n_kv_heads, int max_len, int max_prefix) {
   const int G = n_heads / n_kv_heads;
   TilePlan p;
-  p.own = tile_splits(16l * B * ((G + 15) / 16), n_kv_heads, max_len);
-  p.prefix = max_prefix > 0 ? tile_splits((long)B * G, n_kv_heads, max_prefix) : 0;
+  p.own = tile_splits((long)B * n_kv_heads * blocks_of(G), max_len);
+  // (as though one group had all rows)
+  p.prefix = max_prefix > 0 ? tile_splits((long)n_kv_heads * blocks_of((long)B * G), max_prefix) : 0;
+  if (g_tile_own > 0) p.own = g_tile_own;
+  if (g_tile_prefix > 0 && p.prefix > 0) p.prefix = g_tile_prefix;
   return p;
 }
 size_t tile_states_bytes(int B, int n_heads, int head_dim, int states) {
-  return states <= 1 ? 0 : (size_t)B * n_heads * states * (head_dim + 2) * sizeof(float);
+  return states <= 1 ? 0 : (size_t)B * n_heads * states * (head_dim + kStatePad) * sizeof(float);
 }
 
 template <int HD, int T>
-static hipError_t launch_tiles(TileArgs a, int groups, long cols, int max_len, int splits, hipStream_t stream) {
-  const int nc = column_tiles(cols);
-  const long blocks = (cols + 16 * nc - 1) / (16 * nc) * a.n_kv_heads;
-  const int pages = (max_len + kKvPage - 1) / kKvPage;
-  a.pages_per_split = (pages + splits - 1) / splits;
-  if (blocks > 0x7fffffffL / kTileThreads || groups > 65535 || splits > 65535) return hipErrorInvalidValue;
-  const dim3 grid((unsigned)blocks, groups, splits), threads(kTileThreads);
-  if (nc == 1) hipLaunchKernelGGL((tile_attention_kernel<HD, T, 1>), grid, threads, 0, stream, a);
-  else hipLaunchKernelGGL((tile_attention_kernel<HD, T, 2>), grid, threads, 0, stream, a);
-  return hipGetLastError();
-}
-
-template <int HD, int T>
-static hipError_t launch_all(const TileAttention& t, hipStream_t stream) {
+static hipError_t launch_tiles(const TileAttention& t, hipStream_t stream) {
+  const int G = t.n_heads / t.n_kv_heads;
   TileArgs a{};
   a.q = (const uint16_t*)t.q; a.q_stride = t.q_stride;
   a.k = t.cache.k; a.v = t.cache.v;
@@ -389,18 +729,42 @@ static hipError_t launch_all(const TileAttention& t, hipStream_t stream) {
   a.scale_log2e = 1.4426950408889634f / sqrtf((float)HD);
   a.n_states = t.plan.prefix + t.plan.own;
   a.o = (uint16_t*)t.o; a.partial = (float*)t.states;
-  const int G = t.n_heads / t.n_kv_heads;
+  long blocks = 0;
+  auto part = [&](TilePart& p, const int32_t* cu, const int32_t* lens, const int32_t* tables, int len_add, int max_pages,
+                  int groups, long cols, int max_len, int splits, int first_state) {
+    const int pages = (max_len + kKvPage - 1) / kKvPage;
+    p.cu_rows = cu; p.lens = lens; p.tables = tables;
+    p.len_add = len_add; p.max_pages = max_pages; p.groups = groups;
+    p.wide = cols > kNarrowCols;
+    p.blocks_x = t.n_kv_heads * blocks_of(cols);
+    p.pages_per_split = (pages + splits - 1) / splits;
+    p.first_state = first_state;
+    blocks += (long)p.blocks_x * groups * splits;
+  };
   if (t.plan.prefix > 0) {
-    a.cu_rows = t.cu_groups; a.lens = t.prefix_lens; a.tables = t.prefix_tables; a.max_pages = t.max_prefix_pages;
-    a.first_state = 0;
-    const hipError_t e = launch_tiles<HD, T>(a, t.n_groups, (long)t.max_rows * G, t.max_prefix, t.plan.prefix, stream);
-    if (e != hipSuccess) return e;
+    part(a.part[0], t.cu_groups, t.prefix_lens, t.prefix_tables, 0, t.max_prefix_pages, t.n_groups, (long)t.max_rows * G,
+         t.max_prefix, t.plan.prefix, 0);
+    a.first_blocks = (int)std::min(blocks, 0x7fffffffL);
   }
-  a.cu_rows = nullptr; a.lens = t.kv_lens; a.len_add = t.kv_len_add; a.tables = t.block_tables; a.max_pages = t.max_blocks;
-  a.first_state = t.plan.prefix;
-  hipError_t e = launch_tiles<HD, T>(a, t.B, G, t.max_kv_len, t.plan.own, stream);
+  part(a.part[1], nullptr, t.kv_lens, t.block_tables, t.kv_len_add, t.max_blocks, t.B, G, t.max_kv_len, t.plan.own,
+       t.plan.prefix);
+  a.part[1].rank = g_tile_rank && t.B > 1;
+  if (blocks > 0x7fffffffL / kTileThreads) return hipErrorInvalidValue;
+  const bool wide = a.part[0].wide || a.part[1].wide;
+  // more than the last-level cache (256 MB) could keep until the next step
+  const double bytes = (double)t.B * t.max_kv_len * t.n_kv_heads * HD * (T == kKvBf16 ? 4 : 2);
+  const bool once = bytes > 256e6;
+  const dim3 grid((unsigned)blocks), threads(kTileThreads);
+  if (T == kKvBf16 || wide) {
+    if (once) hipLaunchKernelGGL((tile_attention_kernel<HD, T, true, true>), grid, threads, 0, stream, a);
+    else hipLaunchKernelGGL((tile_attention_kernel<HD, T, true, false>), grid, threads, 0, stream, a);
+  } else if constexpr (T != kKvBf16) {
+    if (once) hipLaunchKernelGGL((tile_attention_kernel<HD, T, false, true>), grid, threads, 0, stream, a);
+    else hipLaunchKernelGGL((tile_attention_kernel<HD, T, false, false>), grid, threads, 0, stream, a);
+  }
+  hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.n_states == 1) return e;
-  hipLaunchKernelGGL(tile_combine_kernel<HD>, dim3(t.B * t.n_heads), dim3(HD), 0, stream, a.partial, a.n_states, a.o);
+  hipLaunchKernelGGL(tile_combine_kernel<HD>, dim3(t.B * t.n_heads), threads, 0, stream, a.partial, a.n_states, a.o);
   return hipGetLastError();
 }
 
@@ -408,13 +772,13 @@ hipError_t launch_tile_attention(const TileAttention& t, hipStream_t stream) {
   if (t.n_kv_heads <= 0 || t.n_heads % t.n_kv_heads != 0 || t.B > 65535) return hipErrorInvalidValue;
   if (t.plan.own < 1 || (t.plan.own + t.plan.prefix > 1 && !t.states)) return hipErrorInvalidValue;
   if (t.head_dim == 128) {
-    if (t.cache.type == kKvBf16) return launch_all<128, kKvBf16>(t, stream);
-    if (t.cache.type == kKvE4m3) return launch_all<128, kKvE4m3>(t, stream);
-    if (t.cache.type == kKvInt8) return launch_all<128, kKvInt8>(t, stream);
+    if (t.cache.type == kKvBf16) return launch_tiles<128, kKvBf16>(t, stream);
+    if (t.cache.type == kKvE4m3) return launch_tiles<128, kKvE4m3>(t, stream);
+    if (t.cache.type == kKvInt8) return launch_tiles<128, kKvInt8>(t, stream);
   } else if (t.head_dim == 64) {
-    if (t.cache.type == kKvBf16) return launch_all<64, kKvBf16>(t, stream);
-    if (t.cache.type == kKvE4m3) return launch_all<64, kKvE4m3>(t, stream);
-    if (t.cache.type == kKvInt8) return launch_all<64, kKvInt8>(t, stream);
+    if (t.cache.type == kKvBf16) return launch_tiles<64, kKvBf16>(t, stream);
+    if (t.cache.type == kKvE4m3) return launch_tiles<64, kKvE4m3>(t, stream);
+    if (t.cache.type == kKvInt8) return launch_tiles<64, kKvInt8>(t, stream);
   }
   return hipErrorInvalidValue;
 }
