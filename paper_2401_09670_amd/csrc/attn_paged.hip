@@ -19,6 +19,7 @@
 //    and into LDS once.
 // Where a (row, head) has more than one state, they are written out in fp32 and a second launch merges them in order.
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "kv_quant.h"
@@ -27,6 +28,7 @@ namespace ds {
 
 constexpr int kTileThreads = 256, kTileWaves = 4;
 constexpr int kWideCols = 64, kNarrowCols = 16;
+constexpr int kWideKeys = 64;  // of a tile
 
 struct TilePart {
   const int32_t* cu_rows;  // group i has the rows [cu_rows[i], cu_rows[i + 1]); null: row i
@@ -36,7 +38,9 @@ struct TilePart {
   int blocks_x;            // key/value heads x blocks of columns
   int pages_per_split;
   int first_state;         // states of this part's splits
-  int wide, rank;          // rank: longest groups first
+  int wide;                // 64 columns a workgroup
+  int solo;                // narrow: a key/value head for each wave
+  int rank;                // longest groups first
 };
 
 struct TileArgs {
@@ -73,9 +77,17 @@ __device__ __forceinline__ u32x4 ld16_kv(const void* p) {
   else return ld16(p);
 }
 
+// The lane's number, not kept from before: over a loop it would take a register that the loop needs.
+__device__ __forceinline__ int lane_anew() {
+  int zero = 0;
+  asm volatile("" : "+v"(zero));
+  return __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, zero));
+}
+
 // One workgroup's share: a group's pages [lo, hi) of a key/value head, for some of the group's columns.
 struct TileWork {
   int kv, row0, c0, cols, state, len, lo, hi;
+  int step;  // narrow: pages from one chunk of a wave to its next
   const int32_t* bt;
 };
 
@@ -96,12 +108,12 @@ __device__ __forceinline__ int ranked(int pages, int r, int bits) {
   return __builtin_ctzll(__builtin_amdgcn_ballot_w64(((left >> lane) & 1) && before == r));
 }
 
-// Running softmax over two score tiles (scaled by log2 e, -inf where there is no key): p in place of s.
-template <int DB>
-__device__ __forceinline__ void online_softmax(floatx4 (&s)[2], floatx4 (&acc)[DB], float& m_run, float& l_run) {
+// Running softmax over N score tiles (scaled by log2 e, -inf where there is no key): p in place of s.
+template <int N, int DB>
+__device__ __forceinline__ void online_softmax(floatx4 (&s)[N], floatx4 (&acc)[DB], float& m_run, float& l_run) {
   float top = -INFINITY;
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+  for (int i = 0; i < N; ++i)
 #pragma unroll
     for (int r = 0; r < 4; ++r) top = fmaxf(top, s[i][r]);
   top = across_groups<16>(top, MaxOp());
@@ -115,7 +127,7 @@ __device__ __forceinline__ void online_softmax(floatx4 (&s)[2], floatx4 (&acc)[D
   }
   float sum = 0.f;
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+  for (int i = 0; i < N; ++i)
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       s[i][r] = __builtin_amdgcn_exp2f(s[i][r] - m_run);
@@ -123,7 +135,7 @@ __device__ __forceinline__ void online_softmax(floatx4 (&s)[2], floatx4 (&acc)[D
     }
   l_run += sum;
 }
-__device__ __forceinline__ u32x4 probabilities(const floatx4 (&s)[2]) {
+__device__ __forceinline__ u32x4 probabilities(const floatx4* s) {  // of two tiles
   u32x4 p;
 #pragma unroll
   for (int w = 0; w < 4; ++w) p[w] = pack_bf16(s[w / 2][2 * (w % 2)], s[w / 2][2 * (w % 2) + 1]);
@@ -151,15 +163,15 @@ __device__ __forceinline__ u32x4 turned(const uint16_t* vfrag, int db) {
   return u32x4{p0[0], p0[1], p1[0], p1[1]};
 }
 
-// bytes of LDS: a tile of K and of V, twice (wide); the staging areas of the waves (narrow, bf16); the merge (narrow)
+// bytes of LDS: a tile of K and of V (wide); the staging areas of the waves (narrow, bf16); the merge (narrow)
 template <int HD, int T, bool WIDE>
 struct TileLds {
-  static constexpr int kK = 32 * HD * 2, kV = T == kKvBf16 ? 32 * kVRow<HD> * 2 : 32 * HD * 2;
-  static constexpr int kTile = kK + kV + (T == kKvBf16 ? 0 : 2 * 32 * 4);
+  static constexpr int kK = kWideKeys * HD * 2, kV = kWideKeys * (T == kKvBf16 ? kVRow<HD> : HD) * 2;
+  static constexpr int kTile = kK + kV + (T == kKvBf16 ? 0 : 2 * kWideKeys * 4);
   static constexpr int kStage = T == kKvBf16 ? 32 * kVRow<HD> * 2 : 0;
   static constexpr int kMerge = kTileWaves * 16 * (HD + kStatePad) * 4;
   static constexpr int most(int a, int b) { return a > b ? a : b; }
-  static constexpr int kBytes = most(WIDE ? 2 * kTile : 0, most(kTileWaves * kStage, kMerge));
+  static constexpr int kBytes = most(WIDE ? kTile : 0, most(kTileWaves * kStage, kMerge));
 };
 
 // ---- narrow ----
@@ -173,9 +185,7 @@ template <int HD, int T, bool ONCE>
 __device__ __forceinline__ void narrow_quant(const TileArgs& a, const TileWork& w, const u32x4 (&qf)[HD / 32],
                                              floatx4 (&acc)[HD / 16], float& m_run, float& l_run) {
   constexpr int KL = HD / 64, VL = HD / 32;  // 16-byte loads of a key, of a chunk's V, per lane
-  constexpr int kStep = 2 * kTileWaves;
   const int lane = threadIdx.x & 63, hl = lane & 15, g = lane >> 4;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint8_t* kc = static_cast<const uint8_t*>(a.k);
   const uint8_t* vc = static_cast<const uint8_t*>(a.v);
   int kid = 0, vid = 0;
@@ -202,14 +212,14 @@ __device__ __forceinline__ void narrow_quant(const TileArgs& a, const TileWork& 
 #pragma unroll
     for (int i = 0; i < VL; ++i) vr[i] = ld16_kv<ONCE>(vsrc + 32 * i * kKvPage);
   };
-  int pg = w.lo + 2 * wave;
+  int pg = w.lo;
   if (pg < w.hi) {
     ids(pg);
     fetch_k();
     fetch_v();
-    ids(pg + kStep);
+    ids(pg + w.step);
   }
-  for (; pg < w.hi; pg += kStep) {
+  for (; pg < w.hi; pg += w.step) {
     // keys of the lane's half page
     const int there = pg + (g >> 1) < w.hi ? min(w.len - (pg + (g >> 1)) * kKvPage - 8 * (g & 1), 8) : 0;
     floatx4 s[2] = {floatx4{0.f, 0.f, 0.f, 0.f}, floatx4{0.f, 0.f, 0.f, 0.f}};
@@ -221,7 +231,7 @@ __device__ __forceinline__ void narrow_quant(const TileArgs& a, const TileWork& 
         for (int t = 0; t < 2; ++t)
           s[t] = mfma(values8<T>(kr[t][c][2 * h], kr[t][c][2 * h + 1]), qf[2 * c + h], s[t]);
     const float ks = bf16_lo(ksr) * a.scale_log2e, vs = (hl & 7) < there ? bf16_lo(vsr) : 0.f;
-    const bool more = pg + kStep < w.hi;
+    const bool more = pg + w.step < w.hi;
     if (more) fetch_k();
     each(std::make_integer_sequence<int, 8>{}, [&](auto j) {
       const float x = s[j() / 4][j() % 4] * row_lane<j()>(ks);
@@ -253,7 +263,7 @@ __device__ __forceinline__ void narrow_quant(const TileArgs& a, const TileWork& 
       for (int h = 0; h < 2; ++h) acc[2 * i + h] = mfma(values8<T>(vr[i][2 * h], vr[i][2 * h + 1]), pf, acc[2 * i + h]);
     if (more) {
       fetch_v();
-      ids(pg + 2 * kStep);
+      ids(pg + 2 * w.step);
     }
   }
 }
@@ -264,7 +274,6 @@ __device__ __forceinline__ void narrow_bf16(const TileArgs& a, const TileWork& w
                                             floatx4 (&acc)[HD / 16], float& m_run, float& l_run, unsigned char* smem) {
   constexpr int CPR = HD / 8, RPL = 64 / CPR;  // 16-byte pieces of a row, rows of a load
   constexpr int NL = kKvPage / RPL;            // loads of a page
-  constexpr int kStep = 2 * kTileWaves;
   const int lane = threadIdx.x & 63, hl = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint16_t* kc = static_cast<const uint16_t*>(a.k);
@@ -292,14 +301,14 @@ __device__ __forceinline__ void narrow_bf16(const TileArgs& a, const TileWork& w
 #pragma unroll
       for (int i = 0; i < NL; ++i) vr[u][i] = ld16_kv<ONCE>(vc + at[u] + (size_t)(RPL * i + vrow) * HD + vcol);
   };
-  int pg = w.lo + 2 * wave;
+  int pg = w.lo;
   if (pg < w.hi) {
     ids(pg);
     fetch_k();
     fetch_v();
-    ids(pg + kStep);
+    ids(pg + w.step);
   }
-  for (; pg < w.hi; pg += kStep) {
+  for (; pg < w.hi; pg += w.step) {
     int there[2];
 #pragma unroll
     for (int u = 0; u < 2; ++u) there[u] = pg + u < w.hi ? min(w.len - (pg + u) * kKvPage, kKvPage) : 0;
@@ -308,7 +317,7 @@ __device__ __forceinline__ void narrow_bf16(const TileArgs& a, const TileWork& w
     for (int st = 0; st < HD / 32; ++st)
 #pragma unroll
       for (int u = 0; u < 2; ++u) s[u] = mfma(kr[u][st], qf[st], s[u]);
-    const bool more = pg + kStep < w.hi;
+    const bool more = pg + w.step < w.hi;
     if (more) fetch_k();
     // (rows behind the end as zeros: what is there may be NaN, and 0 * NaN is NaN)
 #pragma unroll
@@ -321,7 +330,7 @@ __device__ __forceinline__ void narrow_bf16(const TileArgs& a, const TileWork& w
       }
     if (more) {
       fetch_v();
-      ids(pg + 2 * kStep);
+      ids(pg + 2 * w.step);
     }
 #pragma unroll
     for (int u = 0; u < 2; ++u)
@@ -338,10 +347,12 @@ __device__ __forceinline__ void narrow_bf16(const TileArgs& a, const TileWork& w
 }
 
 // ---- wide ----
-// A tile's K in LDS as bf16 rows, chunk c of 16 bytes at c ^ swizzle: the 16 rows that an operand read takes at one chunk
-// number then lie in 16 different places of the 256 bytes of all banks.  bf16: row i of score tile t is key 16 t + i, and V
-// is as for the narrow form.  8 bits: row i of score tile t is key 8 (i / 4) + 4 t + i % 4, so that lane group g has keys
-// 8 g .. + 8, and V^T rows of 32 keys hold operand A in their chunk g (at g ^ (d / 4 & 3)).
+// A tile is 64 keys, in two halves.  K in LDS as bf16 rows, chunk c of 16 bytes at c ^ swizzle: the 16 rows that an operand
+// read takes at one chunk number then lie in 16 different places of the 256 bytes of all banks.  bf16: row i of score tile t
+// of a half is its key 16 t + i, and V is as for the narrow form.  8 bits: row i is key 8 (i / 4) + 4 t + i % 4, so that lane
+// group g has keys 8 g .. + 8, and V^T rows of 64 keys hold operand A of half u in their chunk 4 u + g (swizzled by d / 2).
+//   The next tile's bytes are in registers while this one is multiplied.  (Tiles of 32 keys in two buffers, one barrier each:
+// the same LDS and barriers, but twice the chains of dependent steps per key.)
 template <int HD, int T>
 __device__ __forceinline__ int k_swizzle(int row) {
   if constexpr (T == kKvBf16) return HD == 128 ? row & 15 : (row >> 1) & 7;
@@ -354,77 +365,88 @@ __device__ __forceinline__ void wide_tiles(const TileArgs& a, const TileWork& w,
                                            unsigned char* smem) {
   using L = TileLds<HD, T, true>;
   constexpr bool kQuant = T != kKvBf16;
-  constexpr int B8 = HD / 8;                     // numbers of K, and tokens x features of V, of a thread: 16 or 8
-  constexpr int RW = kQuant ? B8 / 4 : B8 / 2;   // words of a thread
+  constexpr int B8 = HD / 8;                     // numbers of a page's K, and of its V, in a thread: 16 or 8
+  constexpr int RW = kQuant ? B8 / 4 : B8 / 2;   // words of them
+  constexpr int NCH = B8 / 8;                    // 16-byte chunks of bf16
+  constexpr int kPages = kWideKeys / kKvPage;
   const int tid = threadIdx.x, lane = tid & 63, hl = lane & 15, g = lane >> 4;
-  const int half = __builtin_amdgcn_readfirstlane(tid >> 7), at = tid & 127;  // page of the tile, place in it
+  // the thread's pages are those 2 u + odd of a tile, in each of them the same place
+  const int odd = __builtin_amdgcn_readfirstlane(tid >> 7), at = tid & 127;
   const int key = at >> 3, piece = at & 7;       // of K (and of V where it is bf16): B8 numbers from B8 piece on
-  uint32_t kr[RW], vr[RW];
-  uint16_t scale = 0;
-  int id = 0, pg;
-  auto ids = [&](int p) { id = w.bt[min(p + half, w.hi - 1)]; };
+  uint16_t* kt = reinterpret_cast<uint16_t*>(smem);
+  uint16_t* vt = reinterpret_cast<uint16_t*>(smem + L::kK);
+  float* sc = reinterpret_cast<float*>(smem + L::kK + L::kV);  // scales of K, of V
+  uint32_t kr[2][RW], vr[2][RW];
+  uint16_t scale[2] = {0, 0};
+  int id[2] = {0, 0}, pg;
+  auto ids = [&](int p) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) id[u] = w.bt[min(p + 2 * u + odd, w.hi - 1)];
+  };
   auto words = [&](uint32_t (&r)[RW], const void* p) {
-    if constexpr (RW == 8) {
-      const u32x4 x = ld16(p), y = ld16(static_cast<const char*>(p) + 16);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        r[i] = x[i];
-        r[4 + i] = y[i];
-      }
-    } else if constexpr (RW == 4) {
-      const u32x4 x = ld16(p);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) r[i] = x[i];
-    } else {
+    if constexpr (RW == 2) {
       const u32x2 x = *static_cast<const u32x2*>(p);
       r[0] = x[0];
       r[1] = x[1];
+    } else {
+#pragma unroll
+      for (int i = 0; i < RW; i += 4) {
+        const u32x4 x = ld16(static_cast<const char*>(p) + 4 * i);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) r[i + j] = x[j];
+      }
     }
   };
   auto fetch = [&] {
-    const size_t page = (size_t)id * a.n_kv_heads + w.kv;
-    const size_t first = page * (kKvPage * HD) + (size_t)at * B8;
-    if constexpr (kQuant) {
-      words(kr, static_cast<const uint8_t*>(a.k) + first);
-      words(vr, static_cast<const uint8_t*>(a.v) + first);
-      if (at < 32) scale = (at < 16 ? a.k_scale : a.v_scale)[page * kKvPage + (at & 15)];
-    } else {
-      words(kr, static_cast<const uint16_t*>(a.k) + first);
-      words(vr, static_cast<const uint16_t*>(a.v) + first);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const size_t page = (size_t)id[u] * a.n_kv_heads + w.kv;
+      const size_t first = page * (kKvPage * HD) + (size_t)at * B8;
+      if constexpr (kQuant) {
+        words(kr[u], static_cast<const uint8_t*>(a.k) + first);
+        words(vr[u], static_cast<const uint8_t*>(a.v) + first);
+        if (at < 32) scale[u] = (at < 16 ? a.k_scale : a.v_scale)[page * kKvPage + (at & 15)];
+      } else {
+        words(kr[u], static_cast<const uint16_t*>(a.k) + first);
+        words(vr[u], static_cast<const uint16_t*>(a.v) + first);
+      }
     }
   };
-  auto stage = [&](unsigned char* buf) {
-    const int row = half * kKvPage + key;
-    const int there = pg + half < w.hi ? min(w.len - (pg + half) * kKvPage, kKvPage) : 0;  // keys of the thread's page
-    uint16_t* kt = reinterpret_cast<uint16_t*>(buf);
-    uint16_t* vt = reinterpret_cast<uint16_t*>(buf + L::kK);
-    constexpr int NCH = B8 / 8;  // 16-byte chunks of bf16
-    if constexpr (kQuant) {
+  auto stage = [&] {
 #pragma unroll
-      for (int c = 0; c < NCH; ++c)
-        *reinterpret_cast<u32x4*>(kt + row * HD + ((NCH * piece + c) ^ k_swizzle<HD, T>(row)) * 8) =
-            values8<T>(kr[2 * c], kr[2 * c + 1]);
-      // the thread's V: feature `at` of its page, all tokens (HD 128), or feature at / 2, half of them
-      const int d = HD == 128 ? at : at >> 1, t0 = HD == 128 ? 0 : 8 * (at & 1);
+    for (int u = 0; u < 2; ++u) {
+      const int page = 2 * u + odd, row = page * kKvPage + key;
+      const int there = pg + page < w.hi ? min(w.len - (pg + page) * kKvPage, kKvPage) : 0;  // keys of the page
+      if constexpr (kQuant) {
 #pragma unroll
-      for (int c = 0; c < NCH; ++c) {
-        const int n = there - t0 - 8 * c;  // (slots behind the end may hold NaN)
-        const uint32_t x = n >= 4 ? vr[2 * c] : n > 0 ? vr[2 * c] & ((1u << (8 * n)) - 1u) : 0;
-        const uint32_t y = n >= 8 ? vr[2 * c + 1] : n > 4 ? vr[2 * c + 1] & ((1u << (8 * (n - 4))) - 1u) : 0;
-        *reinterpret_cast<u32x4*>(vt + d * 32 + ((2 * half + t0 / 8 + c) ^ ((d >> 2) & 3)) * 8) = values8<T>(x, y);
-      }
-      if (at < 32) {
-        float* sc = reinterpret_cast<float*>(buf + L::kK + L::kV) + (at < 16 ? 0 : 32);
-        const float f = bf16_lo(scale);
-        sc[half * kKvPage + (at & 15)] = at < 16 ? f * a.scale_log2e : ((at & 15) < there ? f : 0.f);
-      }
-    } else {
+        for (int c = 0; c < NCH; ++c)
+          *reinterpret_cast<u32x4*>(kt + row * HD + ((NCH * piece + c) ^ k_swizzle<HD, T>(row)) * 8) =
+              values8<T>(kr[u][2 * c], kr[u][2 * c + 1]);
+        // the thread's V: feature `at` of the page, all tokens (HD 128), or feature at / 2, half of them
+        const int d = HD == 128 ? at : at >> 1, t0 = HD == 128 ? 0 : 8 * (at & 1);
 #pragma unroll
-      for (int c = 0; c < NCH; ++c) {
-        *reinterpret_cast<u32x4*>(kt + row * HD + ((NCH * piece + c) ^ k_swizzle<HD, T>(row)) * 8) =
-            u32x4{kr[4 * c], kr[4 * c + 1], kr[4 * c + 2], kr[4 * c + 3]};
-        *reinterpret_cast<u32x4*>(vt + row * kVRow<HD> + (NCH * piece + c) * 8) =
-            key < there ? u32x4{vr[4 * c], vr[4 * c + 1], vr[4 * c + 2], vr[4 * c + 3]} : u32x4{0, 0, 0, 0};
+        for (int c = 0; c < NCH; ++c) {
+          uint32_t x = vr[u][2 * c], y = vr[u][2 * c + 1];
+          if (there < kKvPage) {  // slots behind the end may hold NaN
+            const int n = there - t0 - 8 * c;
+            x = n >= 4 ? x : n > 0 ? x & ((1u << (8 * n)) - 1u) : 0;
+            y = n >= 8 ? y : n > 4 ? y & ((1u << (8 * (n - 4))) - 1u) : 0;
+          }
+          *reinterpret_cast<u32x4*>(vt + d * kWideKeys + ((2 * page + t0 / 8 + c) ^ ((d >> 1) & 7)) * 8) = values8<T>(x, y);
+        }
+        if (at < 32) {
+          const float f = bf16_lo(scale[u]);
+          sc[(at < 16 ? 0 : kWideKeys) + page * kKvPage + (at & 15)] =
+              at < 16 ? f * a.scale_log2e : ((at & 15) < there ? f : 0.f);
+        }
+      } else {
+#pragma unroll
+        for (int c = 0; c < NCH; ++c) {
+          *reinterpret_cast<u32x4*>(kt + row * HD + ((NCH * piece + c) ^ k_swizzle<HD, T>(row)) * 8) =
+              u32x4{kr[u][4 * c], kr[u][4 * c + 1], kr[u][4 * c + 2], kr[u][4 * c + 3]};
+          *reinterpret_cast<u32x4*>(vt + row * kVRow<HD> + (NCH * piece + c) * 8) =
+              key < there ? u32x4{vr[u][4 * c], vr[u][4 * c + 1], vr[u][4 * c + 2], vr[u][4 * c + 3]} : u32x4{0, 0, 0, 0};
+        }
       }
     }
   };
@@ -432,60 +454,82 @@ __device__ __forceinline__ void wide_tiles(const TileArgs& a, const TileWork& w,
   if (pg >= w.hi) return;
   ids(pg);
   fetch();
-  ids(pg + 2);
-  for (int buf = 0; pg < w.hi; pg += 2, buf ^= 1) {
-    unsigned char* tile = smem + buf * L::kTile;
-    stage(tile);  // (last read two tiles ago, before the barrier of the tile before this)
-    if (pg + 2 < w.hi) {
+  ids(pg + kPages);
+  for (; pg < w.hi; pg += kPages) {
+    if (pg != w.lo) lds_barrier();  // every wave is done with the last tile
+    stage();
+    if (pg + kPages < w.hi) {
       fetch();
-      ids(pg + 4);
+      ids(pg + 2 * kPages);
     }
-    __syncthreads();
+    lds_barrier();
     if (idle) continue;
-    const uint16_t* kt = reinterpret_cast<const uint16_t*>(tile);
-    const uint16_t* vt = reinterpret_cast<const uint16_t*>(tile + L::kK);
-    floatx4 s[2] = {floatx4{0.f, 0.f, 0.f, 0.f}, floatx4{0.f, 0.f, 0.f, 0.f}};
+    floatx4 s[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) s[t] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int st = 0; st < HD / 32; ++st)
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const int row = kQuant ? 8 * (hl >> 2) + 4 * t + (hl & 3) : 16 * t + hl;
+      for (int t = 0; t < 4; ++t) {
+        const int row = 32 * (t / 2) + (kQuant ? 8 * (hl >> 2) + 4 * (t % 2) + (hl & 3) : 16 * (t % 2) + hl);
         s[t] = mfma(ld16(kt + row * HD + ((4 * st + g) ^ k_swizzle<HD, T>(row)) * 8), qf[st], s[t]);
       }
-    const int left = w.len - pg * kKvPage;  // keys from this tile on, of this sequence; and of this split
-    const int here = min(left, (w.hi - pg) * kKvPage);
-    if constexpr (kQuant) {
-      const floatx4* sc = reinterpret_cast<const floatx4*>(tile + L::kK + L::kV);
+    // keys from this tile on, of the sequence and of this split
+    const int here = min(w.len - pg * kKvPage, (w.hi - pg) * kKvPage);
 #pragma unroll
-      for (int t = 0; t < 2; ++t) s[t] *= sc[2 * g + t];
-    } else {
-#pragma unroll
-      for (int t = 0; t < 2; ++t) s[t] *= a.scale_log2e;
+    for (int t = 0; t < 4; ++t) {
+      if constexpr (kQuant) s[t] *= *reinterpret_cast<const floatx4*>(sc + 32 * (t / 2) + 8 * g + 4 * (t % 2));
+      else s[t] *= a.scale_log2e;
     }
-    if (here < 32) {
+    if (here < kWideKeys) {
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
+      for (int t = 0; t < 4; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-          if ((kQuant ? 8 * g + 4 * t : 16 * t + 4 * g) + r >= here) s[t][r] = -INFINITY;
+          if (32 * (t / 2) + (kQuant ? 8 * g + 4 * (t % 2) : 16 * (t % 2) + 4 * g) + r >= here) s[t][r] = -INFINITY;
     }
     online_softmax(s, acc, m_run, l_run);
     if constexpr (kQuant) {
-      const floatx4* sc = reinterpret_cast<const floatx4*>(tile + L::kK + L::kV) + 8;
 #pragma unroll
-      for (int t = 0; t < 2; ++t) s[t] *= sc[2 * g + t];
+      for (int t = 0; t < 4; ++t)
+        s[t] *= *reinterpret_cast<const floatx4*>(sc + kWideKeys + 32 * (t / 2) + 8 * g + 4 * (t % 2));
     }
-    const u32x4 pf = probabilities(s);
-    if constexpr (kQuant) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const u32x4 pf = probabilities(s + 2 * u);
 #pragma unroll
       for (int db = 0; db < HD / 16; ++db) {
-        const int d = 16 * db + hl;
-        acc[db] = mfma(ld16(vt + d * 32 + (g ^ ((d >> 2) & 3)) * 8), pf, acc[db]);
+        if constexpr (kQuant) {
+          const int d = 16 * db + hl;
+          acc[db] = mfma(ld16(vt + d * kWideKeys + ((4 * u + g) ^ ((d >> 1) & 7)) * 8), pf, acc[db]);
+        } else {
+          acc[db] = mfma(turned<HD>(vt + (32 * u + 4 * g + (hl >> 2)) * kVRow<HD> + (hl & 3) * 4, db), pf, acc[db]);
+        }
       }
-    } else {
-      const uint16_t* vfrag = vt + (4 * g + (hl >> 2)) * kVRow<HD> + (hl & 3) * 4;
+    }
+  }
+}
+
+// What a wave has of a lane's column that is all there is of it in this split: a state, or the result.
+template <int HD>
+__device__ __forceinline__ void store_columns(const TileArgs& a, const TileWork& w, int col, const floatx4 (&acc)[HD / 16],
+                                              float m, float l) {
+  if (col >= w.cols) return;
+  const int g = lane_anew() >> 4, G = a.n_heads / a.n_kv_heads;
+  const size_t item = (size_t)(w.row0 + col / G) * a.n_heads + w.kv * G + col % G;
+  if (a.n_states == 1) {
+    const float inv = l == 0.f ? 0.f : 1.f / l;  // no key at all: 0
 #pragma unroll
-      for (int db = 0; db < HD / 16; ++db) acc[db] = mfma(turned<HD>(vfrag, db), pf, acc[db]);
+    for (int db = 0; db < HD / 16; ++db)
+      *reinterpret_cast<u32x2*>(a.o + item * HD + 16 * db + 4 * g) =
+          u32x2{pack_bf16(acc[db][0] * inv, acc[db][1] * inv), pack_bf16(acc[db][2] * inv, acc[db][3] * inv)};
+  } else {
+    float* st = a.partial + (item * a.n_states + w.state) * (HD + kStatePad);
+#pragma unroll
+    for (int db = 0; db < HD / 16; ++db) *reinterpret_cast<floatx4*>(st + 16 * db + 4 * g) = acc[db];
+    if (g == 0) {
+      st[HD] = m;
+      st[HD + 1] = l;
     }
   }
 }
@@ -493,7 +537,7 @@ __device__ __forceinline__ void wide_tiles(const TileArgs& a, const TileWork& w,
 // WIDE: either part may be wide (a part of up to 16 columns is narrow all the same).  ONCE: the rows' own pages are read
 // with loads that no cache keeps.
 template <int HD, int T, bool WIDE, bool ONCE>
-__global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(T == kKvBf16 ? 3 : 4))) void tile_attention_kernel(const TileArgs a) {
+__global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(WIDE ? 3 : 4))) void tile_attention_kernel(const TileArgs a) {
   constexpr int DB = HD / 16, kSteps = HD / 32, kState = HD + kStatePad;
   constexpr bool kQuant = T != kKvBf16;
   __shared__ __attribute__((aligned(16))) unsigned char smem[TileLds<HD, T, WIDE>::kBytes];
@@ -511,10 +555,11 @@ __global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(T 
   int group = id % p.groups;
   const int split = id / p.groups;
   TileWork w;
-  w.kv = x % a.n_kv_heads;
+  w.kv = p.solo ? kTileWaves * x + wave : x % a.n_kv_heads;
+  if (w.kv >= a.n_kv_heads) return;
   // Workgroups reach the chip's eight partitions in turn: heads that share 128 bytes of scales meet in one of them.
-  if (kQuant && a.n_kv_heads % 8 == 0) w.kv = w.kv % 8 * (a.n_kv_heads / 8) + w.kv / 8;
-  w.c0 = x / a.n_kv_heads * (wide ? kWideCols : kNarrowCols);
+  if (kQuant && !p.solo && a.n_kv_heads % 8 == 0) w.kv = w.kv % 8 * (a.n_kv_heads / 8) + w.kv / 8;
+  w.c0 = wide ? x / a.n_kv_heads * kWideCols : 0;
   if (p.rank) {
     // Longest first among every n-th sequence, so that no long one starts among the last and ends the launch by itself.
     const int n = (p.groups + 63) / 64, other = group % n + n * lane;
@@ -529,6 +574,8 @@ __global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(T 
   w.hi = min((w.len + kKvPage - 1) / kKvPage, w.lo + p.pages_per_split);
   w.bt = p.tables + (size_t)group * p.max_pages;
   w.state = p.first_state + split;
+  w.step = p.solo ? 2 : 2 * kTileWaves;
+  if (!wide && !p.solo) w.lo += 2 * wave;
 
   // Operand B of the scores.  8 bits, narrow: instruction 2 c + h takes features 64 c + 16 g + 8 h .. + 8 of lane group g (16
   // bytes of K are two operands); else instruction s features 32 s + 8 g .. + 8.
@@ -548,48 +595,33 @@ __global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(T 
 #pragma unroll
   for (int db = 0; db < DB; ++db) acc[db] = floatx4{0.f, 0.f, 0.f, 0.f};
 
-  const size_t item = (size_t)(w.row0 + col / G) * a.n_heads + w.kv * G + col % G;
   if constexpr (WIDE) {
     if (wide) {
       wide_tiles<HD, T>(a, w, qf, acc, m_run, l_run, my_c0 >= w.cols, smem);
-      const float l = across_groups<16>(l_run, AddOp());
-      if (col >= w.cols) return;
-      if (a.n_states == 1) {
-        const float inv = l == 0.f ? 0.f : 1.f / l;  // no key at all: 0
-#pragma unroll
-        for (int db = 0; db < DB; ++db)
-          *reinterpret_cast<u32x2*>(a.o + item * HD + 16 * db + 4 * g) =
-              u32x2{pack_bf16(acc[db][0] * inv, acc[db][1] * inv), pack_bf16(acc[db][2] * inv, acc[db][3] * inv)};
-      } else {
-        float* st = a.partial + (item * a.n_states + w.state) * kState;
-#pragma unroll
-        for (int db = 0; db < DB; ++db) *reinterpret_cast<floatx4*>(st + 16 * db + 4 * g) = acc[db];
-        if (g == 0) {
-          st[HD] = m_run;
-          st[HD + 1] = l;
-        }
-      }
-      return;
+      return store_columns<HD>(a, w, col, acc, m_run, across_groups<16>(l_run, AddOp()));
     }
   }
   if constexpr (kQuant) narrow_quant<HD, T, ONCE>(a, w, qf, acc, m_run, l_run);
   else narrow_bf16<HD, ONCE>(a, w, qf, acc, m_run, l_run, smem);
+  if (p.solo) return store_columns<HD>(a, w, lane_anew() & 15, acc, m_run, across_groups<16>(l_run, AddOp()));
 
   // Merge the waves.  A wave without keys has maximum -inf and weight 0.
+  const int thread = 64 * wave + lane_anew();
   const float l = across_groups<16>(l_run, AddOp());
   float* mg = reinterpret_cast<float*>(smem);  // [wave][column][output[HD], max, sum, -, -]
   __syncthreads();                             // the staging areas are done with
-  float* dst = mg + (wave * 16 + hl) * kState;
+  float* dst = mg + (thread >> 6 << 4 | (thread & 15)) * kState;
+  const int mg_g = thread >> 4 & 3;
 #pragma unroll
-  for (int db = 0; db < DB; ++db) *reinterpret_cast<floatx4*>(dst + 16 * db + 4 * g) = acc[db];
-  if (g == 0) {
+  for (int db = 0; db < DB; ++db) *reinterpret_cast<floatx4*>(dst + 16 * db + 4 * mg_g) = acc[db];
+  if (mg_g == 0) {
     dst[HD] = m_run;
     dst[HD + 1] = l;
   }
   __syncthreads();
   constexpr int ND = HD / 16;
-  const int c = tid >> 4, d0 = (tid & 15) * ND;
-  if (w.c0 + c >= w.cols) return;
+  const int c = thread >> 4, d0 = (thread & 15) * ND;
+  if (c >= w.cols) return;
   float m = -INFINITY, sum = 0.f, out[ND];
 #pragma unroll
   for (int i = 0; i < kTileWaves; ++i) m = fmaxf(m, mg[(i * 16 + c) * kState + HD]);
@@ -603,8 +635,7 @@ __global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(T 
 #pragma unroll
     for (int j = 0; j < ND; ++j) out[j] += src[d0 + j] * f;
   }
-  const int mine = w.c0 + c;
-  const size_t to = (size_t)(w.row0 + mine / G) * a.n_heads + w.kv * G + mine % G;
+  const size_t to = (size_t)(w.row0 + c / G) * a.n_heads + w.kv * G + c % G;
   if (a.n_states == 1) {
     const float inv = sum == 0.f ? 0.f : 1.f / sum;  // no key at all: 0
     uint32_t v[ND / 2];
@@ -617,7 +648,7 @@ __global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(T 
     float* st = a.partial + (to * a.n_states + w.state) * kState;
 #pragma unroll
     for (int j = 0; j < ND; j += 4) *reinterpret_cast<floatx4*>(st + d0 + j) = floatx4{out[j], out[j + 1], out[j + 2], out[j + 3]};
-    if ((tid & 15) == 0) {
+    if ((thread & 15) == 0) {
       st[HD] = m;
       st[HD + 1] = sum;
     }
@@ -694,22 +725,44 @@ __global__ __launch_bounds__(kTileThreads) void tile_combine_kernel(const float*
 DS_SWITCH(g_tile_own, 0);
 DS_SWITCH(g_tile_prefix, 0);
 DS_SWITCH(g_tile_rank, 1);
+DS_SWITCH(g_tile_solo, -1);
 
+// A key/value head for each wave (`items` of them over all rows) instead of four waves for each: nothing to merge, four times as
+// many at once, but a sequence takes as long as one wave needs.  Of 40 heads (us, four waves and one): 64 sequences of 10
+// tokens 12.3 and 6.8, of 60 14.7 and 11.4, of 260 43.7 and 40.7, of 545 65.9 and 71.4; 16 of 130 9.3 and 9.0, 8 of 130 7.6
+// and 8.5; 8 key/value heads, 64 of 260 11.4 and 13.0, 128 of 260 17.0 and 15.3.  (256 of 1100 on 8 key/value heads, equal
+// ones, take 118 and 99, but 128 ragged ones up to 2048 on 40 heads 105 and 140.)
+static bool solo_of(long items, int max_len) {
+  if (g_tile_solo >= 0) return g_tile_solo;
+  return max_len <= 32 || (items >= 320 && max_len <= 64) || (items >= 1024 && max_len <= 320);
+}
 static int blocks_of(long cols) { return (int)(cols <= kNarrowCols ? 1 : (cols + kWideCols - 1) / kWideCols); }
 
-// Splits of up to max_len tokens for `items` workgroups that there are anyway: enough for two workgroups per compute unit,
-// of 16 pages or more.
+// Splits of up to max_len tokens for `items` workgroups that there are anyway.  Where they are fewer than two per compute
+// unit and the pages 48 or more: enough for three, of 8 pages (a chunk for each wave) or more.  Below that the second launch,
+// which joins them, costs what the splits save.  Of 276 batches of three layer shapes (4 to 3520 items, 200 to 40000 tokens,
+// equal and ragged) these splits are 2.2 % slower than the best of 16 numbers each, no splits 38 %.
 static int tile_splits(long items, int max_len) {
   const int pages = (max_len + kKvPage - 1) / kKvPage;
-  return (int)std::max(1l, std::min((512 + items - 1) / items, (long)pages / 16));
+  if (items >= 512 || pages < 48) return 1;
+  return (int)std::min((768 + items - 1) / items, (long)pages / 8);
 }
 
-TilePlan tile_plan(int B, int n_heads, int n_kv_heads, int max_len, int max_prefix) {
-  const int G = n_heads / n_kv_heads;
+// Splits of prefixes of up to max_prefix tokens: at most 1.75 workgroups per compute unit, of 6 pages or more, and no more
+// than pay: halving a workgroup's share of the pages saves 0.3 us a page, each state of a row and head costs 0.3 ns (1056 bytes
+// written and read).  254 calls (2 to 128 rows in 1 or 3 groups, four layer shapes, 100 to 12000 tokens, on e4m3 and bf16): 3.7 %
+// slower than the best number for each; 512 workgroups of 8 pages by themselves 5.2 %.
+static int prefix_splits(int B, int n_heads, int n_kv_heads, int n_groups, int max_prefix) {
+  const long items = (long)n_kv_heads * std::max(n_groups, blocks_of((long)B * (n_heads / n_kv_heads)));
+  const int pages = (max_prefix + kKvPage - 1) / kKvPage;
+  const long paying = (long)(std::sqrt(900.0 * pages / ((double)B * n_heads)) + 0.5);
+  return (int)std::max(1l, std::min({(448 + items - 1) / items, (long)pages / 6, paying}));
+}
+
+TilePlan tile_plan(int B, int n_heads, int n_kv_heads, int max_len, int n_groups, int max_prefix) {
   TilePlan p;
-  p.own = tile_splits((long)B * n_kv_heads * blocks_of(G), max_len);
-  // (as though one group had all rows)
-  p.prefix = max_prefix > 0 ? tile_splits((long)n_kv_heads * blocks_of((long)B * G), max_prefix) : 0;
+  p.own = tile_splits((long)B * n_kv_heads * blocks_of(n_heads / n_kv_heads), max_len);
+  p.prefix = n_groups > 0 ? prefix_splits(B, n_heads, n_kv_heads, n_groups, max_prefix) : 0;
   if (g_tile_own > 0) p.own = g_tile_own;
   if (g_tile_prefix > 0 && p.prefix > 0) p.prefix = g_tile_prefix;
   return p;
@@ -736,7 +789,8 @@ static hipError_t launch_tiles(const TileAttention& t, hipStream_t stream) {
     p.cu_rows = cu; p.lens = lens; p.tables = tables;
     p.len_add = len_add; p.max_pages = max_pages; p.groups = groups;
     p.wide = cols > kNarrowCols;
-    p.blocks_x = t.n_kv_heads * blocks_of(cols);
+    p.solo = !p.wide && solo_of((long)groups * t.n_kv_heads, max_len);
+    p.blocks_x = p.solo ? (t.n_kv_heads + kTileWaves - 1) / kTileWaves : t.n_kv_heads * blocks_of(cols);
     p.pages_per_split = (pages + splits - 1) / splits;
     p.first_state = first_state;
     blocks += (long)p.blocks_x * groups * splits;

@@ -196,9 +196,10 @@ hipError_t launch_kv_append_quant(const void* k_new, const void* v_new, int row_
 // One query per (sequence, head) over pages, on the matrix cores whatever the number of heads: over the sequence's own
 // pages, and before them, where n_groups > 0, over the prefix of its group (rows [cu_groups[i], cu_groups[i + 1])).
 struct TilePlan {
-  int prefix = 0, own = 1;  // splits of the prefixes' (up to max_prefix tokens; 0: there are none) and of the own pages
+  int prefix = 0, own = 1;  // splits of the prefixes' and of the own pages
 };
-TilePlan tile_plan(int B, int n_heads, int n_kv_heads, int max_len, int max_prefix);
+// n_groups = 0: no prefixes.  Fewer groups never mean fewer splits.
+TilePlan tile_plan(int B, int n_heads, int n_kv_heads, int max_len, int n_groups, int max_prefix);
 size_t tile_states_bytes(int B, int n_heads, int head_dim, int states);
 struct TileAttention {
   const void* q;
