@@ -1168,7 +1168,7 @@ ds_status ds_kv_migrate_quant(ds_ctx* ctx, const void* k_src, const void* v_src,
       return st;
   const ds::KvCache cache{k_cache, v_cache, k_scale, v_scale, kv_type};
   DS_LAUNCH(ctx, s, DS_K_KV_MIGRATE,
-            ds::launch_kv_migrate_quant(k_src, v_src, cu_seqlens, B, max_seqlen, block_tables, max_blocks_per_seq, cache,
+            ds::launch_kv_migrate_quant(k_src, v_src, cu_seqlens, B, t, max_seqlen, block_tables, max_blocks_per_seq, cache,
                                         ctx->cfg.n_kv_heads, ctx->cfg.head_dim, s));
   return DS_OK;
 }
@@ -1189,7 +1189,7 @@ ds_status ds_kv_read_quant(ds_ctx* ctx, const int32_t* cu_seqlens, int32_t B, in
   const ds::KvCache cache{const_cast<void*>(k_cache), const_cast<void*>(v_cache), const_cast<void*>(k_scale),
                           const_cast<void*>(v_scale), kv_type};
   DS_LAUNCH(ctx, s, DS_K_KV_MIGRATE,
-            ds::launch_kv_read_quant(cu_seqlens, B, max_seqlen, block_tables, max_blocks_per_seq, cache,
+            ds::launch_kv_read_quant(cu_seqlens, B, t, max_seqlen, block_tables, max_blocks_per_seq, cache,
                                      ctx->cfg.n_kv_heads, ctx->cfg.head_dim, k_dst, v_dst, s));
   return DS_OK;
 }

@@ -183,10 +183,10 @@ struct KvCache {
 
 // contiguous [t, n, s] -> pages of 8 bits; pages -> contiguous rows; new rows (row stride `row_stride` elements) of B
 // sequences -> slot ctx_lens[i] (negative: none).
-hipError_t launch_kv_migrate_quant(const void* k_src, const void* v_src, const int32_t* cu_seqlens, int B, int max_seqlen,
-                                   const int32_t* block_tables, int max_blocks, const KvCache& cache, int n_heads,
-                                   int head_dim, hipStream_t stream);
-hipError_t launch_kv_read_quant(const int32_t* cu_seqlens, int B, int max_seqlen, const int32_t* block_tables,
+hipError_t launch_kv_migrate_quant(const void* k_src, const void* v_src, const int32_t* cu_seqlens, int B, int t,
+                                   int max_seqlen, const int32_t* block_tables, int max_blocks, const KvCache& cache,
+                                   int n_heads, int head_dim, hipStream_t stream);
+hipError_t launch_kv_read_quant(const int32_t* cu_seqlens, int B, int t, int max_seqlen, const int32_t* block_tables,
                                 int max_blocks, const KvCache& cache, int n_heads, int head_dim, void* k_dst, void* v_dst,
                                 hipStream_t stream);
 hipError_t launch_kv_append_quant(const void* k_new, const void* v_new, int row_stride, const int32_t* ctx_lens,
