@@ -537,7 +537,8 @@ __device__ __forceinline__ void store_columns(const TileArgs& a, const TileWork&
 // WIDE: either part may be wide (a part of up to 16 columns is narrow all the same).  ONCE: the rows' own pages are read
 // with loads that no cache keeps.
 template <int HD, int T, bool WIDE, bool ONCE>
-__global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(WIDE ? 3 : 4))) void tile_attention_kernel(const TileArgs a) {
+__global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(WIDE ? 3 : 4))) void tile_attention_kernel(
+    const TileArgs a) {
   constexpr int DB = HD / 16, kSteps = HD / 32, kState = HD + kStatePad;
   constexpr bool kQuant = T != kKvBf16;
   __shared__ __attribute__((aligned(16))) unsigned char smem[TileLds<HD, T, WIDE>::kBytes];
@@ -563,13 +564,16 @@ __global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(WI
   if (p.rank) {
     // Longest first among every n-th sequence, so that no long one starts among the last and ends the launch by itself.
     const int n = (p.groups + 63) / 64, other = group % n + n * lane;
-    const int pages = other < p.groups ? max(p.lens[other] + p.len_add + kKvPage - 1, 0) / kKvPage : -1;
-    group = group % n + n * ranked(min(pages, p.max_pages), group / n, 32 - __builtin_clz(p.max_pages));
+    const int len = other < p.groups ? max(p.lens[other] + p.len_add, 0) : -2 * kKvPage;
+    const int at = ranked(min((len + kKvPage - 1) / kKvPage, p.max_pages), group / n, 32 - __builtin_clz(p.max_pages));
+    group = group % n + n * at;
+    w.len = __builtin_amdgcn_readlane(len, at);
+  } else {
+    w.len = p.lens[group] + p.len_add;
   }
   w.row0 = p.cu_rows ? p.cu_rows[group] : group;
   w.cols = (p.cu_rows ? p.cu_rows[group + 1] - w.row0 : 1) * G;
   if (w.c0 >= w.cols) return;
-  w.len = p.lens[group] + p.len_add;
   w.lo = split * p.pages_per_split;
   w.hi = min((w.len + kKvPage - 1) / kKvPage, w.lo + p.pages_per_split);
   w.bt = p.tables + (size_t)group * p.max_pages;
@@ -655,24 +659,36 @@ __global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(WI
   }
 }
 
-// The states of a (row, head) as one, in a fixed order: the same bits whenever.  Wave w takes states w, w + 4, ...: its lanes
-// have the maxima and sums of 64 of them at once, and then HD / 64 features each, the states asked for 8 at a time.
-template <int HD>
-__global__ __launch_bounds__(kTileThreads) void tile_combine_kernel(const float* __restrict__ partial, int n_states,
+// The states of a (row, head) as one, in a fixed order: the same bits whenever.  W waves take a (row, head), wave w states w,
+// w + W, ...: its lanes have the maxima and sums of 64 of them at once, and then HD / 64 features each, the states asked for 8
+// at a time.
+template <int HD, int W>
+__global__ __launch_bounds__(kTileThreads) void tile_combine_kernel(const float* __restrict__ partial, int items, int n_states,
                                                                     uint16_t* __restrict__ o) {
   constexpr int ND = HD / 64, kState = HD + kStatePad, U = 8;
-  __shared__ float merge[kTileWaves][HD + 2];
-  const size_t item = blockIdx.x;
+  __shared__ float merge[W == 1 ? 1 : W][HD + 2];
+  const int lane = threadIdx.x & 63, in_wg = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = in_wg % W;
+  const size_t item = (size_t)blockIdx.x * (kTileWaves / W) + in_wg / W;
+  if (item >= (size_t)items) return;  // (W = 1: a wave by itself; else never)
   const float* src = partial + item * n_states * kState;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   float m_run = -INFINITY, l_run = 0.f, out[ND] = {};
-  for (int s0 = wave; s0 < n_states; s0 += 64 * kTileWaves) {
-    const int n = min((n_states - s0 + kTileWaves - 1) / kTileWaves, 64);  // of them in this turn
+  for (int s0 = wave; s0 < n_states; s0 += 64 * W) {
+    const int n = min((n_states - s0 + W - 1) / W, 64);  // of them in this turn
     float m = -INFINITY, l = 0.f;
     if (lane < n) {
-      m = src[(size_t)(s0 + kTileWaves * lane) * kState + HD];
-      l = src[(size_t)(s0 + kTileWaves * lane) * kState + HD + 1];
+      m = src[(size_t)(s0 + W * lane) * kState + HD];
+      l = src[(size_t)(s0 + W * lane) * kState + HD + 1];
     }
+    float v[U][ND];
+    auto load = [&](int i0) {  // (behind the last: the last again, not used)
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const float* st = src + (size_t)(s0 + W * min(i0 + u, n - 1)) * kState + ND * lane;
+#pragma unroll
+        for (int j = 0; j < ND; ++j) v[u][j] = st[j];
+      }
+    };
+    load(0);
     float top = lane_op<1>(m, MaxOp());
     top = lane_op<2>(top, MaxOp());
     top = lane_op<kMirror4>(top, MaxOp());
@@ -684,13 +700,7 @@ __global__ __launch_bounds__(kTileThreads) void tile_combine_kernel(const float*
     for (int j = 0; j < ND; ++j) out[j] *= alpha;
     m_run = m_new;
     for (int i0 = 0; i0 < n; i0 += U) {
-      float v[U][ND];
-#pragma unroll
-      for (int u = 0; u < U; ++u) {  // (behind the last: the last again, not used)
-        const float* st = src + (size_t)(s0 + kTileWaves * min(i0 + u, n - 1)) * kState + ND * lane;
-#pragma unroll
-        for (int j = 0; j < ND; ++j) v[u][j] = st[j];
-      }
+      if (i0 > 0) load(i0);
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const float fu = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), min(i0 + u, n - 1)));
@@ -699,6 +709,12 @@ __global__ __launch_bounds__(kTileThreads) void tile_combine_kernel(const float*
           for (int j = 0; j < ND; ++j) out[j] += v[u][j] * fu;
       }
     }
+  }
+  if constexpr (W == 1) {
+    const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
+    if constexpr (ND == 2) reinterpret_cast<uint32_t*>(o)[item * 64 + lane] = pack_bf16(out[0] * inv, out[1] * inv);
+    else reinterpret_cast<__bf16*>(o)[item * HD + lane] = (__bf16)(out[0] * inv);
+    return;
   }
 #pragma unroll
   for (int j = 0; j < ND; ++j) merge[wave][ND * lane + j] = out[j];
@@ -711,9 +727,9 @@ __global__ __launch_bounds__(kTileThreads) void tile_combine_kernel(const float*
   if (d >= HD) return;
   float m = -INFINITY, sum = 0.f, r = 0.f;
 #pragma unroll
-  for (int i = 0; i < kTileWaves; ++i) m = fmaxf(m, merge[i][HD]);
+  for (int i = 0; i < W; ++i) m = fmaxf(m, merge[i][HD]);
 #pragma unroll
-  for (int i = 0; i < kTileWaves; ++i) {
+  for (int i = 0; i < W; ++i) {
     const float f = merge[i][HD] > -INFINITY ? __builtin_amdgcn_exp2f(merge[i][HD] - m) : 0.f;
     sum += merge[i][HD + 1] * f;
     r += merge[i][d] * f;
@@ -739,33 +755,43 @@ static bool solo_of(long items, int max_len) {
 static int blocks_of(long cols) { return (int)(cols <= kNarrowCols ? 1 : (cols + kWideCols - 1) / kWideCols); }
 
 // Splits of up to max_len tokens for `items` workgroups that there are anyway.  Where they are fewer than two per compute
-// unit and the pages 48 or more: enough for three, of 8 pages (a chunk for each wave) or more.  Below that the second launch,
-// which joins them, costs what the splits save.  Of 276 batches of three layer shapes (4 to 3520 items, 200 to 40000 tokens,
-// equal and ragged) these splits are 2.2 % slower than the best of 16 numbers each, no splits 38 %.
+// unit and the pages 48 or more: enough for three, of 8 pages (a chunk for each wave) or more, of 48 where there are 160
+// workgroups already.  Below that the second launch, which joins them, costs what the splits save.  Of 115 batches of three
+// layer shapes (4 to 1200 items, 500 to 60000 tokens, equal and ragged) these splits are 4 % slower than the best of up to 13
+// numbers each; 8 pages everywhere 6 %.
 static int tile_splits(long items, int max_len) {
   const int pages = (max_len + kKvPage - 1) / kKvPage;
   if (items >= 512 || pages < 48) return 1;
-  return (int)std::min((768 + items - 1) / items, (long)pages / 8);
+  return (int)std::max(1l, std::min((768 + items - 1) / items, (long)pages / (items < 160 ? 8 : 48)));
 }
 
 // Splits of prefixes of up to max_prefix tokens: at most 1.75 workgroups per compute unit, of 6 pages or more, and no more
 // than pay: halving a workgroup's share of the pages saves 0.3 us a page, each state of a row and head costs 0.3 ns (1056 bytes
 // written and read).  254 calls (2 to 128 rows in 1 or 3 groups, four layer shapes, 100 to 12000 tokens, on e4m3 and bf16): 3.7 %
 // slower than the best number for each; 512 workgroups of 8 pages by themselves 5.2 %.
-static int prefix_splits(int B, int n_heads, int n_kv_heads, int n_groups, int max_prefix) {
+//   Where the rows' own pages keep the chip busy for longer, fewer do: down to a third, since max_len may be a generous bound.
+// (40 heads, 64 rows of 16 to 256 bf16 tokens behind 2048: 7 splits 52 us, 2 of them 46.)
+static int prefix_splits(int B, int n_heads, int n_kv_heads, int n_groups, int max_prefix, double own_bytes) {
   const long items = (long)n_kv_heads * std::max(n_groups, blocks_of((long)B * (n_heads / n_kv_heads)));
   const int pages = (max_prefix + kKvPage - 1) / kKvPage;
-  const long paying = (long)(std::sqrt(900.0 * pages / ((double)B * n_heads)) + 0.5);
-  return (int)std::max(1l, std::min({(448 + items - 1) / items, (long)pages / 6, paying}));
+  const double paying = std::min(std::sqrt(900.0 * pages / ((double)B * n_heads)), (double)((448 + items - 1) / items));
+  const double own_us = own_bytes / 2 / 5.5e6;  // (half of the bound, at 5.5 TB/s)
+  const double enough = std::max(paying / 3, std::min(paying, 0.3 * pages / std::max(own_us, 1e-3)));
+  return (int)std::max(1l, std::min((long)(enough + 0.5), (long)pages / 6));
 }
 
-TilePlan tile_plan(int B, int n_heads, int n_kv_heads, int max_len, int n_groups, int max_prefix) {
+TilePlan tile_plan(int B, int n_heads, int n_kv_heads, int head_dim, int kv_type, int max_len, int n_groups, int max_prefix) {
   TilePlan p;
   p.own = tile_splits((long)B * n_kv_heads * blocks_of(n_heads / n_kv_heads), max_len);
-  p.prefix = n_groups > 0 ? prefix_splits(B, n_heads, n_kv_heads, n_groups, max_prefix) : 0;
+  const double own_bytes = (double)B * max_len * n_kv_heads * head_dim * (kv_type == kKvBf16 ? 4 : 2);
+  p.prefix = n_groups > 0 ? prefix_splits(B, n_heads, n_kv_heads, n_groups, max_prefix, own_bytes) : 0;
   if (g_tile_own > 0) p.own = g_tile_own;
   if (g_tile_prefix > 0 && p.prefix > 0) p.prefix = g_tile_prefix;
   return p;
+}
+int tile_most_states(int B, int n_heads, int n_kv_heads, int max_len, int max_prefix) {
+  return tile_splits((long)B * n_kv_heads * blocks_of(n_heads / n_kv_heads), max_len) +
+         (max_prefix > 0 ? prefix_splits(B, n_heads, n_kv_heads, 1, max_prefix, 0.0) : 0);
 }
 size_t tile_states_bytes(int B, int n_heads, int head_dim, int states) {
   return states <= 1 ? 0 : (size_t)B * n_heads * states * (head_dim + kStatePad) * sizeof(float);
@@ -818,7 +844,13 @@ static hipError_t launch_tiles(const TileAttention& t, hipStream_t stream) {
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.n_states == 1) return e;
-  hipLaunchKernelGGL(tile_combine_kernel<HD>, dim3(t.B * t.n_heads), threads, 0, stream, a.partial, a.n_states, a.o);
+  // Few states: a wave is enough for them, and a quarter of the workgroups (2560 of up to 9 states 5.6 -> 4.7 us).
+  const int items = t.B * t.n_heads;
+  if (a.n_states <= kTileWaves * 8)
+    hipLaunchKernelGGL((tile_combine_kernel<HD, 1>), dim3((items + kTileWaves - 1) / kTileWaves), threads, 0, stream, a.partial,
+                       items, a.n_states, a.o);
+  else
+    hipLaunchKernelGGL((tile_combine_kernel<HD, kTileWaves>), dim3(items), threads, 0, stream, a.partial, items, a.n_states, a.o);
   return hipGetLastError();
 }
 

@@ -491,8 +491,8 @@ size_t tile_states(const ds_ctx* ctx, int max_batch, int max_ctx, int max_prefix
   if (hit != ctx->tile_states.end()) return hit->second;
   size_t most = 0;
   for (int b = 1; b <= max_batch; ++b) {
-    const ds::TilePlan p = ds::tile_plan(b, c.n_heads, c.n_kv_heads, max_ctx, max_prefix > 0 ? 1 : 0, max_prefix);
-    most = std::max(most, ds::tile_states_bytes(b, c.n_heads, c.head_dim, p.own + p.prefix));
+    const int states = ds::tile_most_states(b, c.n_heads, c.n_kv_heads, max_ctx, max_prefix);
+    most = std::max(most, ds::tile_states_bytes(b, c.n_heads, c.head_dim, states));
   }
   most = align_up(most, 256);
   if (ctx->tile_states.size() < 4096) ctx->tile_states[key] = most;
@@ -982,7 +982,7 @@ static ds::TileAttention tile_attention(const ds_ctx* ctx, const StepCache& cach
   t.kv_len_add = kv_len_add; t.B = B; t.max_blocks = max_blocks; t.max_kv_len = max_kv_len;
   t.cache = cache.kv;
   t.n_heads = c.n_heads; t.n_kv_heads = c.n_kv_heads; t.head_dim = c.head_dim;
-  t.plan = ds::tile_plan(B, c.n_heads, c.n_kv_heads, max_kv_len, cache.n_groups, cache.max_prefix);
+  t.plan = ds::tile_plan(B, c.n_heads, c.n_kv_heads, c.head_dim, cache.kv.type, max_kv_len, cache.n_groups, cache.max_prefix);
   t.o = o; t.states = states;
   return t;
 }

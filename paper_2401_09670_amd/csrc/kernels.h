@@ -198,8 +198,9 @@ hipError_t launch_kv_append_quant(const void* k_new, const void* v_new, int row_
 struct TilePlan {
   int prefix = 0, own = 1;  // splits of the prefixes' and of the own pages
 };
-// n_groups = 0: no prefixes.  Fewer groups never mean fewer splits.
-TilePlan tile_plan(int B, int n_heads, int n_kv_heads, int max_len, int n_groups, int max_prefix);
+// n_groups = 0: no prefixes.  tile_most_states: no plan of B rows up to these lengths has more states of a row and head.
+TilePlan tile_plan(int B, int n_heads, int n_kv_heads, int head_dim, int kv_type, int max_len, int n_groups, int max_prefix);
+int tile_most_states(int B, int n_heads, int n_kv_heads, int max_len, int max_prefix);
 size_t tile_states_bytes(int B, int n_heads, int head_dim, int states);
 struct TileAttention {
   const void* q;
