@@ -12,7 +12,9 @@ Two halves, deliberately separate:
 * ``GpuStack`` - the device side: L layers of seeded random parameters, embedding tables, the KV pool,
   and the per-phase loops that call ``ds_embed`` -> L x (``ds_prefill`` + ``ds_kv_migrate``) ->
   ``ds_next_token`` and ``ds_embed`` -> L x ``ds_decode_step`` -> ``ds_next_token``.  Every step of the
-  arithmetic runs inside the library; this file only sequences calls and owns buffers.
+  arithmetic runs inside the library; this file only sequences calls and owns buffers.  With a pool of 8 bits
+  (``kv_cache`` "e4m3" or "int8") the hand-off is ``ds_kv_migrate_quant`` and the step ``ds_decode_step_quant``: a page
+  takes about half the bytes, so the same memory holds the K/V of about twice the requests.
 
 ``run_workload`` drives both over a synthetic request list and reports whole-stack prefill tokens/s,
 time per output token (mean / P50 / P90 over decoding steps), hand-off GB/s and the roofline fractions
@@ -36,6 +38,7 @@ from . import synth
 
 VOCAB = 50272      # OPT's vocabulary (Sec. 6.1 uses the OPT series)
 N_POS = 2048       # OPT's learned position table; longer contexts are clamped by ds_embed
+KV_CACHES = {"bf16": 0, "e4m3": 1, "int8": 2}   # what a pool's pages hold: the library's DS_KV_*
 
 
 # ---------------------------------------------------------------------------------------------------
@@ -232,14 +235,21 @@ def prefill_flops(lens: Sequence[int], shape: synth.ModelShape, n_layers: int, v
     return n_layers * per_layer + 2.0 * len(lens) * h * vocab
 
 
-def decode_bytes(ctx_lens: Sequence[int], shape: synth.ModelShape, n_layers: int, vocab: int) -> float:
+def kv_token_bytes(shape: synth.ModelShape, kv_cache: str = "bf16") -> int:
+    """Bytes that one token's K and V take in one layer's pool: 2 a number, or 1 and 2 for a head's row's scale."""
+    per_head = 2 * shape.head_dim if kv_cache == "bf16" else shape.head_dim + 2
+    return 2 * shape.kv_heads * per_head
+
+
+def decode_bytes(ctx_lens: Sequence[int], shape: synth.ModelShape, n_layers: int, vocab: int,
+                 kv_cache: str = "bf16") -> float:
     """Weights once + K and V of every cached token (incl. the new one) once + activations (App. A.3),
     per layer, + the vocabulary matrix once."""
     h, m = shape.hidden, shape.ffn
     B = len(ctx_lens)
     kvw = shape.kv_heads * shape.head_dim
     weights = 2.0 * (h * shape.qkv_width + h * h + 2 * h * m)
-    kv = 2.0 * 2.0 * kvw * float(sum(int(c) + 1 for c in ctx_lens))
+    kv = kv_token_bytes(shape, kv_cache) * float(sum(int(c) + 1 for c in ctx_lens))
     act = 2.0 * (8 * B * h + 2 * B * m) + 2.0 * 2 * B * kvw
     return n_layers * (weights + kv + act) + 2.0 * h * vocab
 
@@ -253,9 +263,11 @@ class GpuStack:
     def __init__(self, shape: synth.ModelShape, n_layers: int, seed: int, pool_blocks: int, max_batch: int,
                  max_prefill_tokens: int, max_ctx: int, max_blocks_per_seq: int, vocab: int = VOCAB,
                  n_pos: int = N_POS, max_requests: int = 4096, overlap_handoff: bool = False, log=lambda s: None,
-                 pool_layers: Optional[int] = None):
+                 pool_layers: Optional[int] = None, kv_cache: str = "bf16"):
         import torch
         from . import binding
+        if kv_cache not in KV_CACHES:
+            raise ValueError(f"kv_cache {kv_cache!r} is none of {', '.join(KV_CACHES)}")
         if not torch.cuda.is_available():
             raise RuntimeError("GpuStack needs a GPU")
         self.torch, self.shape, self.L = torch, shape, int(n_layers)
@@ -293,9 +305,16 @@ class GpuStack:
         # whose KV does not fit beside the weights can still be stepped through the whole stack at its true
         # shape.  Every kernel does the work it would do, the cache contents (and so the outputs) are meaningless.
         self.pool_layers = int(pool_layers or self.L)
+        self.kv_cache = kv_cache
         pool_shape = (self.pool_layers, self.num_blocks, shape.kv_heads, shape.block_size, s)
-        self.k_pool = torch.empty(pool_shape, dtype=torch.bfloat16, device=self.dev)
-        self.v_pool = torch.empty(pool_shape, dtype=torch.bfloat16, device=self.dev)
+        pool_dtype = torch.bfloat16 if kv_cache == "bf16" else torch.uint8
+        self.k_pool = torch.empty(pool_shape, dtype=pool_dtype, device=self.dev)
+        self.v_pool = torch.empty(pool_shape, dtype=pool_dtype, device=self.dev)
+        if kv_cache != "bf16":
+            # V pages of 8 bits hold a feature's 16 tokens together
+            self.v_pool = self.v_pool.view(*pool_shape[:3], s, shape.block_size)
+            self.k_scale = torch.empty(pool_shape[:4], dtype=torch.bfloat16, device=self.dev)
+            self.v_scale = torch.empty_like(self.k_scale)
 
         T = int(max_prefill_tokens)
         self.max_prefill_tokens = T
@@ -310,8 +329,10 @@ class GpuStack:
         self.ws_prefill = torch.empty(max(self.ctx.ds_prefill_workspace_bytes(T), 256) if T else 256,
                                       dtype=torch.uint8, device=self.dev)
         self.da, self.db = torch.empty((self.max_batch, h), **bf), torch.empty((self.max_batch, h), **bf)
-        self.ws_decode = torch.empty(max(self.ctx.ds_decode_workspace_bytes(self.max_batch, self.max_ctx), 256),
-                                     dtype=torch.uint8, device=self.dev)
+        decode_bytes_of = (self.ctx.ds_decode_workspace_bytes if kv_cache == "bf16"
+                           else self.ctx.ds_decode_quant_workspace_bytes)
+        self.ws_decode = torch.empty(max(decode_bytes_of(self.max_batch, self.max_ctx), 256), dtype=torch.uint8,
+                                     device=self.dev)
         self.ws_next = torch.empty(max(self.ctx.ds_next_token_workspace_bytes(256, self.vocab), 256),
                                    dtype=torch.uint8, device=self.dev)
         self.cur_tok = torch.zeros(self.max_batch, dtype=torch.int32, device=self.dev)      # per decode row
@@ -337,13 +358,35 @@ class GpuStack:
     def fill_pool_pages(self, pages: Sequence[int]) -> None:
         """Seeded N(0,1) K/V in the given pages of every layer (decode-only workloads whose contexts were
         not produced by a prefill here)."""
-        idx = self._i32(pages).long()
         bs, s, nk = self.shape.block_size, self.shape.head_dim, self.shape.kv_heads
+        if self.kv_cache != "bf16":
+            for p0 in range(0, len(pages), 1024):       # each page handed off as a sequence of its own
+                table = self._i32(np.asarray(pages[p0:p0 + 1024], np.int32).reshape(-1, 1))
+                n = table.shape[0]
+                cu = self._i32(bs * np.arange(n + 1))
+                for li in range(self.pool_layers):
+                    k, v = (self.torch.empty((n * bs, nk, s), dtype=self.torch.bfloat16, device=self.dev)
+                            .normal_(0.0, 1.0, generator=self.gen) for _ in range(2))
+                    self._hand_off(li, k, v, cu, n, n * bs, bs, table)
+            return
+        idx = self._i32(pages).long()
         for pool in (self.k_pool, self.v_pool):
             for li in range(self.pool_layers):
                 blk = self.torch.empty((len(pages), nk, bs, s), dtype=self.torch.bfloat16, device=self.dev)
                 blk.normal_(0.0, 1.0, generator=self.gen)
                 pool[li].index_copy_(0, idx, blk)
+
+    def _pool(self, li: int):
+        """What the library's calls take of layer li's pool."""
+        i = li % self.pool_layers
+        if self.kv_cache == "bf16":
+            return self.k_pool[i], self.v_pool[i], self.num_blocks
+        return (self.k_pool[i], self.v_pool[i], self.k_scale[i], self.v_scale[i], self.num_blocks,
+                KV_CACHES[self.kv_cache])
+
+    def _hand_off(self, li: int, k, v, cu, B: int, t: int, longest: int, table) -> None:
+        call = self.ctx.ds_kv_migrate if self.kv_cache == "bf16" else self.ctx.ds_kv_migrate_quant
+        call(k, v, cu, B, t, longest, table, table.shape[1], *self._pool(li))
 
     # ---- prefill phase: embed -> L x (layer, hand-off) -> first token of every prompt ----
     def prefill(self, lens: Sequence[int], rids: Sequence[int], table: np.ndarray):
@@ -377,13 +420,11 @@ class GpuStack:
                 with torch.cuda.stream(self.handoff_stream):
                     self.handoff_stream.wait_event(ready)
                     a = self._event()
-                    self.ctx.ds_kv_migrate(k_out, v_out, cu, B, t, mx, bt, table.shape[1], self.k_pool[li % self.pool_layers],
-                                           self.v_pool[li % self.pool_layers], self.num_blocks)
+                    self._hand_off(li, k_out, v_out, cu, B, t, mx, bt)
                     mig.append((a, self._event()))
             else:
                 a = self._event()
-                self.ctx.ds_kv_migrate(k_out, v_out, cu, B, t, mx, bt, table.shape[1], self.k_pool[li % self.pool_layers],
-                                       self.v_pool[li % self.pool_layers], self.num_blocks)
+                self._hand_off(li, k_out, v_out, cu, B, t, mx, bt)
                 mig.append((a, self._event()))
             if self.capture is not None and li in self.capture:
                 self.capture[li].append(dict(kind="prefill", lens=list(lens), x=x.clone(), y=y.clone(),
@@ -425,13 +466,15 @@ class GpuStack:
         x, y = self.da[:B], self.db[:B]
         start = self._event()
         self.ctx.ds_embed(ids, cl, self.tok_emb, self.vocab, self.pos_emb, self.n_pos, B, x)
+        step = self.ctx.ds_decode_step if self.kv_cache == "bf16" else self.ctx.ds_decode_step_quant
         for li in range(self.L):
-            self.ctx.ds_decode_step(self.layers[li], x, cl, bt, B, table.shape[1], max_ctx, self.k_pool[li % self.pool_layers],
-                                    self.v_pool[li % self.pool_layers], self.num_blocks, y, self.ws_decode)
+            step(self.layers[li], x, cl, bt, B, table.shape[1], max_ctx, *self._pool(li), y, self.ws_decode)
             if self.capture is not None and li in self.capture:
+                scales = {} if self.kv_cache == "bf16" else dict(k_scale=self.k_scale[li % self.pool_layers].clone(),
+                                                                 v_scale=self.v_scale[li % self.pool_layers].clone())
                 self.capture[li].append(dict(kind="decode", ctx=np.array(ctx_lens), table=np.array(table),
                                              x=x.clone(), y=y.clone(), k_pool=self.k_pool[li % self.pool_layers].clone(),
-                                             v_pool=self.v_pool[li % self.pool_layers].clone()))
+                                             v_pool=self.v_pool[li % self.pool_layers].clone(), **scales))
             x, y = y, x
         self.ctx.ds_next_token(x, None, B, self.lnf_g, self.lnf_b, self.tok_emb, self.vocab, self.next_tok, None,
                                self.ws_next)
@@ -499,7 +542,7 @@ def run_workload(stack: GpuStack, sched: Scheduler, max_steps: Optional[int] = N
     return dict(prefills=prefills, steps=steps, wall_s=time.time() - t0, finished=len(sched.finished))
 
 
-def summarise(raw: dict, shape: synth.ModelShape, n_layers: int, vocab: int = VOCAB) -> dict:
+def summarise(raw: dict, shape: synth.ModelShape, n_layers: int, vocab: int = VOCAB, kv_cache: str = "bf16") -> dict:
     """Rates and roofline fractions from run_workload's timings."""
     out = dict(finished=raw["finished"], wall_s=raw["wall_s"])
     P = raw["prefills"]
@@ -508,7 +551,8 @@ def summarise(raw: dict, shape: synth.ModelShape, n_layers: int, vocab: int = VO
         # serial hand-off: its time is taken out of the prefill figure; overlapped: it hides inside it
         ms = sum(p["ms"] - (0.0 if p.get("overlapped") else p["migrate_ms"]) for p in P)
         fl = sum(prefill_flops(p["lens"], shape, n_layers, vocab) for p in P)
-        mig_bytes = sum(2.0 * 2 * 2 * shape.kv_heads * shape.head_dim * sum(p["lens"]) for p in P) * n_layers
+        mig_bytes = sum((4.0 * shape.kv_heads * shape.head_dim + kv_token_bytes(shape, kv_cache)) * sum(p["lens"])
+                        for p in P) * n_layers
         mig_ms = sum(p["migrate_ms"] for p in P)
         out["prefill"] = dict(batches=len(P), prompts=sum(len(p["lens"]) for p in P), tokens=tok, ms=ms,
                               tokens_per_s=tok / (ms * 1e-3), tflops=fl / (ms * 1e-3) / 1e12,
@@ -519,7 +563,7 @@ def summarise(raw: dict, shape: synth.ModelShape, n_layers: int, vocab: int = VO
     S = raw["steps"]
     if S:
         ms = np.array([s["ms"] for s in S])
-        by = np.array([decode_bytes(s["ctx"], shape, n_layers, vocab) for s in S])
+        by = np.array([decode_bytes(s["ctx"], shape, n_layers, vocab, kv_cache) for s in S])
         out["decode"] = dict(steps=len(S), tokens=int(sum(s["batch"] for s in S)),
                              mean_batch=float(np.mean([s["batch"] for s in S])),
                              mean_ctx=float(np.sum([s["kv_tokens"] for s in S]) / np.sum([s["batch"] for s in S])),
@@ -557,12 +601,12 @@ def requests_for(cfg: dict, count: int) -> List[Request]:
     return reqs
 
 
-def plan_for(cfg: dict, reqs: Sequence[Request], pool_gb: float) -> dict:
+def plan_for(cfg: dict, reqs: Sequence[Request], pool_gb: float, kv_cache: str = "bf16") -> dict:
     """Buffer and pool sizes for a request list: the pool takes pool_gb of memory or what the whole list
     needs at once, whichever is smaller."""
     shape, L, bs = cfg["shape"], cfg["layers"], cfg["shape"].block_size
     life = [synth.blocks_needed(r.prompt_len + max(r.output_len - 1, 0), bs) for r in reqs]
-    page_bytes = 2 * 2 * shape.kv_heads * shape.head_dim * bs * L
+    page_bytes = kv_token_bytes(shape, kv_cache) * bs * L
     blocks = min(int(pool_gb * 1e9 // page_bytes), int(sum(life)))
     cap = cfg.get("prefill_token_cap") or max(sum(cfg.get("prefill_lens", [0])), max(r.prompt_len for r in reqs))
     longest_prompt = max((r.prompt_len for r in reqs if not r.preloaded), default=0)
@@ -571,7 +615,8 @@ def plan_for(cfg: dict, reqs: Sequence[Request], pool_gb: float) -> dict:
                 max_ctx=int(max(life)) * bs, max_batch=int(cfg["decode_batch"]))
 
 
-def timing_only_decode(cfg: dict, batch: int, steps: int, pool_gb: float, log=lambda s: None) -> dict:
+def timing_only_decode(cfg: dict, batch: int, steps: int, pool_gb: float, log=lambda s: None,
+                       kv_cache: str = "bf16") -> dict:
     """TIMING ONLY - the outputs of this run mean nothing.  Steps a decode batch of `batch` requests through the
     whole stack at the contexts the workload recipe gives (prompt + a seeded share of the output already
     generated), with every layer's weights resident but KV pools for only as many layers as fit `pool_gb`;
@@ -592,14 +637,20 @@ def timing_only_decode(cfg: dict, batch: int, steps: int, pool_gb: float, log=la
     ctx0 = (pl + np.floor(frac * np.maximum(ol - 1, 0))).astype(np.int32)      # tokens cached when timing starts
     cap = ctx0 + steps
     table, nblk = synth.make_block_tables([int(c) for c in cap], bs, seed)
-    layer_bytes = 2 * 2 * shape.kv_heads * shape.head_dim * bs * nblk
+    layer_bytes = kv_token_bytes(shape, kv_cache) * bs * nblk
     pool_layers = int(max(1, min(L, pool_gb * 1e9 // layer_bytes)))
     log(f"timing-only: batch {batch}, contexts {int(ctx0.min())}..{int(ctx0.max())} (mean {ctx0.mean():.0f}), "
         f"{nblk} pages = {layer_bytes / 1e9:.2f} GB per layer, pools for {pool_layers} of {L} layers")
     stack = GpuStack(shape, L, seed, nblk, batch, 0, int(cap.max()) + 1, table.shape[1], max_requests=batch,
-                     log=log, pool_layers=pool_layers)
-    stack.k_pool.normal_(0.0, 1.0, generator=stack.gen)
-    stack.v_pool.normal_(0.0, 1.0, generator=stack.gen)
+                     log=log, pool_layers=pool_layers, kv_cache=kv_cache)
+    for pool in (stack.k_pool, stack.v_pool):
+        if kv_cache == "bf16":
+            pool.normal_(0.0, 1.0, generator=stack.gen)
+        else:
+            pool.random_(0, 0x70, generator=stack.gen)   # bytes that are numbers in either form
+    if kv_cache != "bf16":
+        stack.k_scale.fill_(2.0 ** -6)
+        stack.v_scale.fill_(2.0 ** -6)
     stack.cur_tok.copy_(torch.randint(0, stack.vocab, (batch,), generator=stack.gen, device=stack.dev,
                                       dtype=torch.int32))
     rows = list(range(batch))
@@ -608,7 +659,7 @@ def timing_only_decode(cfg: dict, batch: int, steps: int, pool_gb: float, log=la
         ev.append((ctx0 + max(j - 2, 0), stack.decode_step(rows, ctx0 + max(j - 2, 0), table)))
     torch.cuda.synchronize()
     S = [dict(batch=batch, kv_tokens=int(c.sum()) + batch, ctx=c, ms=a.elapsed_time(b)) for c, (a, b) in ev[2:]]
-    res = summarise(dict(prefills=[], steps=S, wall_s=0.0, finished=0), shape, L)["decode"]
+    res = summarise(dict(prefills=[], steps=S, wall_s=0.0, finished=0), shape, L, kv_cache=kv_cache)["decode"]
     res.update(pool_layers=pool_layers, layers=L, layer_kv_gb=layer_bytes / 1e9, ctx_min=int(ctx0.min()),
                ctx_max=int(ctx0.max()))
     return res
@@ -636,7 +687,8 @@ def to_markdown(cfg: dict, plan: dict, n_req: int, res: dict, cmd: str) -> str:
              f"Produced by `{cmd}`; random parameters, synthetic requests (lengths from the seeded recipe, token ids "
              "random, generation greedy through the tied vocabulary matrix).", "",
              f"{n_req} requests; decode batch up to {plan['max_batch']}; prefill batches first come first served up to "
-             f"{plan['token_cap']} tokens; KV pool {plan['pool_blocks']} pages of 16 tokens = "
+             f"{plan['token_cap']} tokens; KV pool {plan['pool_blocks']} pages of 16 tokens"
+             f"{'' if plan.get('kv_cache', 'bf16') == 'bf16' else ' of ' + plan['kv_cache']} = "
              f"{plan['pool_blocks'] * plan['page_bytes'] / 1e9:.1f} GB over all layers; admission reserves a request's "
              "whole life in pages. Phases are serialised on the one GPU and timed separately.", ""]
     if "prefill" in res:
@@ -676,6 +728,8 @@ def main(argv=None) -> int:
     ap.add_argument("--max-steps", type=int, default=0)
     ap.add_argument("--overlap-handoff", action="store_true",
                     help="run each layer's KV hand-off on a second stream beside the next layer's prefill")
+    ap.add_argument("--kv-cache", choices=list(KV_CACHES), default="bf16",
+                    help="what the KV pool's pages hold: bf16, or 8 bits a number with a scale for each token and head")
     ap.add_argument("--out", type=str, default="")
     ap.add_argument("--timing-only-batch", type=int, default=0,
                     help="TIMING ONLY: step a decode batch of this size through the whole stack with KV pools for as "
@@ -688,7 +742,7 @@ def main(argv=None) -> int:
         sh, Lt = cfg["shape"], cfg["layers"]
         wgb = Lt * 2.0 * (sh.hidden * sh.qkv_width + sh.hidden ** 2 + 2 * sh.hidden * sh.ffn) / 1e9
         r = timing_only_decode(cfg, a.timing_only_batch, a.max_steps or 16, a.pool_gb or max(8.0, 250.0 - wgb),
-                               log=lambda s: print(f"[instance] {s}", flush=True))
+                               log=lambda s: print(f"[instance] {s}", flush=True), kv_cache=a.kv_cache)
         md = timing_only_markdown(cfg, r, "python -m paper_2401_09670_amd.instance "
                                   + " ".join(argv if argv is not None else sys.argv[1:]))
         print(md)
@@ -702,7 +756,7 @@ def main(argv=None) -> int:
     shape, L = cfg["shape"], cfg["layers"]
     weight_gb = L * 2.0 * (shape.hidden * shape.qkv_width + shape.hidden ** 2 + 2 * shape.hidden * shape.ffn) / 1e9
     pool_gb = a.pool_gb or max(8.0, min(160.0, 250.0 - weight_gb))
-    plan = plan_for(cfg, reqs, pool_gb)
+    plan = dict(plan_for(cfg, reqs, pool_gb, a.kv_cache), kv_cache=a.kv_cache)
 
     def log(s):
         print(f"[instance] {s}", flush=True)
@@ -711,11 +765,11 @@ def main(argv=None) -> int:
         f"({plan['pool_blocks'] * plan['page_bytes'] / 1e9:.1f} GB)")
     stack = GpuStack(shape, L, cfg["seed"], plan["pool_blocks"], plan["max_batch"], plan["max_prefill_tokens"],
                      plan["max_ctx"], plan["max_blocks"], max_requests=len(reqs), overlap_handoff=a.overlap_handoff,
-                     log=log)
+                     log=log, kv_cache=a.kv_cache)
     sched = Scheduler(reqs, BlockPool(plan["pool_blocks"], cfg["seed"]), plan["max_batch"], plan["token_cap"],
                       shape.block_size, plan["max_blocks"])
     raw = run_workload(stack, sched, a.max_steps or None, log)
-    res = summarise(raw, shape, L)
+    res = summarise(raw, shape, L, kv_cache=a.kv_cache)
     cmd = "python -m paper_2401_09670_amd.instance " + " ".join(argv if argv is not None else sys.argv[1:])
     md = to_markdown(cfg, plan, len(reqs), res, cmd)
     print(md)
