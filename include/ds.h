@@ -99,7 +99,9 @@ const char *ds_last_error(const ds_ctx *ctx);
  * ds_prefill, ds_prefill_attention and ds_kv_migrate check cu_seqlens (starts at 0, ends at t, every
  * length in [1, max_seqlen]); ds_kv_migrate, ds_decode_step and ds_decode_attention check that every
  * page a sequence's tokens need is named in block_tables with an id in [0, num_blocks), and that
- * ctx_lens[i] + 1 lies in [1, max_ctx] (kv_lens[i] in [0, max_kv_len]). */
+ * ctx_lens[i] + 1 lies in [1, max_ctx] (kv_lens[i] in [0, max_kv_len]).  The calls for 8 bits and for shared prefixes
+ * check the same, cu_groups (from 0 to B, no group above max_group_rows), the prefixes' lengths and pages, and that no
+ * two rows append to one page of 8 bits. */
 ds_status ds_set_validate(ds_ctx *ctx, int32_t on);
 
 /* Workspace (device bytes) for ds_prefill with up to max_tokens packed tokens.
@@ -294,7 +296,8 @@ ds_status ds_kv_read_quant(ds_ctx *ctx, const int32_t *cu_seqlens, int32_t B, in
 /* One new row of K and V for each of B sequences, written at position ctx_lens[i] (tokens before it; its page must be in
  * block_tables).  Row i starts row_stride * i elements (a multiple of 8, at least n_kv s) behind k_new / v_new: they may
  * point into the rows of a QKV product.  ctx_lens[i] = -1 marks a row that only pads the batch: nothing is written for
- * it.  No two rows may name the same slot. */
+ * it.  No two rows of a call may write into the same page: the pieces of a V page that hold the new token are read, changed
+ * and written whole (the debug validation checks it). */
 ds_status ds_kv_append_quant(ds_ctx *ctx, const void *k_new, const void *v_new, int32_t row_stride,
                              const int32_t *ctx_lens, const int32_t *block_tables, int32_t B,
                              int32_t max_blocks_per_seq, void *k_cache, void *v_cache, void *k_scale, void *v_scale,
@@ -311,6 +314,7 @@ ds_status ds_decode_attention_quant(ds_ctx *ctx, const void *q, const int32_t *k
 
 /* ds_decode_step on such a cache: the new token's rows are quantised, appended, and attended over as they then stand.
  * ctx_lens[i] = -1: a row that pads the batch (nothing is appended, its attention is 0, its y is the layer's of that).
+ * As for ds_kv_append_quant no two rows write into the same page.
  * A workspace below what ds_decode_quant_workspace_bytes reports may serve with plans of the products that split less. */
 ds_status ds_decode_step_quant(ds_ctx *ctx, const ds_layer_weights *w, const void *x, const int32_t *ctx_lens,
                                const int32_t *block_tables, int32_t B, int32_t max_blocks_per_seq, int32_t max_ctx,
@@ -336,7 +340,8 @@ ds_status ds_decode_attention_shared(ds_ctx *ctx, const void *q, const int32_t *
                                      size_t workspace_bytes, void *stream);
 
 /* ds_decode_step for such rows, on a cache of any kv_type: ctx_lens[i] own tokens before this step (the prefix not
- * counted), the new one appended behind them. */
+ * counted), the new one appended behind them, into a page that is no other row's and no prefix's.  On 8 bits a row of
+ * ctx_lens[i] = -1 appends nothing and attends over its group's prefix alone; with DS_KV_BF16 ctx_lens[i] >= 0. */
 ds_status ds_decode_step_shared(ds_ctx *ctx, const ds_layer_weights *w, const void *x, const int32_t *cu_groups,
                                 int32_t n_groups, int32_t max_group_rows, const int32_t *prefix_lens,
                                 const int32_t *prefix_tables, int32_t max_prefix_blocks, int32_t max_prefix_len,

@@ -15,8 +15,8 @@
 // (group, key/value head, block of columns, split of the pages) of either part:
 //  * narrow, up to 16 columns: the waves take turns by chunks of 32 keys, from global memory straight to registers, and
 //    their states (maximum, sum, output) are merged through LDS.  HBM bounds it.
-//  * wide, 64 columns: each wave has 16 of them, and all see the same tiles of 32 keys, which the workgroup brings to bf16
-//    and into LDS once.
+//  * wide, 64 columns: each wave has 16 of them, and all see the same tiles of 64 keys, which the workgroup brings to bf16
+//    and into LDS once.  What a tile takes in LDS accesses and softmax bounds it, not its bytes.
 // Where a (row, head) has more than one state, they are written out in fp32 and a second launch merges them in order.
 #include <algorithm>
 #include <cmath>
@@ -34,7 +34,7 @@ struct TilePart {
   const int32_t* cu_rows;  // group i has the rows [cu_rows[i], cu_rows[i + 1]); null: row i
   const int32_t* lens;
   const int32_t* tables;
-  int len_add, max_pages, groups;
+  int len_add, max_len, max_pages, groups;
   int blocks_x;            // key/value heads x blocks of columns
   int pages_per_split;
   int first_state;         // states of this part's splits
@@ -571,6 +571,7 @@ __global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(WI
   } else {
     w.len = p.lens[group] + p.len_add;
   }
+  w.len = min(w.len, p.max_len);
   w.row0 = p.cu_rows ? p.cu_rows[group] : group;
   w.cols = (p.cu_rows ? p.cu_rows[group + 1] - w.row0 : 1) * G;
   if (w.c0 >= w.cols) return;
@@ -813,7 +814,7 @@ static hipError_t launch_tiles(const TileAttention& t, hipStream_t stream) {
                   int groups, long cols, int max_len, int splits, int first_state) {
     const int pages = (max_len + kKvPage - 1) / kKvPage;
     p.cu_rows = cu; p.lens = lens; p.tables = tables;
-    p.len_add = len_add; p.max_pages = max_pages; p.groups = groups;
+    p.len_add = len_add; p.max_len = max_len; p.max_pages = max_pages; p.groups = groups;
     p.wide = cols > kNarrowCols;
     p.solo = !p.wide && solo_of((long)groups * t.n_kv_heads, max_len);
     p.blocks_x = p.solo ? (t.n_kv_heads + kTileWaves - 1) / kTileWaves : t.n_kv_heads * blocks_of(cols);

@@ -12,6 +12,7 @@
 #include <mutex>
 #include <new>
 #include <tuple>
+#include <unordered_map>
 #include <utility>
 #include <vector>
 
@@ -432,6 +433,23 @@ ds_status validate_lens(ds_ctx* ctx, const char* who, const int32_t* lens_dev, i
       return fail(ctx, DS_ERR_BOUNDS, "%s: sequence %d attends over %ld tokens, outside [%d, %d]", who, i, l, lo,
                   bound);
     tokens[i] = (int32_t)l;
+  }
+  return DS_OK;
+}
+
+// No two rows of a call write into one page (tokens[i]: the row's with the new one; 0: it writes nothing).
+ds_status validate_new_pages(ds_ctx* ctx, const char* who, const int32_t* bt_dev, int B, int max_blocks,
+                             const std::vector<int32_t>& tokens, hipStream_t s) {
+  std::vector<int32_t> bt;
+  ds_status st = fetch_i32(ctx, bt_dev, (size_t)B * max_blocks, s, bt);
+  if (st != DS_OK) return st;
+  std::unordered_map<int32_t, int> writer;
+  for (int i = 0; i < B; ++i) {
+    if (tokens[i] <= 0) continue;
+    const int32_t id = bt[(size_t)i * max_blocks + (tokens[i] - 1) / ctx->cfg.block_size];
+    const auto first = writer.emplace(id, i);
+    if (!first.second)
+      return fail(ctx, DS_ERR_BOUNDS, "%s: rows %d and %d both write into block %d", who, first.first->second, i, id);
   }
   return DS_OK;
 }
@@ -905,6 +923,8 @@ static ds_status check_cache(ds_ctx* ctx, const char* who, const void* k, const 
   return DS_OK;
 }
 
+constexpr int32_t kMostTokens = INT32_MAX - 1024;  // of a sequence or prefix on pages in tiles: their positions are 32 bits
+
 // Packed rows and the pages of their sequences.
 static ds_status check_rows(ds_ctx* ctx, const char* who, const void* k_rows, const void* v_rows, const int32_t* cu_seqlens,
                             int32_t B, int32_t t, int32_t max_seqlen, const int32_t* block_tables, int32_t max_blocks) {
@@ -932,7 +952,7 @@ static ds_status check_groups(ds_ctx* ctx, const char* who, const int32_t* cu_gr
                               int32_t max_group_rows, const int32_t* prefix_lens, const int32_t* prefix_tables,
                               int32_t max_prefix_blocks, int32_t max_prefix_len, int32_t B) {
   if (!cu_groups || !prefix_lens || !prefix_tables) return fail(ctx, DS_ERR_INVALID_ARG, "%s: NULL pointer", who);
-  if (n_groups <= 0 || max_group_rows <= 0 || max_prefix_blocks <= 0 || max_prefix_len <= 0 ||
+  if (n_groups <= 0 || max_group_rows <= 0 || max_prefix_blocks <= 0 || max_prefix_len <= 0 || max_prefix_len > kMostTokens ||
       (int64_t)n_groups * max_group_rows < B)
     return fail(ctx, DS_ERR_INVALID_ARG, "%s: non-positive size, or groups that cannot hold %d rows", who, B);
   if ((int64_t)max_prefix_blocks * ctx->cfg.block_size < max_prefix_len)
@@ -1001,7 +1021,7 @@ static ds_status decode_step(ds_ctx* ctx, const ds_layer_weights* w, const void*
     return fail(ctx, DS_ERR_INVALID_ARG, "%s: NULL pointer", who);
   if (B <= 0 || max_ctx <= 0 || num_blocks <= 0 || max_blocks_per_seq <= 0)
     return fail(ctx, DS_ERR_INVALID_ARG, "%s: non-positive size", who);
-  if ((int64_t)max_blocks_per_seq * ctx->cfg.block_size < max_ctx)
+  if ((int64_t)max_blocks_per_seq * ctx->cfg.block_size < max_ctx || (cache.tiles && max_ctx > kMostTokens))
     return fail(ctx, DS_ERR_INVALID_ARG, "%s: max_ctx %d does not fit %d blocks per sequence", who, max_ctx,
                 max_blocks_per_seq);
   if (x == y) return fail(ctx, DS_ERR_INVALID_ARG, "%s: y must not alias x", who);
@@ -1033,6 +1053,9 @@ static ds_status decode_step(ds_ctx* ctx, const ds_layer_weights* w, const void*
     std::vector<int32_t> lens;
     if ((st = validate_lens(ctx, who, ctx_lens, B, 1, cache.kv.type == ds::kKvBf16 ? 1 : 0, max_ctx, s, lens)) != DS_OK) return st;
     if ((st = validate_tables(ctx, who, block_tables, B, max_blocks_per_seq, num_blocks, lens, s)) != DS_OK) return st;
+    if (cache.kv.type != ds::kKvBf16 &&
+        (st = validate_new_pages(ctx, who, block_tables, B, max_blocks_per_seq, lens, s)) != DS_OK)
+      return st;
     if (cache.n_groups > 0 &&
         (st = validate_groups(ctx, who, cache.cu_groups, cache.n_groups, cache.max_group_rows, B, cache.prefix_lens,
                               cache.prefix_tables, cache.max_prefix_blocks, cache.max_prefix, num_blocks, s)) != DS_OK)
@@ -1213,6 +1236,7 @@ ds_status ds_kv_append_quant(ds_ctx* ctx, const void* k_new, const void* v_new, 
     const int most = (int)std::min<int64_t>((int64_t)max_blocks_per_seq * ctx->cfg.block_size, INT32_MAX);
     if (ds_status st = validate_lens(ctx, who, ctx_lens, B, 1, 0, most, s, lens)) return st;
     if (ds_status st = validate_tables(ctx, who, block_tables, B, max_blocks_per_seq, num_blocks, lens, s)) return st;
+    if (ds_status st = validate_new_pages(ctx, who, block_tables, B, max_blocks_per_seq, lens, s)) return st;
   }
   const ds::KvCache cache{k_cache, v_cache, k_scale, v_scale, kv_type};
   DS_LAUNCH(ctx, s, DS_K_KV_APPEND,
@@ -1226,7 +1250,7 @@ static ds_status paged_attention(ds_ctx* ctx, const char* who, const void* q, co
                                  const int32_t* block_tables, int32_t B, int32_t max_blocks_per_seq, int32_t max_kv_len,
                                  int32_t num_blocks, void* o, void* workspace, size_t workspace_bytes, void* stream) {
   if (!q || !kv_lens || !block_tables || !o) return fail(ctx, DS_ERR_INVALID_ARG, "%s: NULL pointer", who);
-  if (B <= 0 || max_kv_len <= 0 || max_blocks_per_seq <= 0 ||
+  if (B <= 0 || max_kv_len <= 0 || max_kv_len > kMostTokens || max_blocks_per_seq <= 0 ||
       (int64_t)max_blocks_per_seq * ctx->cfg.block_size < max_kv_len)
     return fail(ctx, DS_ERR_INVALID_ARG, "%s: non-positive or inconsistent size", who);
   if (!aligned16(q) || !aligned16(o) || !aligned16(workspace))

@@ -1,0 +1,93 @@
+"""Pages of 8 bits with many sequences of unlike lengths, heads dealt out to single waves, bounds below the lengths, and rows
+that would write into one page."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import kv_quant_oracle as kvo
+from oracle import ds_oracle as orc
+from paper_2401_09670_amd import binding, synth
+from tests import gpu_util as gu
+from tests.kv_pages import KINDS, Cache, rows
+from tests.test_gpu_kv_quant import _expect, _poisoned, _same
+from tests.test_gpu_paged_attention import _attend, _check, _check_shared, _ctx, _groups, _shared
+from tests.test_gpu_quant_steps import _bounds, _pages
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("kind", ["e4m3", "int8"])
+@pytest.mark.parametrize("n,s,B", [(5, 64, 200), (2, 128, 65), (9, 128, 64)])
+def test_hand_off_of_many_prompts(gpu, n, s, B, kind):
+    rng, k = np.random.default_rng(B), KINDS[kind]
+    lens = [int(l) for l in np.where(rng.random(B) < 0.1, rng.integers(100, 200, B), rng.integers(1, 36, B))]
+    t = sum(lens)
+    k_bits, v_bits = rows(rng, t, n, s), rows(rng, t, n, s)
+    table, nb = synth.make_block_tables(lens, 16, 2)
+    before = _poisoned(nb, n, s)
+    pages = tuple(x.clone() for x in before)
+    ctx, cu, bt = _ctx(n, n, s), gu.i32_dev(synth.cu_seqlens(lens)), gu.i32_dev(table)
+    ctx.ds_kv_migrate_quant(gu.to_dev(k_bits), gu.to_dev(v_bits), cu, B, t, max(lens), bt, table.shape[1], *pages, nb, k)
+    _same(pages, _expect(before, k, k_bits, v_bits, lens, table))
+    back = torch.empty((2, t, n, s), dtype=torch.bfloat16, device="cuda")
+    ctx.ds_kv_read_quant(cu, B, t, max(lens), bt, table.shape[1], *pages, nb, k, back[0], back[1])
+    torch.cuda.synchronize()
+    for got, bits in zip(back, (k_bits, v_bits)):
+        stands = kvo.stands_for(*kvo.quantise(orc.from_bf16_bits(bits), k), k)
+        want = synth.bf16_bits_to_f32(synth.f32_to_bf16_bits(stands.astype(np.float32)))
+        assert np.array_equal(gu.to_f64(got), want)
+
+
+@pytest.mark.parametrize("kind", ["e4m3", "int8"])
+@pytest.mark.parametrize("n,n_kv,s,most,B", [(5, 5, 64, 32, 70), (6, 3, 128, 30, 3), (8, 8, 128, 300, 130), (14, 7, 64, 64, 150)])
+def test_a_head_for_each_wave(gpu, n, n_kv, s, most, B, kind):
+    """Short sequences: no merge, and key/value heads that do not fill a workgroup's waves."""
+    rng = np.random.default_rng(n)
+    lens = [0, most, 1] + [int(l) for l in rng.integers(0, most + 1, B - 3)]
+    c = Cache(kind, lens, n_kv, s, seed=n)
+    q = gu.to_dev(rows(rng, B, n, s))
+    _check(_attend(_ctx(n, n_kv, s), q, c), q, c, n, s)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+def test_many_rows_behind_many_prefixes(gpu, kind):
+    n, n_kv, s, g = 4, 2, 64, 70
+    rng = np.random.default_rng(4)
+    rows_of = [int(r) for r in rng.integers(0, 4, g)]
+    prefix, own = [int(p) for p in rng.integers(0, 90, g)], [int(l) for l in rng.integers(0, 50, sum(rows_of))]
+    c, cu = _groups(rows_of, prefix, own, n_kv, s, kind, 3)
+    q = gu.to_dev(rows(rng, len(own), n, s))
+    _check_shared(_shared(_ctx(n, n_kv, s), q, c, cu, prefix, own), q, c, cu, s)
+
+
+@pytest.mark.parametrize("B,bound,lens", [(2, 100, [130, 40]), (1, 1000, [1100]), (3, 17, [500, 16, 18])])
+def test_a_bound_below_the_lengths_drops_the_rest(gpu, B, bound, lens):
+    n, s = 4, 64
+    c = Cache("e4m3", lens, n, s, seed=4)
+    q = gu.to_dev(rows(np.random.default_rng(1), B, n, s))
+    kept = [min(l, bound) for l in lens]
+    ctx = _ctx(n, n, s)
+    o = _attend(ctx, q, c, max_len=bound)
+    _check(o, q, c, n, s, lens=kept)
+    assert torch.equal(o, _attend(ctx, q, c, lens=kept, max_len=bound))
+
+
+def test_two_rows_into_one_page_are_named(gpu):
+    shape = synth.TINY
+    ctx, h = gu.make_ctx(shape), shape.hidden
+    ctx.ds_set_validate(True)
+    lw, _keep = gu.weights_to_dev(synth.make_layer_weights(shape, 1))
+    x, y = (torch.zeros(3, h, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    bt = gu.i32_dev([[0, 1], [2, 3], [4, 1]])
+    ws = gu.workspace(ctx.ds_decode_shared_workspace_bytes(3, 32, 32))
+    groups = (gu.i32_dev([0, 3]), 1, 3, gu.i32_dev([20]), gu.i32_dev([[6, 7]]), 2, 32)
+    for kind in (binding.KV_E4M3, binding.KV_INT8):
+        cache = (*_pages(kind, 8, shape), 8, kind)
+        new = torch.zeros(3, shape.kv_heads, shape.head_dim, dtype=torch.bfloat16, device="cuda")
+        calls = [lambda l: ctx.ds_kv_append_quant(new, new, shape.kv_heads * shape.head_dim, l, bt, 3, 2, *cache),
+                 lambda l: ctx.ds_decode_step_quant(lw, x, l, bt, 3, 2, 32, *cache, y, ws),
+                 lambda l: ctx.ds_decode_step_shared(lw, x, *groups, l, bt, 3, 2, 32, *cache, y, ws)]
+        for call in calls:
+            call(gu.i32_dev([16, 5, 15]))       # (page 1 of the first row alone)
+            call(gu.i32_dev([-1, 5, 16]))
+            _bounds(lambda: call(gu.i32_dev([17, 5, 30])), "rows 0 and 2 both write into block 1")
