@@ -535,9 +535,9 @@ __device__ __forceinline__ void store_columns(const TileArgs& a, const TileWork&
 }
 
 // WIDE: either part may be wide (a part of up to 16 columns is narrow all the same).  ONCE: the rows' own pages are read
-// with loads that no cache keeps.
-template <int HD, int T, bool WIDE, bool ONCE>
-__global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(WIDE ? 3 : 4))) void tile_attention_kernel(
+// with loads that no cache keeps.  JOINED: part 0 has no workgroups, a row's take its group's prefix and then its own pages.
+template <int HD, int T, bool WIDE, bool ONCE, bool JOINED>
+__global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(WIDE || (JOINED && T == kKvBf16) ? 3 : 4))) void tile_attention_kernel(
     const TileArgs a) {
   constexpr int DB = HD / 16, kSteps = HD / 32, kState = HD + kStatePad;
   constexpr bool kQuant = T != kKvBf16;
@@ -606,8 +606,26 @@ __global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(WI
       return store_columns<HD>(a, w, col, acc, m_run, across_groups<16>(l_run, AddOp()));
     }
   }
-  if constexpr (kQuant) narrow_quant<HD, T, ONCE>(a, w, qf, acc, m_run, l_run);
-  else narrow_bf16<HD, ONCE>(a, w, qf, acc, m_run, l_run, smem);
+  TileWork next;
+  if constexpr (JOINED) {
+    const TilePart& pre = a.part[0];
+    int of = 0;  // the row's group: as many end at the row or before
+    for (int i0 = 0; i0 < pre.groups; i0 += 64)
+      of += __builtin_popcountll(
+          __builtin_amdgcn_ballot_w64(i0 + lane < pre.groups && pre.cu_rows[min(i0 + lane, pre.groups - 1) + 1] <= group));
+    of = min(of, pre.groups - 1);
+    next = w;
+    w.len = min(pre.lens[of], pre.max_len);
+    w.hi = (w.len + kKvPage - 1) / kKvPage;
+    w.bt = pre.tables + (size_t)of * pre.max_pages;
+    if (!p.solo) next.lo = 2 * ((wave - (w.hi + 1) / 2) & (kTileWaves - 1));  // (the wave whose turn it is)
+  }
+#pragma unroll 1
+  for (int seg = JOINED ? 0 : 1; seg < 2; ++seg) {
+    if constexpr (kQuant) narrow_quant<HD, T, ONCE>(a, w, qf, acc, m_run, l_run);
+    else narrow_bf16<HD, ONCE>(a, w, qf, acc, m_run, l_run, smem);
+    if constexpr (JOINED) w = next;
+  }
   if (p.solo) return store_columns<HD>(a, w, lane_anew() & 15, acc, m_run, across_groups<16>(l_run, AddOp()));
 
   // Merge the waves.  A wave without keys has maximum -inf and weight 0.
@@ -739,17 +757,19 @@ __global__ __launch_bounds__(kTileThreads) void tile_combine_kernel(const float*
 }
 
 // ---- plans ----
+constexpr double kOnceBytes = 256e6;  // of own pages: more than the last-level cache could keep until the next step
 DS_SWITCH(g_tile_own, 0);
 DS_SWITCH(g_tile_prefix, 0);
 DS_SWITCH(g_tile_rank, 1);
 DS_SWITCH(g_tile_solo, -1);
+DS_SWITCH(g_tile_join, -1);
 
 // A key/value head for each wave (`items` of them over all rows) instead of four waves for each: nothing to merge, four times as
 // many at once, but a sequence takes as long as one wave needs.  Of 40 heads (us, four waves and one): 64 sequences of 10
 // tokens 12.3 and 6.8, of 60 14.7 and 11.4, of 260 43.7 and 40.7, of 545 65.9 and 71.4; 16 of 130 9.3 and 9.0, 8 of 130 7.6
 // and 8.5; 8 key/value heads, 64 of 260 11.4 and 13.0, 128 of 260 17.0 and 15.3.  (256 of 1100 on 8 key/value heads, equal
 // ones, take 118 and 99, but 128 ragged ones up to 2048 on 40 heads 105 and 140.)
-static bool solo_of(long items, int max_len) {
+static bool solo_of(long items, long max_len) {
   if (g_tile_solo >= 0) return g_tile_solo;
   return max_len <= 32 || (items >= 320 && max_len <= 64) || (items >= 1024 && max_len <= 320);
 }
@@ -760,10 +780,10 @@ static int blocks_of(long cols) { return (int)(cols <= kNarrowCols ? 1 : (cols +
 // workgroups already.  Below that the second launch, which joins them, costs what the splits save.  Of 115 batches of three
 // layer shapes (4 to 1200 items, 500 to 60000 tokens, equal and ragged) these splits are 4 % slower than the best of up to 13
 // numbers each; 8 pages everywhere 6 %.
-static int tile_splits(long items, int max_len) {
-  const int pages = (max_len + kKvPage - 1) / kKvPage;
+static int tile_splits(long items, long max_len) {
+  const long pages = (max_len + kKvPage - 1) / kKvPage;
   if (items >= 512 || pages < 48) return 1;
-  return (int)std::max(1l, std::min((768 + items - 1) / items, (long)pages / (items < 160 ? 8 : 48)));
+  return (int)std::max(1l, std::min((768 + items - 1) / items, pages / (items < 160 ? 8 : 48)));
 }
 
 // Splits of prefixes of up to max_prefix tokens: at most 1.75 workgroups per compute unit, of 6 pages or more, and no more
@@ -781,11 +801,30 @@ static int prefix_splits(int B, int n_heads, int n_kv_heads, int n_groups, int m
   return (int)std::max(1l, std::min((long)(enough + 0.5), (long)pages / 6));
 }
 
+// One launch in which every row reads its group's prefix for itself, and no states: where the prefix is short or the rows are
+// few.  The bytes read again, out of caches, cost 0.1 us a MB, the states of a row and head 0.25 ns each, the second launch 2.4
+// us.  836 calls (1 to 160 rows in 1 or 4 groups, three layer shapes, prefixes of 16 to 800 tokens, own tokens up to 700, all
+// types): 0.4 % slower than the better way for each; two parts always 23 %, joined always 11 %.  (us, two parts and joined: 5
+// rows of 4 heads behind 45 tokens 7.6 and 5.0; e4m3, 64 rows of 64 heads on 8 behind 200 11.8 and 8.3; 64 rows of 40 heads
+// behind 200 11.9 and 21.3.)
+static bool joined_of(int splits, int B, int n_heads, int n_kv_heads, int head_dim, int kv_type, int max_len, int max_prefix,
+                      double own_bytes) {
+  const int G = n_heads / n_kv_heads;
+  if (G > kNarrowCols || own_bytes > kOnceBytes) return false;
+  if (tile_splits((long)B * n_kv_heads, (long)max_len + max_prefix) > 1) return false;
+  if (g_tile_join >= 0) return g_tile_join;
+  const double again = (double)B * max_prefix * n_kv_heads * head_dim * (kv_type == kKvBf16 ? 4 : 2);
+  return again * 0.1e-6 < 2.4 + 0.25e-3 * B * n_heads * (splits + 1.0);
+}
+
 TilePlan tile_plan(int B, int n_heads, int n_kv_heads, int head_dim, int kv_type, int max_len, int n_groups, int max_prefix) {
   TilePlan p;
   p.own = tile_splits((long)B * n_kv_heads * blocks_of(n_heads / n_kv_heads), max_len);
   const double own_bytes = (double)B * max_len * n_kv_heads * head_dim * (kv_type == kKvBf16 ? 4 : 2);
-  p.prefix = n_groups > 0 ? prefix_splits(B, n_heads, n_kv_heads, n_groups, max_prefix, own_bytes) : 0;
+  if (n_groups > 0) {
+    p.prefix = prefix_splits(B, n_heads, n_kv_heads, n_groups, max_prefix, own_bytes);
+    p.joined = joined_of(p.prefix, B, n_heads, n_kv_heads, head_dim, kv_type, max_len, max_prefix, own_bytes);
+  }
   if (g_tile_own > 0) p.own = g_tile_own;
   if (g_tile_prefix > 0 && p.prefix > 0) p.prefix = g_tile_prefix;
   return p;
@@ -807,41 +846,47 @@ static hipError_t launch_tiles(const TileAttention& t, hipStream_t stream) {
   a.k_scale = (const uint16_t*)t.cache.k_scale; a.v_scale = (const uint16_t*)t.cache.v_scale;
   a.n_heads = t.n_heads; a.n_kv_heads = t.n_kv_heads;
   a.scale_log2e = 1.4426950408889634f / sqrtf((float)HD);
-  a.n_states = t.plan.prefix + t.plan.own;
+  a.n_states = t.plan.joined ? 1 : t.plan.prefix + t.plan.own;
   a.o = (uint16_t*)t.o; a.partial = (float*)t.states;
   long blocks = 0;
   auto part = [&](TilePart& p, const int32_t* cu, const int32_t* lens, const int32_t* tables, int len_add, int max_pages,
-                  int groups, long cols, int max_len, int splits, int first_state) {
-    const int pages = (max_len + kKvPage - 1) / kKvPage;
+                  int groups, long cols, long max_len, int splits, int first_state) {
+    const long pages = (max_len + kKvPage - 1) / kKvPage;
     p.cu_rows = cu; p.lens = lens; p.tables = tables;
-    p.len_add = len_add; p.max_len = max_len; p.max_pages = max_pages; p.groups = groups;
+    p.len_add = len_add; p.max_len = (int)max_len; p.max_pages = max_pages; p.groups = groups;
     p.wide = cols > kNarrowCols;
     p.solo = !p.wide && solo_of((long)groups * t.n_kv_heads, max_len);
     p.blocks_x = p.solo ? (t.n_kv_heads + kTileWaves - 1) / kTileWaves : t.n_kv_heads * blocks_of(cols);
-    p.pages_per_split = (pages + splits - 1) / splits;
+    p.pages_per_split = (int)((pages + splits - 1) / splits);
     p.first_state = first_state;
     blocks += (long)p.blocks_x * groups * splits;
   };
-  if (t.plan.prefix > 0) {
+  const bool joined = t.plan.joined;
+  if (joined) {
+    TilePart& p = a.part[0];
+    p.cu_rows = t.cu_groups; p.lens = t.prefix_lens; p.tables = t.prefix_tables;
+    p.max_len = t.max_prefix; p.max_pages = t.max_prefix_pages; p.groups = t.n_groups;
+  } else if (t.plan.prefix > 0) {
     part(a.part[0], t.cu_groups, t.prefix_lens, t.prefix_tables, 0, t.max_prefix_pages, t.n_groups, (long)t.max_rows * G,
          t.max_prefix, t.plan.prefix, 0);
     a.first_blocks = (int)std::min(blocks, 0x7fffffffL);
   }
-  part(a.part[1], nullptr, t.kv_lens, t.block_tables, t.kv_len_add, t.max_blocks, t.B, G, t.max_kv_len, t.plan.own,
-       t.plan.prefix);
+  part(a.part[1], nullptr, t.kv_lens, t.block_tables, t.kv_len_add, t.max_blocks, t.B, G,
+       joined ? (long)t.max_kv_len + t.max_prefix : t.max_kv_len, joined ? 1 : t.plan.own, joined ? 0 : t.plan.prefix);
+  a.part[1].max_len = t.max_kv_len;
   a.part[1].rank = g_tile_rank && t.B > 1;
   if (blocks > 0x7fffffffL / kTileThreads) return hipErrorInvalidValue;
   const bool wide = a.part[0].wide || a.part[1].wide;
-  // more than the last-level cache (256 MB) could keep until the next step
-  const double bytes = (double)t.B * t.max_kv_len * t.n_kv_heads * HD * (T == kKvBf16 ? 4 : 2);
-  const bool once = bytes > 256e6;
+  const bool once = (double)t.B * t.max_kv_len * t.n_kv_heads * HD * (T == kKvBf16 ? 4 : 2) > kOnceBytes;
   const dim3 grid((unsigned)blocks), threads(kTileThreads);
-  if (T == kKvBf16 || wide) {
-    if (once) hipLaunchKernelGGL((tile_attention_kernel<HD, T, true, true>), grid, threads, 0, stream, a);
-    else hipLaunchKernelGGL((tile_attention_kernel<HD, T, true, false>), grid, threads, 0, stream, a);
+  if (joined) {
+    hipLaunchKernelGGL((tile_attention_kernel<HD, T, false, false, true>), grid, threads, 0, stream, a);
+  } else if (T == kKvBf16 || wide) {
+    if (once) hipLaunchKernelGGL((tile_attention_kernel<HD, T, true, true, false>), grid, threads, 0, stream, a);
+    else hipLaunchKernelGGL((tile_attention_kernel<HD, T, true, false, false>), grid, threads, 0, stream, a);
   } else if constexpr (T != kKvBf16) {
-    if (once) hipLaunchKernelGGL((tile_attention_kernel<HD, T, false, true>), grid, threads, 0, stream, a);
-    else hipLaunchKernelGGL((tile_attention_kernel<HD, T, false, false>), grid, threads, 0, stream, a);
+    if (once) hipLaunchKernelGGL((tile_attention_kernel<HD, T, false, true, false>), grid, threads, 0, stream, a);
+    else hipLaunchKernelGGL((tile_attention_kernel<HD, T, false, false, false>), grid, threads, 0, stream, a);
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.n_states == 1) return e;

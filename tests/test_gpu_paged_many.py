@@ -10,7 +10,7 @@ from paper_2401_09670_amd import binding, synth
 from tests import gpu_util as gu
 from tests.kv_pages import KINDS, Cache, rows
 from tests.test_gpu_kv_quant import _expect, _poisoned, _same
-from tests.test_gpu_paged_attention import _attend, _check, _check_shared, _ctx, _groups, _shared
+from tests.test_gpu_paged_attention import GROUPS, SHAPES, _attend, _check, _check_shared, _ctx, _groups, _shared
 from tests.test_gpu_quant_steps import _bounds, _pages
 
 pytestmark = pytest.mark.gpu
@@ -49,15 +49,47 @@ def test_a_head_for_each_wave(gpu, n, n_kv, s, most, B, kind):
     _check(_attend(_ctx(n, n_kv, s), q, c), q, c, n, s)
 
 
+@pytest.mark.parametrize("slack", [0, 1000])       # short ones: each row reads its prefix; bounds of long ones: two parts
 @pytest.mark.parametrize("kind", ["bf16", "e4m3"])
-def test_many_rows_behind_many_prefixes(gpu, kind):
+def test_many_rows_behind_many_prefixes(gpu, kind, slack):
     n, n_kv, s, g = 4, 2, 64, 70
     rng = np.random.default_rng(4)
     rows_of = [int(r) for r in rng.integers(0, 4, g)]
     prefix, own = [int(p) for p in rng.integers(0, 90, g)], [int(l) for l in rng.integers(0, 50, sum(rows_of))]
     c, cu = _groups(rows_of, prefix, own, n_kv, s, kind, 3)
     q = gu.to_dev(rows(rng, len(own), n, s))
-    _check_shared(_shared(_ctx(n, n_kv, s), q, c, cu, prefix, own), q, c, cu, s)
+    _check_shared(_shared(_ctx(n, n_kv, s), q, c, cu, prefix, own, slack=slack), q, c, cu, s)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3", "int8"])
+@pytest.mark.parametrize("n,n_kv,s", SHAPES)
+def test_short_prefixes_within_bounds_of_long_ones(gpu, n, n_kv, s, kind):
+    """The prefixes as a part of their own, most of its splits without any page."""
+    ctx = _ctx(n, n_kv, s)
+    for seed, (rows_of, prefix, own) in enumerate(GROUPS):
+        c, cu = _groups(rows_of, prefix, own, n_kv, s, kind, seed)
+        q = gu.to_dev(rows(np.random.default_rng(seed), len(own), n, s))
+        o = _shared(ctx, q, c, cu, prefix, own, slack=1000)
+        _check_shared(o, q, c, cu, s)
+        assert torch.equal(o, _shared(ctx, q, c, cu, prefix, own, slack=1000))
+
+
+@pytest.mark.parametrize("slack", [0, 1000])
+@pytest.mark.parametrize("kind", ["bf16", "e4m3", "int8"])
+@pytest.mark.parametrize("where", ["prefix", "own"])
+def test_nan_goes_where_it_is_seen(gpu, kind, where, slack):
+    n, s = 4, 64
+    rng = np.random.default_rng(3)
+    prefix, own = [90, 33], [10, 20, 30]
+    t = sum(prefix) + sum(own)
+    kb, vb = rows(rng, t, n, s), rows(rng, t, n, s)
+    kb[89 if where == "prefix" else sum(prefix) + 10 + 19, 2, 7] = 0x7fc0
+    c = Cache(kind, prefix + own, n, s, 5, k_bits=kb, v_bits=vb)
+    q = gu.to_dev(rows(rng, 3, n, s))
+    o = gu.to_f64(_shared(_ctx(n, n, s), q, c, np.array([0, 2, 3]), prefix, own, slack=slack))
+    nan = np.zeros(o.shape, bool)
+    nan[0 if where == "prefix" else 1:2, 2] = True
+    np.testing.assert_array_equal(np.isnan(o), nan)
 
 
 @pytest.mark.parametrize("B,bound,lens", [(2, 100, [130, 40]), (1, 1000, [1100]), (3, 17, [500, 16, 18])])
