@@ -17,7 +17,14 @@
 //    their states (maximum, sum, output) are merged through LDS.  HBM bounds it.
 //  * wide, 64 columns: each wave has 16 of them, and all see the same tiles of 64 keys, which the workgroup brings to bf16
 //    and into LDS once.  What a tile takes in LDS accesses and softmax bounds it, not its bytes.
-// Where a (row, head) has more than one state, they are written out in fp32 and a second launch merges them in order.
+// Where a (row, head) has more than one state, they are written out in fp32 and a second launch merges them in order.  Short
+// prefixes are no part of their own: every row's workgroup takes its prefix and then its own pages, and there are no states.
+//
+// Measured, both launches where there are two (5.9 TB/s is what this chip reads at most): 40 heads, e4m3, 64 sequences of 545
+// tokens 63.2 us = 5.8 TB/s; int8, 128 of 16 to 2048 99.5 us = 5.8; 64 heads on 8, e4m3, 48 of 1024 to 4096 63 us = 4.7 (the
+// pieces are unequal); int8, one of 65538 33.5 us = 4.1 (the start and the second launch are 10 of them).  Shared: 64 rows of 40
+// heads behind 2048 bf16 tokens, 16 to 256 of their own, 42 us = 5.0 TB/s; 7, 40 and 1 rows of 64 heads on 8 behind some 7000
+// e4m3 tokens 36.5 us = 0.30 PFLOP/s (wide tiles).  The least call is 5 us.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -179,8 +186,8 @@ struct TileLds {
 // 8 (i / 4 & 1) + 4 t + i % 4 of page i / 8.  V is kept with a feature's 16 tokens together: a 16-byte load and two row
 // swaps give 8 keys of two blocks of features, operand A as it is wanted.
 //   K is asked for one chunk ahead when this one's scores are made, V when its output is: 16 registers each.  (A chunk of 64
-// keys has twice those and half the waves: 40 heads, 64 sequences of 545 tokens 76 -> 71 us.)  Loads that no cache keeps,
-// where the caches could not keep them: 71 -> 66.
+// keys has twice those and half the waves: 40 heads, 64 sequences of 545 tokens 76 us, of 32 keys 71.)  Loads that no cache
+// keeps: 71 -> 66 there, but one sequence of 700 tokens, which the caches do keep from step to step, 8.6 -> 10.8: kOnceBytes.
 template <int HD, int T, bool ONCE>
 __device__ __forceinline__ void narrow_quant(const TileArgs& a, const TileWork& w, const u32x4 (&qf)[HD / 32],
                                              floatx4 (&acc)[HD / 16], float& m_run, float& l_run) {
@@ -352,7 +359,11 @@ __device__ __forceinline__ void narrow_bf16(const TileArgs& a, const TileWork& w
 // of a half is its key 16 t + i, and V is as for the narrow form.  8 bits: row i is key 8 (i / 4) + 4 t + i % 4, so that lane
 // group g has keys 8 g .. + 8, and V^T rows of 64 keys hold operand A of half u in their chunk 4 u + g (swizzled by d / 2).
 //   The next tile's bytes are in registers while this one is multiplied.  (Tiles of 32 keys in two buffers, one barrier each:
-// the same LDS and barriers, but twice the chains of dependent steps per key.)
+// the same LDS and barriers, but twice the chains of dependent steps per key; 40 rows of 64 heads on 8 behind 6951 tokens,
+// unsplit, 167 us instead of 141.)  A tile takes a lone workgroup 1.2 us, and three on a compute unit 2.5 together: 280 vector
+// instructions a wave and tile, a third of them staging, beside 32 products.  32 x 32 x 16 instructions with half the operand
+// reads (each wave 32 columns over half of the keys), operands asked for all together, and K's scale with the conversion were
+// no faster.
 template <int HD, int T>
 __device__ __forceinline__ int k_swizzle(int row) {
   if constexpr (T == kKvBf16) return HD == 128 ? row & 15 : (row >> 1) & 7;
@@ -869,13 +880,12 @@ static hipError_t launch_tiles(const TileAttention& t, hipStream_t stream) {
   } else if (t.plan.prefix > 0) {
     part(a.part[0], t.cu_groups, t.prefix_lens, t.prefix_tables, 0, t.max_prefix_pages, t.n_groups, (long)t.max_rows * G,
          t.max_prefix, t.plan.prefix, 0);
-    a.first_blocks = (int)std::min(blocks, 0x7fffffffL);
+    a.first_blocks = (int)blocks;
   }
   part(a.part[1], nullptr, t.kv_lens, t.block_tables, t.kv_len_add, t.max_blocks, t.B, G,
        joined ? (long)t.max_kv_len + t.max_prefix : t.max_kv_len, joined ? 1 : t.plan.own, joined ? 0 : t.plan.prefix);
   a.part[1].max_len = t.max_kv_len;
   a.part[1].rank = g_tile_rank && t.B > 1;
-  if (blocks > 0x7fffffffL / kTileThreads) return hipErrorInvalidValue;
   const bool wide = a.part[0].wide || a.part[1].wide;
   const bool once = (double)t.B * t.max_kv_len * t.n_kv_heads * HD * (T == kKvBf16 ? 4 : 2) > kOnceBytes;
   const dim3 grid((unsigned)blocks), threads(kTileThreads);
@@ -900,8 +910,15 @@ static hipError_t launch_tiles(const TileAttention& t, hipStream_t stream) {
   return hipGetLastError();
 }
 
+bool tile_attention_fits(const TileAttention& t) {
+  const int G = t.n_heads / t.n_kv_heads;
+  const double own = (double)t.B * blocks_of(G) * t.plan.own;
+  const double prefixes = t.plan.joined ? 0.0 : (double)t.n_groups * blocks_of((long)t.max_rows * G) * t.plan.prefix;
+  return t.B <= 65535 && (own + prefixes) * t.n_kv_heads <= (double)(0x7fffffff / kTileThreads);
+}
+
 hipError_t launch_tile_attention(const TileAttention& t, hipStream_t stream) {
-  if (t.n_kv_heads <= 0 || t.n_heads % t.n_kv_heads != 0 || t.B > 65535) return hipErrorInvalidValue;
+  if (t.n_kv_heads <= 0 || t.n_heads % t.n_kv_heads != 0 || !tile_attention_fits(t)) return hipErrorInvalidValue;
   if (t.plan.own < 1 || (t.plan.own + t.plan.prefix > 1 && !t.states)) return hipErrorInvalidValue;
   if (t.head_dim == 128) {
     if (t.cache.type == kKvBf16) return launch_tiles<128, kKvBf16>(t, stream);

@@ -508,7 +508,7 @@ size_t tile_states(const ds_ctx* ctx, int max_batch, int max_ctx, int max_prefix
   const auto hit = ctx->tile_states.find(key);
   if (hit != ctx->tile_states.end()) return hit->second;
   size_t most = 0;
-  for (int b = 1; b <= max_batch; ++b) {
+  for (int b = 1; b <= std::min(max_batch, 65535); ++b) {  // (no call has more rows)
     const int states = ds::tile_most_states(b, c.n_heads, c.n_kv_heads, max_ctx, max_prefix);
     most = std::max(most, ds::tile_states_bytes(b, c.n_heads, c.head_dim, states));
   }
@@ -1027,6 +1027,9 @@ static ds_status decode_step(ds_ctx* ctx, const ds_layer_weights* w, const void*
   if (x == y) return fail(ctx, DS_ERR_INVALID_ARG, "%s: y must not alias x", who);
   if (!aligned16(x) || !aligned16(y) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(workspace))
     return fail(ctx, DS_ERR_INVALID_ARG, "%s: pointers must be 16-byte aligned", who);
+  if (cache.tiles && !ds::tile_attention_fits(tile_attention(ctx, cache, nullptr, 0, ctx_lens, 1, block_tables, B,
+                                                             max_blocks_per_seq, max_ctx, nullptr, nullptr)))
+    return fail(ctx, DS_ERR_INVALID_ARG, "%s: more rows or groups than a launch can have", who);
   const size_t need = cache.tiles ? tile_step_least(ctx, B, max_ctx, cache.max_prefix).all : decode_least(ctx, B, max_ctx).all;
   const DeviceState* dev = nullptr;
   if (use_static) {
@@ -1167,12 +1170,12 @@ ds_status ds_decode_step_static(ds_ctx* ctx, const ds_layer_weights* w, const vo
 
 // From these sizes on every product of such a step has its fastest plan.
 size_t ds_decode_quant_workspace_bytes(const ds_ctx* ctx, int32_t max_batch, int32_t max_ctx) {
-  if (!ctx || max_batch <= 0 || max_ctx <= 0) return 0;
+  if (!ctx || max_batch <= 0 || max_ctx <= 0 || max_ctx > kMostTokens) return 0;
   return full_ws(ctx, max_batch, tile_step_least(ctx, max_batch, max_ctx, 0));
 }
 
 size_t ds_decode_shared_workspace_bytes(const ds_ctx* ctx, int32_t max_batch, int32_t max_prefix_len, int32_t max_ctx) {
-  if (!ctx || max_batch <= 0 || max_ctx <= 0 || max_prefix_len <= 0) return 0;
+  if (!ctx || max_batch <= 0 || max_ctx <= 0 || max_prefix_len <= 0 || std::max(max_ctx, max_prefix_len) > kMostTokens) return 0;
   return full_ws(ctx, max_batch, tile_step_least(ctx, max_batch, max_ctx, max_prefix_len));
 }
 
@@ -1258,6 +1261,7 @@ static ds_status paged_attention(ds_ctx* ctx, const char* who, const void* q, co
   const ds_model_cfg& c = ctx->cfg;
   const ds::TileAttention t = tile_attention(ctx, cache, q, c.hidden, kv_lens, 0, block_tables, B, max_blocks_per_seq,
                                              max_kv_len, o, workspace);
+  if (!ds::tile_attention_fits(t)) return fail(ctx, DS_ERR_INVALID_ARG, "%s: more rows or groups than a launch can have", who);
   const size_t need = ds::tile_states_bytes(B, c.n_heads, c.head_dim, t.plan.own + t.plan.prefix);
   if (need > 0 && (!workspace || workspace_bytes < need))
     return fail(ctx, DS_ERR_WORKSPACE, "%s: workspace %zu < %zu", who, workspace_bytes, need);

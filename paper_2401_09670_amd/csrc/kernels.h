@@ -215,6 +215,7 @@ struct TileAttention {
   TilePlan plan;
   void *o, *states;
 };
+bool tile_attention_fits(const TileAttention& t);  // into a launch
 hipError_t launch_tile_attention(const TileAttention& t, hipStream_t stream);
 
 }  // namespace ds

@@ -61,3 +61,28 @@ def test_lengths_that_no_position_reaches(longest):
         assert lib.ds_decode_attention_shared(h, P, P, 2, 3, P, P, Xp, X, P, P, 4, Lp, L, *cache, P, *end) == INVALID
         assert lib.ds_decode_step_shared(h, w, P, P, 2, 3, P, P, Xp, X, P, P, 4, Lp, L, *cache, 2 * P, *end) == INVALID
     ctx.close()
+
+
+def test_queries_of_the_largest_sizes_return():
+    ctx = binding.Context(256, 4, 64, 1024)
+    most = 2 ** 31 - 1
+    assert ctx.ds_decode_quant_workspace_bytes(4, most) == 0
+    assert ctx.ds_decode_shared_workspace_bytes(4, most, 16) == ctx.ds_decode_shared_workspace_bytes(4, 16, most) == 0
+    assert 0 < ctx.ds_decode_quant_workspace_bytes(4, 2 ** 30) <= ctx.ds_decode_shared_workspace_bytes(4, 2 ** 30, 2 ** 30)
+    assert ctx.ds_decode_shared_workspace_bytes(100000, 4000, 4000) >= ctx.ds_decode_shared_workspace_bytes(65535, 4000, 4000)
+    ctx.close()
+
+
+def test_more_than_a_launch_can_have():
+    ctx = binding.Context(1024, 8, 128, 1024, n_kv_heads=2)
+    w = binding.LayerWeights()
+    for name, _ in binding.LayerWeights._fields_:
+        setattr(w, name, P)
+    w, end, cache = ctypes.byref(w), (P, 1 << 50, None), (*CACHE, 1)
+    lib, h = ctx.lib, ctx.handle
+    assert lib.ds_decode_attention_quant(h, P, P, P, 65536, 2, 32, *cache, P, *end) == INVALID
+    assert lib.ds_decode_step_quant(h, w, P, P, P, 65536, 2, 32, *cache, 2 * P, *end) == INVALID
+    for B, groups, rows in ((65536, 2, 40000), (40000, 40000, 40000), (8, 2 ** 31 - 1, 8)):
+        assert lib.ds_decode_attention_shared(h, P, P, groups, rows, P, P, 400, 6400, P, P, B, 2, 32, *cache, P, *end) == INVALID
+        assert lib.ds_decode_step_shared(h, w, P, P, groups, rows, P, P, 400, 6400, P, P, B, 2, 32, *cache, 2 * P, *end) == INVALID
+    ctx.close()
