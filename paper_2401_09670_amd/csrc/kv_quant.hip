@@ -1,7 +1,7 @@
 // The paged cache of 8 bits as it is written (hand-off, append) and read back.  Formats and layout: kv_quant.h.
 // All three move bytes: what has to be read and written bounds them.  12 ragged prompts of 40 heads, 5197 tokens, int8: 160 MB
-// written off in 30 us (5.4 TB/s) and read back in 36 (4.4); 8 of 2048, 96 heads, e4m3: 1.2 GB in 230 and 226 us (5.3; a large
-// copy reaches 5.15 here).
+// written off in 30 us (5.4 TB/s) and read back in 26 (6.2); 8 of 2048, 96 heads, e4m3: 1.2 GB in 231 and 209 us (5.3 and 5.8; a
+// large copy reaches 5.15 here).
 #include <type_traits>
 
 #include "kv_quant.h"
@@ -52,8 +52,8 @@ __device__ __forceinline__ uint32_t row_amax(const uint32_t (&w)[N]) {
 
 // A wave takes one page of one head of K or of V; a workgroup 4 heads, and those of a page follow each other.
 //   Sequence i has the places cu[i] / 16 + i and on, as many as it has pages or more, and there are t / 16 + B of them in all:
-// next to none is for nothing, however unlike the lengths are.  (A grid of the longest sequence's pages times sequences: 12
-// ragged prompts of 40 heads, 5197 tokens, 39 us written and 43 read back instead of 30 and 36.)
+// next to none is for nothing, however unlike the lengths are.  (A grid of the longest sequence's pages times sequences took 8 us
+// more either way for the 12 prompts.)
 struct PagePlace {
   int seq, page, head, ntok;
   size_t row0;  // of the page's first token
@@ -145,7 +145,9 @@ __global__ __launch_bounds__(kQuantThreads) void kv_migrate_quant_kernel(
   }
 }
 
-// The reverse: pages -> rows, each value times its scale, rounded to bf16.
+// The reverse: pages -> rows, each value times its scale, rounded to bf16.  The rows are stored past the caches: a head's piece of
+// a row is 128 or 256 bytes and its neighbours come from other waves (the 12 prompts 37.5 -> 26.0 us).  Pages loaded or
+// written (above) that way are not faster: 34.2 with the loads alone, the hand-off 29.8 -> 32.9.
 template <int HD, int T>
 __global__ __launch_bounds__(kQuantThreads) void kv_read_quant_kernel(
     const int32_t* __restrict__ cu_seqlens, int B, int max_seqlen, const int32_t* __restrict__ block_tables, int max_blocks,
@@ -213,8 +215,9 @@ __global__ __launch_bounds__(kQuantThreads) void kv_read_quant_kernel(
       }
     }
     if (4 * g + i < p.ntok) {
-      if constexpr (W == 2) st16(dst + (size_t)(4 * g + i) * h, u32x4{w[0], w[1], w[2], w[3]});
-      else *reinterpret_cast<u32x2*>(dst + (size_t)(4 * g + i) * h) = u32x2{w[0], w[1]};
+      if constexpr (W == 2)
+        __builtin_nontemporal_store(u32x4{w[0], w[1], w[2], w[3]}, reinterpret_cast<u32x4*>(dst + (size_t)(4 * g + i) * h));
+      else __builtin_nontemporal_store(u32x2{w[0], w[1]}, reinterpret_cast<u32x2*>(dst + (size_t)(4 * g + i) * h));
     }
   }
 }
@@ -256,11 +259,14 @@ __global__ __launch_bounds__(kQuantThreads) void kv_append_quant_kernel(
     return;
   }
   // V: a byte in each of the page's 16-byte pieces.  The pieces are read, changed and written whole: written byte by byte,
-  // each of the page's lines is half-masked on its way to memory (40 heads, 64 sequences 6.9 -> 5.3 us, 128 10.3 -> 7.1).
+  // each of the page's lines is half-masked on its way to memory (40 heads, 64 sequences 6.9 -> 5.3 us, 128 10.3 -> 7.1).  They
+  // go past the caches both ways: lines left changed in an L2 are what the next launch waits for (with the attention behind
+  // it, 64 sequences 75.8 -> 70.3 us, 128 117.3 -> 108.3; the stores alone past them 75.9 and 117.6, the loads alone 71.8 and
+  // 116.4).
   uint8_t* vp = v_cache + page * (HD * kKvPage) + c * kKvPage;
   u32x4 piece[E];  // of feature 16 i + c
 #pragma unroll
-  for (int i = 0; i < E; ++i) piece[i] = ld16(vp + i * 16 * kKvPage);
+  for (int i = 0; i < E; ++i) piece[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(vp + i * 16 * kKvPage));
   uint8_t* row = rows[threadIdx.x >> 4];
 #pragma unroll
   for (int j = 0; j < W; ++j) *reinterpret_cast<uint32_t*>(row + E * c + 4 * j) = quantise4<T>(w[2 * j], w[2 * j + 1], sc, inv);
@@ -274,7 +280,7 @@ __global__ __launch_bounds__(kQuantThreads) void kv_append_quant_kernel(
 #pragma unroll
     for (int q = 0; q < 4; ++q)
       if (q == slot >> 2) piece[i][q] = (piece[i][q] & ~(0xffu << shift)) | v;
-    st16(vp + i * 16 * kKvPage, piece[i]);
+    __builtin_nontemporal_store(piece[i], reinterpret_cast<u32x4*>(vp + i * 16 * kKvPage));
   }
 }
 
