@@ -123,3 +123,60 @@ def test_two_rows_into_one_page_are_named(gpu):
             call(gu.i32_dev([16, 5, 15]))       # (page 1 of the first row alone)
             call(gu.i32_dev([-1, 5, 16]))
             _bounds(lambda: call(gu.i32_dev([17, 5, 30])), "rows 0 and 2 both write into block 1")
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+def test_prefixes_behind_4_gib(gpu, kind):
+    """Pages whose bytes lie behind 32 bits' reach, under wide tiles, under narrow ones and where every row reads its prefix."""
+    n, s, prefix, own = 40, 128, [50, 37], [int(l) for l in np.random.default_rng(2).integers(0, 40, 22)]
+    c, cu = _groups([20, 2], prefix, own, n, s, kind, 11)
+    nb = 2 ** 32 // (n * 16 * s * (2 if kind == "bf16" else 1)) + c.nb + 5
+    far = torch.arange(nb - c.nb, nb, device="cuda")
+    for name in ("k", "v", "ks", "vs"):
+        t = getattr(c, name)
+        if t is not None:
+            big = torch.empty((nb, *t.shape[1:]), dtype=t.dtype, device="cuda")
+            big[far] = t
+            setattr(c, name, big)
+    c.table, c.nb = np.where(c.table >= 0, c.table + (nb - c.nb), -1).astype(np.int32), nb
+    q = gu.to_dev(rows(np.random.default_rng(3), 22, n, s))
+    for slack in (0, 1000):
+        _check_shared(_shared(_ctx(n, n, s), q, c, cu, prefix, own, slack=slack), q, c, cu, s)
+
+
+def test_states_in_a_graph(gpu):
+    """Two captured graphs of calls that split, on one workspace, replayed in turn after the queries changed."""
+    n, n_kv, s = 16, 2, 128
+    ctx, rng = _ctx(n, n_kv, s), np.random.default_rng(0)
+    prefix, own = [1500], [900, 20, 33]
+    c, cu = _groups([3], prefix, own, n_kv, s, "e4m3", 2)
+    q = gu.to_dev(rows(rng, 3, n, s))
+    cud, pl, pt, bt, ol = gu.i32_dev(cu), gu.i32_dev(prefix), gu.i32_dev(c.table[:1]), gu.i32_dev(c.table[1:]), gu.i32_dev(own)
+    mb = c.table.shape[1]
+    ws = gu.workspace(ctx.ds_decode_shared_workspace_bytes(3, 1500, 900))
+
+    def shared(o):
+        ctx.ds_decode_attention_shared(q, cud, 1, 3, pl, pt, mb, 1500, ol, bt, 3, mb, 900, *c.args, o, ws)
+
+    def alone(o):
+        ctx.ds_decode_attention_quant(q, ol, bt, 3, mb, 900, *c.args, o, ws)
+
+    outs, graphs = [torch.empty_like(q), torch.empty_like(q)], []
+    for call, o in zip((shared, alone), outs):
+        call(torch.empty_like(q))
+        torch.cuda.synchronize()
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            call(o)
+    for i in range(3):
+        q.copy_(gu.to_dev(rows(rng, 3, n, s)))
+        ws.fill_(255)
+        for g in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        for call, o in zip((shared, alone), outs):
+            eager = torch.empty_like(q)
+            call(eager)
+            torch.cuda.synchronize()
+            assert torch.equal(o, eager), i
+    _check_shared(outs[0], q, c, cu, s)
