@@ -8,6 +8,7 @@
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
+#include <exception>
 #include <map>
 #include <mutex>
 #include <new>
@@ -378,7 +379,11 @@ ds_status ensure_device(ds_ctx* ctx, const DeviceState** out = nullptr) {
 
 // ---- debug validation of device index arrays (ctx->validate) ----
 ds_status fetch_i32(ds_ctx* ctx, const int32_t* dev, size_t n, hipStream_t s, std::vector<int32_t>& out) {
-  out.resize(n);
+  try {
+    out.resize(n);
+  } catch (const std::exception&) {
+    return fail(ctx, DS_ERR_INVALID_ARG, "validation: no memory for %zu entries", n);
+  }
   hipError_t e = hipMemcpyAsync(out.data(), dev, n * sizeof(int32_t), hipMemcpyDeviceToHost, s);
   if (e == hipSuccess) e = hipStreamSynchronize(s);
   if (e != hipSuccess) return fail(ctx, DS_ERR_HIP, "validation copy failed: %s", hipGetErrorString(e));
@@ -443,13 +448,17 @@ ds_status validate_new_pages(ds_ctx* ctx, const char* who, const int32_t* bt_dev
   std::vector<int32_t> bt;
   ds_status st = fetch_i32(ctx, bt_dev, (size_t)B * max_blocks, s, bt);
   if (st != DS_OK) return st;
-  std::unordered_map<int32_t, int> writer;
-  for (int i = 0; i < B; ++i) {
-    if (tokens[i] <= 0) continue;
-    const int32_t id = bt[(size_t)i * max_blocks + (tokens[i] - 1) / ctx->cfg.block_size];
-    const auto first = writer.emplace(id, i);
-    if (!first.second)
-      return fail(ctx, DS_ERR_BOUNDS, "%s: rows %d and %d both write into block %d", who, first.first->second, i, id);
+  try {
+    std::unordered_map<int32_t, int> writer;
+    for (int i = 0; i < B; ++i) {
+      if (tokens[i] <= 0) continue;
+      const int32_t id = bt[(size_t)i * max_blocks + (tokens[i] - 1) / ctx->cfg.block_size];
+      const auto first = writer.emplace(id, i);
+      if (!first.second)
+        return fail(ctx, DS_ERR_BOUNDS, "%s: rows %d and %d both write into block %d", who, first.first->second, i, id);
+    }
+  } catch (const std::exception&) {
+    return fail(ctx, DS_ERR_INVALID_ARG, "%s: no memory for the pages of %d rows", who, B);
   }
   return DS_OK;
 }
@@ -513,7 +522,10 @@ size_t tile_states(const ds_ctx* ctx, int max_batch, int max_ctx, int max_prefix
     most = std::max(most, ds::tile_states_bytes(b, c.n_heads, c.head_dim, states));
   }
   most = align_up(most, 256);
-  if (ctx->tile_states.size() < 4096) ctx->tile_states[key] = most;
+  try {
+    if (ctx->tile_states.size() < 4096) ctx->tile_states[key] = most;
+  } catch (const std::exception&) {  // (not kept then)
+  }
   return most;
 }
 
@@ -941,10 +953,10 @@ static ds_status check_rows(ds_ctx* ctx, const char* who, const void* k_rows, co
 static ds_status validate_rows(ds_ctx* ctx, const char* who, const int32_t* cu_seqlens, int32_t B, int32_t t,
                                int32_t max_seqlen, const int32_t* block_tables, int32_t max_blocks, int32_t num_blocks,
                                hipStream_t s) {
-  std::vector<int32_t> cu, lens((size_t)B);
+  std::vector<int32_t> cu;
   if (ds_status st = validate_cu(ctx, who, cu_seqlens, B, t, max_seqlen, s, cu)) return st;
-  for (int i = 0; i < B; ++i) lens[i] = cu[i + 1] - cu[i];
-  return validate_tables(ctx, who, block_tables, B, max_blocks, num_blocks, lens, s);
+  for (int i = 0; i < B; ++i) cu[i] = cu[i + 1] - cu[i];  // the lengths
+  return validate_tables(ctx, who, block_tables, B, max_blocks, num_blocks, cu, s);
 }
 
 // The groups of rows that share a prefix.
