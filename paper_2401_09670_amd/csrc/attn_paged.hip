@@ -43,7 +43,7 @@ struct TilePart {
   const int32_t* tables;
   int len_add, max_len, max_pages, groups;
   int blocks_x;            // key/value heads x blocks of columns
-  int pages_per_split;
+  int splits, pages_per_split;  // (0: up to so many pieces, by how unequal the sequences are)
   int first_state;         // states of this part's splits
   int wide;                // 64 columns a workgroup
   int solo;                // narrow: a key/value head for each wave
@@ -61,9 +61,10 @@ struct TileArgs {
   int n_states;      // of a (row, head); 1: o is written
   float scale_log2e;
   uint16_t* o;
-  float* partial;    // [row][head][state][output[HD], max, sum, -, -]
+  float* partial;    // [row][head][state][output[HD], max, sum, states of the own pages (in the first of them), -]
 };
 constexpr int kStatePad = 4;
+constexpr int kLeastPiece = 32;  // pages
 
 // v of lane 16 (lane / 16) + J
 template <int J>
@@ -94,6 +95,8 @@ __device__ __forceinline__ int lane_anew() {
 // One workgroup's share: a group's pages [lo, hi) of a key/value head, for some of the group's columns.
 struct TileWork {
   int kv, row0, c0, cols, state, len, lo, hi;
+  int pieces;  // in the first of those that were cut by what there is; else 0
+  bool whole;  // there is nothing else of the row and head: the result is written, no state
   int step;  // narrow: pages from one chunk of a wave to its next
   const int32_t* bt;
 };
@@ -528,14 +531,15 @@ __device__ __forceinline__ void store_columns(const TileArgs& a, const TileWork&
   if (col >= w.cols) return;
   const int g = lane_anew() >> 4, G = a.n_heads / a.n_kv_heads;
   const size_t item = (size_t)(w.row0 + col / G) * a.n_heads + w.kv * G + col % G;
-  if (a.n_states == 1) {
+  float* st = a.partial + (item * a.n_states + w.state) * (HD + kStatePad);
+  if (w.pieces > 0 && g == 0) reinterpret_cast<int*>(st)[HD + 2] = w.pieces;
+  if (w.whole) {
     const float inv = l == 0.f ? 0.f : 1.f / l;  // no key at all: 0
 #pragma unroll
     for (int db = 0; db < HD / 16; ++db)
       *reinterpret_cast<u32x2*>(a.o + item * HD + 16 * db + 4 * g) =
           u32x2{pack_bf16(acc[db][0] * inv, acc[db][1] * inv), pack_bf16(acc[db][2] * inv, acc[db][3] * inv)};
   } else {
-    float* st = a.partial + (item * a.n_states + w.state) * (HD + kStatePad);
 #pragma unroll
     for (int db = 0; db < HD / 16; ++db) *reinterpret_cast<floatx4*>(st + 16 * db + 4 * g) = acc[db];
     if (g == 0) {
@@ -560,7 +564,8 @@ __global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(WI
   const bool wide = WIDE && p.wide;
   const int G = a.n_heads / a.n_kv_heads;
 
-  // workgroup -> key/value head (fastest), block of columns, group, split
+  // workgroup -> key/value head (fastest), block of columns, group, split.  (With the splits of a sequence next to each other
+  // those without pages come in between, and what has some is dealt to the same few compute units: three times as long.)
   int id = (int)blockIdx.x - (second ? a.first_blocks : 0);
   const int x = id % p.blocks_x;
   id /= p.blocks_x;
@@ -586,8 +591,29 @@ __global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(WI
   w.row0 = p.cu_rows ? p.cu_rows[group] : group;
   w.cols = (p.cu_rows ? p.cu_rows[group + 1] - w.row0 : 1) * G;
   if (w.c0 >= w.cols) return;
-  w.lo = split * p.pages_per_split;
-  w.hi = min((w.len + kKvPage - 1) / kKvPage, w.lo + p.pages_per_split);
+  const int pages = (w.len + kKvPage - 1) / kKvPage;
+  int piece = p.pages_per_split;
+  w.pieces = 0;
+  w.whole = a.n_states == 1;
+  if (piece == 0) {
+    // A piece is two thirds of what each compute unit has of all pages: equal sequences stay whole where they are enough
+    // for the chip, and those are cut that would end the launch by themselves.  What is whole needs no state.
+    float all = 0.f;
+    for (int i0 = 0; i0 < p.groups; i0 += 64) {
+      const int i = i0 + lane;
+      if (i < p.groups) all += (float)((max(min(p.lens[i] + p.len_add, p.max_len), 0) + kKvPage - 1) / kKvPage);
+    }
+    const int fair = (int)fminf(wave_sum(all) * (float)p.blocks_x * (1.f / 384.f), 1e9f);
+    const int most = __builtin_amdgcn_readfirstlane(max(fair, kLeastPiece));
+    const int cuts = min((pages + most - 1) / most, p.splits);
+    piece = cuts <= 1 ? max(pages, 1) : ((pages + cuts - 1) / cuts + 7) & ~7;  // (8: a chunk for each wave)
+    const int pieces = max((pages + piece - 1) / piece, 1);
+    if (split >= pieces) return;
+    if (split == 0) w.pieces = pieces;
+    w.whole = pieces == 1 && p.first_state == 0;
+  }
+  w.lo = split * piece;
+  w.hi = min(pages, w.lo + piece);
   w.bt = p.tables + (size_t)group * p.max_pages;
   w.state = p.first_state + split;
   w.step = p.solo ? 2 : 2 * kTileWaves;
@@ -670,7 +696,9 @@ __global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(WI
     for (int j = 0; j < ND; ++j) out[j] += src[d0 + j] * f;
   }
   const size_t to = (size_t)(w.row0 + c / G) * a.n_heads + w.kv * G + c % G;
-  if (a.n_states == 1) {
+  float* st = a.partial + (to * a.n_states + w.state) * kState;
+  if (w.pieces > 0 && (thread & 15) == 0) reinterpret_cast<int*>(st)[HD + 2] = w.pieces;
+  if (w.whole) {
     const float inv = sum == 0.f ? 0.f : 1.f / sum;  // no key at all: 0
     uint32_t v[ND / 2];
 #pragma unroll
@@ -679,7 +707,6 @@ __global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(WI
     if constexpr (ND == 8) st16(op, u32x4{v[0], v[1], v[2], v[3]});
     else *reinterpret_cast<u32x2*>(op) = u32x2{v[0], v[1]};
   } else {
-    float* st = a.partial + (to * a.n_states + w.state) * kState;
 #pragma unroll
     for (int j = 0; j < ND; j += 4) *reinterpret_cast<floatx4*>(st + d0 + j) = floatx4{out[j], out[j + 1], out[j + 2], out[j + 3]};
     if ((thread & 15) == 0) {
@@ -689,18 +716,24 @@ __global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(WI
   }
 }
 
-// The states of a (row, head) as one, in a fixed order: the same bits whenever.  W waves take a (row, head), wave w states w,
+// The states of a (row, head) as one, in a fixed order: the same bits whenever.  counted >= 0: behind that many there are as
+// many as the next one says.  W waves take a (row, head), wave w states w,
 // w + W, ...: its lanes have the maxima and sums of 64 of them at once, and then HD / 64 features each, the states asked for 8
 // at a time.
 template <int HD, int W>
-__global__ __launch_bounds__(kTileThreads) void tile_combine_kernel(const float* __restrict__ partial, int items, int n_states,
-                                                                    uint16_t* __restrict__ o) {
+__global__ __launch_bounds__(kTileThreads) void tile_combine_kernel(const float* __restrict__ partial, int items, int stride,
+                                                                    int counted, uint16_t* __restrict__ o) {
   constexpr int ND = HD / 64, kState = HD + kStatePad, U = 8;
   __shared__ float merge[W == 1 ? 1 : W][HD + 2];
   const int lane = threadIdx.x & 63, in_wg = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = in_wg % W;
   const size_t item = (size_t)blockIdx.x * (kTileWaves / W) + in_wg / W;
   if (item >= (size_t)items) return;  // (W = 1: a wave by itself; else never)
-  const float* src = partial + item * n_states * kState;
+  const float* src = partial + item * stride * kState;
+  int n_states = stride;
+  if (counted >= 0) {  // (one in all: the result is there already)
+    n_states = counted + __builtin_amdgcn_readfirstlane(reinterpret_cast<const int*>(src)[counted * kState + HD + 2]);
+    if (n_states <= 1) return;
+  }
   float m_run = -INFINITY, l_run = 0.f, out[ND] = {};
   for (int s0 = wave; s0 < n_states; s0 += 64 * W) {
     const int n = min((n_states - s0 + W - 1) / W, 64);  // of them in this turn
@@ -786,13 +819,25 @@ static bool solo_of(long items, long max_len) {
 }
 static int blocks_of(long cols) { return (int)(cols <= kNarrowCols ? 1 : (cols + kWideCols - 1) / kWideCols); }
 
-// Splits of up to max_len tokens for `items` workgroups that there are anyway.  Where they are fewer than two per compute
-// unit and the pages 48 or more: enough for three, of 8 pages (a chunk for each wave) or more, of 48 where there are 160
-// workgroups already.  Below that the second launch, which joins them, costs what the splits save.  Of 115 batches of three
-// layer shapes (4 to 1200 items, 500 to 60000 tokens, equal and ragged) these splits are 4 % slower than the best of up to 13
-// numbers each; 8 pages everywhere 6 %.
+// Where there are 512 workgroups or more without a split: cut by how unequal the sequences are, which only the launch can see,
+// if the longest there may be takes a workgroup (0.2 us a page) clearly longer than such a batch takes at a fifth of the bound,
+// and the second launch.  Of 166 batches of 512 to 1088 (lognormal, uniform and equal lengths up to 1024 to 16000 tokens) 2.8 %
+// slower than the best of none and 12 ways to cut for each; none cut 9.8 %.  (us, none cut and cut, 64 rows of 64 heads on 8:
+// lognormal up to 4096 tokens 55 and 32, up to 2048 32 and 26, up to 1024 17.3 and 19.8; uniform up to 4096 64 and 64; all of
+// 4096 88.9 and 91.5.)
+static bool cut_of(long items, long max_len) {
+  const double pages = (double)((max_len + kKvPage - 1) / kKvPage);
+  return items >= 512 && pages * (0.2 - 0.000163 * (double)items) > 12.0;
+}
+
+// Splits of up to max_len tokens for `items` workgroups that there are anyway; with cut_of the most there may be.  Where they are
+// fewer than two per compute unit and the pages 48 or more: enough for three, of 8 pages (a chunk for each wave) or more, of 48
+// where there are 160 workgroups already.  Below that the second launch, which joins them, costs what the splits save.  Of 115
+// batches of three layer shapes (4 to 1200 items, 500 to 60000 tokens, equal and ragged) these splits are 4 % slower than the
+// best of up to 13 numbers each; 8 pages everywhere 6 %.
 static int tile_splits(long items, long max_len) {
   const long pages = (max_len + kKvPage - 1) / kKvPage;
+  if (cut_of(items, max_len)) return (int)std::max(2l, std::min(4096 / items, pages / kLeastPiece));
   if (items >= 512 || pages < 48) return 1;
   return (int)std::max(1l, std::min((768 + items - 1) / items, pages / (items < 160 ? 8 : 48)));
 }
@@ -831,6 +876,7 @@ static bool joined_of(int splits, int B, int n_heads, int n_kv_heads, int head_d
 TilePlan tile_plan(int B, int n_heads, int n_kv_heads, int head_dim, int kv_type, int max_len, int n_groups, int max_prefix) {
   TilePlan p;
   p.own = tile_splits((long)B * n_kv_heads * blocks_of(n_heads / n_kv_heads), max_len);
+  p.cut = cut_of((long)B * n_kv_heads * blocks_of(n_heads / n_kv_heads), max_len);
   const double own_bytes = (double)B * max_len * n_kv_heads * head_dim * (kv_type == kKvBf16 ? 4 : 2);
   if (n_groups > 0) {
     p.prefix = prefix_splits(B, n_heads, n_kv_heads, n_groups, max_prefix, own_bytes);
@@ -868,7 +914,8 @@ static hipError_t launch_tiles(const TileAttention& t, hipStream_t stream) {
     p.wide = cols > kNarrowCols;
     p.solo = !p.wide && solo_of((long)groups * t.n_kv_heads, max_len);
     p.blocks_x = p.solo ? (t.n_kv_heads + kTileWaves - 1) / kTileWaves : t.n_kv_heads * blocks_of(cols);
-    p.pages_per_split = (int)((pages + splits - 1) / splits);
+    p.splits = splits;
+    p.pages_per_split = !cu && t.plan.cut && splits > 1 ? 0 : (int)((pages + splits - 1) / splits);
     p.first_state = first_state;
     blocks += (long)p.blocks_x * groups * splits;
   };
@@ -904,9 +951,10 @@ static hipError_t launch_tiles(const TileAttention& t, hipStream_t stream) {
   const int items = t.B * t.n_heads;
   if (a.n_states <= kTileWaves * 8)
     hipLaunchKernelGGL((tile_combine_kernel<HD, 1>), dim3((items + kTileWaves - 1) / kTileWaves), threads, 0, stream, a.partial,
-                       items, a.n_states, a.o);
+                       items, a.n_states, t.plan.cut ? t.plan.prefix : -1, a.o);
   else
-    hipLaunchKernelGGL((tile_combine_kernel<HD, kTileWaves>), dim3(items), threads, 0, stream, a.partial, items, a.n_states, a.o);
+    hipLaunchKernelGGL((tile_combine_kernel<HD, kTileWaves>), dim3(items), threads, 0, stream, a.partial, items, a.n_states,
+                       t.plan.cut ? t.plan.prefix : -1, a.o);
   return hipGetLastError();
 }
 

@@ -197,6 +197,7 @@ hipError_t launch_kv_append_quant(const void* k_new, const void* v_new, int row_
 // pages, and before them, where n_groups > 0, over the prefix of its group (rows [cu_groups[i], cu_groups[i + 1])).
 struct TilePlan {
   int prefix = 0, own = 1;  // splits of the prefixes' and of the own pages
+  bool cut = false;         // the own pages into at most `own` pieces, by how unequal the sequences are
   bool joined = false;      // every row reads its prefix for itself, and there are no states
 };
 // n_groups = 0: no prefixes.  tile_most_states: no plan of B rows up to these lengths has more states of a row and head.

@@ -180,3 +180,47 @@ def test_states_in_a_graph(gpu):
             torch.cuda.synchronize()
             assert torch.equal(o, eager), i
     _check_shared(outs[0], q, c, cu, s)
+
+
+def _unequal(rng, B, longest):
+    """Most sequences short, a few long ones, one of them a token beyond a whole number of pieces, some without anything."""
+    lens = rng.integers(0, 60, B)
+    at = rng.permutation(B)[:9]
+    lens[at] = [longest, longest - 1, longest // 2, 512, 513, 1025, 529, 0, 1]
+    return [int(l) for l in lens]
+
+
+@pytest.mark.parametrize("kind", ["e4m3", "int8"])
+@pytest.mark.parametrize("n,n_kv,s,B,longest", [(8, 8, 64, 70, 1900), (32, 8, 128, 64, 2500), (6, 6, 64, 90, 2100), (40, 2, 64, 260, 2000)])
+def test_long_ones_among_many_are_cut(gpu, n, n_kv, s, B, longest, kind):
+    rng = np.random.default_rng(B)
+    lens = _unequal(rng, B, longest)
+    c = Cache(kind, lens, n_kv, s, seed=n)
+    q = gu.to_dev(rows(rng, B, n, s))
+    ctx = _ctx(n, n_kv, s)
+    bound = longest + 200
+    table = np.pad(c.table, ((0, 0), (0, 13)), constant_values=-1)
+    outs = []
+    for fill in (0, 255):                # whatever the workspace holds
+        ws = torch.full((ctx.ds_decode_quant_workspace_bytes(B, bound),), fill, dtype=torch.uint8, device="cuda")
+        o = torch.full_like(q, 9.0)
+        ctx.ds_decode_attention_quant(q, gu.i32_dev(lens), gu.i32_dev(table), B, table.shape[1], bound, *c.args, o, ws)
+        torch.cuda.synchronize()
+        outs.append(o)
+    _check(outs[0], q, c, n, s)
+    assert torch.equal(*outs)
+    # all of one length: nothing is cut
+    kept = [min(l, 40) for l in lens]
+    _check(_attend(ctx, q, c, lens=kept, max_len=longest), q, c, n, s, lens=kept)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+def test_long_ones_among_many_behind_prefixes(gpu, kind):
+    n, n_kv, s, B = 16, 8, 64, 70
+    rng = np.random.default_rng(8)
+    own, prefix = _unequal(rng, B, 1900), [600, 0, 33]
+    c, cu = _groups([40, 3, 27], prefix, own, n_kv, s, kind, 4)
+    q = gu.to_dev(rows(rng, B, n, s))
+    o = _shared(_ctx(n, n_kv, s), q, c, cu, prefix, own)
+    _check_shared(o, q, c, cu, s)
+    assert torch.equal(o, _shared(_ctx(n, n_kv, s), q, c, cu, prefix, own))
