@@ -340,8 +340,8 @@ ds_status ds_decode_attention_shared(ds_ctx *ctx, const void *q, const int32_t *
                                      size_t workspace_bytes, void *stream);
 
 /* ds_decode_step for such rows, on a cache of any kv_type: ctx_lens[i] own tokens before this step (the prefix not
- * counted), the new one appended behind them, into a page that is no other row's and no prefix's.  On 8 bits a row of
- * ctx_lens[i] = -1 appends nothing and attends over its group's prefix alone; with DS_KV_BF16 ctx_lens[i] >= 0. */
+ * counted), the new one appended behind them, into a page that is no other row's and no prefix's.  A row of
+ * ctx_lens[i] = -1 pads the batch: it appends nothing and attends over its group's prefix alone. */
 ds_status ds_decode_step_shared(ds_ctx *ctx, const ds_layer_weights *w, const void *x, const int32_t *cu_groups,
                                 int32_t n_groups, int32_t max_group_rows, const int32_t *prefix_lens,
                                 const int32_t *prefix_tables, int32_t max_prefix_blocks, int32_t max_prefix_len,

@@ -1066,7 +1066,7 @@ static ds_status decode_step(ds_ctx* ctx, const ds_layer_weights* w, const void*
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (ctx->validate) {
     std::vector<int32_t> lens;
-    if ((st = validate_lens(ctx, who, ctx_lens, B, 1, cache.kv.type == ds::kKvBf16 ? 1 : 0, max_ctx, s, lens)) != DS_OK) return st;
+    if ((st = validate_lens(ctx, who, ctx_lens, B, 1, cache.tiles ? 0 : 1, max_ctx, s, lens)) != DS_OK) return st;
     if ((st = validate_tables(ctx, who, block_tables, B, max_blocks_per_seq, num_blocks, lens, s)) != DS_OK) return st;
     if (cache.kv.type != ds::kKvBf16 &&
         (st = validate_new_pages(ctx, who, block_tables, B, max_blocks_per_seq, lens, s)) != DS_OK)

@@ -38,7 +38,7 @@ struct GemmParams {
   // accumulators to partial[s][M][N]; the epilogue then belongs to whoever adds the partials.
   float* partial;
   // Decode QKV projection (N = (n_heads + 2 n_kv_heads) head_dim): with k_cache set, the K and V parts of
-  // row m go to slot ctx_lens[m] of the paged cache [num_blocks, n_kv_heads, 16, head_dim] instead of `out`.
+  // row m go to slot ctx_lens[m] of the paged cache [num_blocks, n_kv_heads, 16, head_dim] instead of `out` (negative: nowhere).
   const int32_t* ctx_lens;
   const int32_t* block_tables;
   int max_blocks;
@@ -524,6 +524,7 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void gemm_dl_kernel(const G
           const int col = n - hq - which * hkv;
           const int head = col / p.head_dim, d = col - head * p.head_dim;
           const int pos = p.ctx_lens[row];
+          if (pos < 0) continue;  // a row that pads the batch
           const int blk = p.block_tables[(size_t)row * p.max_blocks + pos / 16];
           st16((which ? p.v_cache : p.k_cache) + (((size_t)blk * p.n_kv_heads + head) * 16 + (pos % 16)) * p.head_dim + d, o);
         } else {

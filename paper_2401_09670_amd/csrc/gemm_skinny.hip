@@ -65,7 +65,7 @@ struct SkinnyParams {
   float* amax_val = nullptr;
   int32_t* amax_idx = nullptr;
   // Unsplit launches only: with kv_k_cache set (decode QKV projection, N = (n + 2 n_kv) s) the K and V
-  // parts of row m go to slot kv_ctx_lens[m] of the paged cache [num_blocks, n_kv, 16, s] instead of `out`.
+  // parts of row m go to slot kv_ctx_lens[m] of the paged cache [num_blocks, n_kv, 16, s] instead of `out` (negative: nowhere).
   const int32_t* kv_ctx_lens = nullptr;
   const int32_t* kv_block_tables = nullptr;
   int kv_max_blocks = 0;
@@ -118,7 +118,7 @@ struct Epilogue4 {
     const int32_t* at = p.kv_k_cache ? p.kv_block_tables : reinterpret_cast<const int32_t*>(p.W);
     const size_t seqs = p.kv_k_cache ? ~(size_t)0 : 0;
 #pragma unroll
-    for (int t = 0; t < MT; ++t) block[t] = at[((size_t)row(p, lane, t) * p.kv_max_blocks + (pos[t] >> 4)) & seqs];
+    for (int t = 0; t < MT; ++t) block[t] = at[((size_t)row(p, lane, t) * p.kv_max_blocks + (max(pos[t], 0) >> 4)) & seqs];
   }
   __device__ __forceinline__ int row(const SkinnyParams& p, int lane, int t) const {
     return min(first + 16 * t + (lane & 15), p.M - 1);
@@ -136,6 +136,7 @@ struct Epilogue4 {
     const u32x2 o{pack_bf16(r[0], r[1]), pack_bf16(r[2], r[3])};
     const int hq = p.kv_n_heads * p.kv_head_dim, hkv = p.kv_n_kv_heads * p.kv_head_dim;
     if (p.kv_k_cache && n >= hq) {
+      if (pos[t] < 0) return;  // a row that pads the batch
       const int which = n >= hq + hkv;
       const int col = n - hq - which * hkv, shift = __builtin_ctz(p.kv_head_dim);  // 64 or 128
       const int head = col >> shift, d = col - (head << shift);
@@ -858,7 +859,7 @@ __global__ __launch_bounds__(kRedLnThreads) void skinny_reduce_ln_kernel(const S
 
 // The same reduction for the decode QKV projection (N = (n + 2 n_kv) s, one output buffer with row stride N):
 // the Q part is written to out[0]; the K and V parts are this step's new cache rows and go to
-// slot ctx_lens[m] of the paged cache [num_blocks, n_kv, 16, s].
+// slot ctx_lens[m] of the paged cache [num_blocks, n_kv, 16, s] (negative: nowhere).
 __global__ __launch_bounds__(256) void skinny_reduce_kv_kernel(const SkinnyParams p, int n_splits,
                                                                const int32_t* __restrict__ ctx_lens,
                                                                const int32_t* __restrict__ block_tables,
@@ -872,7 +873,7 @@ __global__ __launch_bounds__(256) void skinny_reduce_kv_kernel(const SkinnyParam
   const int n = (int)(idx % chunks_per_row) * 8;
   const EpiPieces e = epi_load(p, m, n);
   const int pos = ctx_lens[m];
-  const int blk = block_tables[(size_t)m * max_blocks + pos / 16];
+  const int blk = block_tables[(size_t)m * max_blocks + max(pos, 0) / 16];
   float v[8];
   sum_partials8(p, n_splits, m, n, v);
   epi_apply(p, e, v);
@@ -884,6 +885,7 @@ __global__ __launch_bounds__(256) void skinny_reduce_kv_kernel(const SkinnyParam
     st16(p.out[0] + (size_t)m * p.N + n, ov);
     return;
   }
+  if (pos < 0) return;  // a row that pads the batch
   const int which = n >= h + hkv;
   const int col = n - h - which * hkv;
   const int head = col / head_dim, d = col - head * head_dim;

@@ -86,7 +86,7 @@ hipError_t launch_gemm(const void* X, const void* W, int M, int N, int K, const 
 //  kLayerNorm: after out = act(..) + residual is written, also write ln_out = LN(out) (row-wise).
 //  kKvAppend : columns [0, n s) go to out[0] as usual; the next n_kv s columns and the n_kv s after
 //              them are this step's K / V rows and go straight into the paged cache
-//              [num_blocks, n_kv, 16, s] at position ctx_lens[row].
+//              [num_blocks, n_kv, 16, s] at position ctx_lens[row] (negative: nowhere).
 struct SkinnyFused {
   enum Kind { kNone = 0, kLayerNorm = 1, kKvAppend = 2 } kind = kNone;
   const void* ln_gamma = nullptr;
@@ -154,7 +154,7 @@ hipError_t launch_kv_migrate(const void* k_src, const void* v_src, const int32_t
                              int max_seqlen, const int32_t* block_tables, int max_blocks, void* k_cache,
                              void* v_cache, int n_heads, int head_dim, hipStream_t stream);
 
-// new K,V rows (row stride `src_stride` elements) of B sequences -> slot ctx_lens[i] of the paged cache
+// new K,V rows (row stride `src_stride` elements) of B sequences -> slot ctx_lens[i] (negative: none) of the paged cache
 hipError_t launch_kv_append(const void* k_new, const void* v_new, int src_stride, const int32_t* ctx_lens,
                             const int32_t* block_tables, int B, int max_blocks, void* k_cache, void* v_cache,
                             int n_heads, int head_dim, hipStream_t stream);

@@ -126,6 +126,7 @@ __global__ __launch_bounds__(256) void kv_append_kernel(const uint16_t* __restri
   const int seq = blockIdx.x;
   const int which = blockIdx.y;
   const int pos = ctx_lens[seq];
+  if (pos < 0) return;  // a row that pads the batch
   const int blk = block_tables[(size_t)seq * max_blocks + pos / kPage];
   const int slot = pos % kPage;
   const int cps = head_dim >> 3;
