@@ -100,8 +100,9 @@ const char *ds_last_error(const ds_ctx *ctx);
  * length in [1, max_seqlen]); ds_kv_migrate, ds_decode_step and ds_decode_attention check that every
  * page a sequence's tokens need is named in block_tables with an id in [0, num_blocks), and that
  * ctx_lens[i] + 1 lies in [1, max_ctx] (kv_lens[i] in [0, max_kv_len]).  The calls for 8 bits and for shared prefixes
- * check the same, cu_groups (from 0 to B, no group above max_group_rows), the prefixes' lengths and pages, and that no
- * two rows append to one page of 8 bits. */
+ * check the same, cu_groups (from 0 to B, no group above max_group_rows), the prefixes' lengths and pages, that no
+ * two rows append to one page of 8 bits, and in ds_decode_step_shared that a row appends to no prefix's and no other
+ * row's page, whatever the pages hold. */
 ds_status ds_set_validate(ds_ctx *ctx, int32_t on);
 
 /* Workspace (device bytes) for ds_prefill with up to max_tokens packed tokens.

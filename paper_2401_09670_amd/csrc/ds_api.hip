@@ -1019,6 +1019,37 @@ static ds::TileAttention tile_attention(const ds_ctx* ctx, const StepCache& cach
   return t;
 }
 
+// Behind prefixes: a new token's page (tokens[i]: the row's with the new one; 0: it writes nothing) is no prefix's and no
+// other row's.  Lengths and tables are within their bounds.
+static ds_status validate_page_owners(ds_ctx* ctx, const char* who, const StepCache& cache, const int32_t* bt_dev, int B,
+                                      int max_blocks, const std::vector<int32_t>& tokens, hipStream_t s) {
+  std::vector<int32_t> bt, lens, pt;
+  if (ds_status st = fetch_i32(ctx, bt_dev, (size_t)B * max_blocks, s, bt)) return st;
+  if (ds_status st = fetch_i32(ctx, cache.prefix_lens, (size_t)cache.n_groups, s, lens)) return st;
+  if (ds_status st = fetch_i32(ctx, cache.prefix_tables, (size_t)cache.n_groups * cache.max_prefix_blocks, s, pt)) return st;
+  const int page = ctx->cfg.block_size;
+  try {
+    std::unordered_map<int32_t, int> writer;
+    for (int i = 0; i < B; ++i)
+      if (tokens[i] > 0) writer.emplace(bt[(size_t)i * max_blocks + (tokens[i] - 1) / page], i);
+    for (int g = 0; g < cache.n_groups; ++g)
+      for (int j = 0; j < (lens[g] + page - 1) / page; ++j) {
+        const auto hit = writer.find(pt[(size_t)g * cache.max_prefix_blocks + j]);
+        if (hit != writer.end())
+          return fail(ctx, DS_ERR_BOUNDS, "%s: row %d writes into block %d, which is prefix %d's", who, hit->second, hit->first, g);
+      }
+    for (int i = 0; i < B; ++i)
+      for (int j = 0; j < (tokens[i] + page - 1) / page; ++j) {
+        const auto hit = writer.find(bt[(size_t)i * max_blocks + j]);
+        if (hit != writer.end() && hit->second != i)
+          return fail(ctx, DS_ERR_BOUNDS, "%s: row %d writes into block %d, which is row %d's", who, hit->second, hit->first, i);
+      }
+  } catch (const std::exception&) {
+    return fail(ctx, DS_ERR_INVALID_ARG, "%s: no memory for the pages of %d rows", who, B);
+  }
+  return DS_OK;
+}
+
 // Every decode-step entry point: `workspace` is the caller's buffer, or null for the static scratch array
 // of the current device (then the step must fit DS_STATIC_SCRATCH_BYTES).
 static ds_status decode_step(ds_ctx* ctx, const ds_layer_weights* w, const void* x, const int32_t* ctx_lens,
@@ -1074,6 +1105,9 @@ static ds_status decode_step(ds_ctx* ctx, const ds_layer_weights* w, const void*
     if (cache.n_groups > 0 &&
         (st = validate_groups(ctx, who, cache.cu_groups, cache.n_groups, cache.max_group_rows, B, cache.prefix_lens,
                               cache.prefix_tables, cache.max_prefix_blocks, cache.max_prefix, num_blocks, s)) != DS_OK)
+      return st;
+    if (cache.n_groups > 0 &&
+        (st = validate_page_owners(ctx, who, cache, block_tables, B, max_blocks_per_seq, lens, s)) != DS_OK)
       return st;
   }
   Carver ws(workspace);
