@@ -304,7 +304,8 @@ ds_status ds_kv_append_quant(ds_ctx *ctx, const void *k_new, const void *v_new, 
                              int32_t max_blocks_per_seq, void *k_cache, void *v_cache, void *k_scale, void *v_scale,
                              int32_t num_blocks, int32_t kv_type, void *stream);
 
-/* ds_decode_attention over such a cache; kv_lens[i] = 0: output 0.  Workspace: ds_decode_quant_workspace_bytes(B,
+/* ds_decode_attention over such a cache; kv_lens[i] = 0: output 0.  Scores are fp32: a key whose score is below its range
+ * weighs nothing (all of them: output 0), one above it makes the row NaN.  Workspace: ds_decode_quant_workspace_bytes(B,
  * max_kv_len), which serves every smaller batch and length too, and ds_decode_step_quant with max_ctx for max_kv_len.
  * The result does not depend on the workspace's size. */
 size_t ds_decode_quant_workspace_bytes(const ds_ctx *ctx, int32_t max_batch, int32_t max_ctx);

@@ -118,7 +118,7 @@ __device__ __forceinline__ int ranked(int pages, int r, int bits) {
   return __builtin_ctzll(__builtin_amdgcn_ballot_w64(((left >> lane) & 1) && before == r));
 }
 
-// Running softmax over N score tiles (scaled by log2 e, -inf where there is no key): p in place of s.
+// Running softmax over N score tiles (scaled by log2 e, -inf where there is no key, or one below fp32's range): p in place of s.
 template <int N, int DB>
 __device__ __forceinline__ void online_softmax(floatx4 (&s)[N], floatx4 (&acc)[DB], float& m_run, float& l_run) {
   float top = -INFINITY;
@@ -633,7 +633,7 @@ __global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(WI
     }
   }
   floatx4 acc[DB];
-  float m_run = -INFINITY, l_run = 0.f;  // l_run: this lane's share of the sum
+  float m_run = kLowestScore, l_run = 0.f;  // l_run: this lane's share of the sum
 #pragma unroll
   for (int db = 0; db < DB; ++db) acc[db] = floatx4{0.f, 0.f, 0.f, 0.f};
 
@@ -665,7 +665,7 @@ __global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(WI
   }
   if (p.solo) return store_columns<HD>(a, w, lane_anew() & 15, acc, m_run, across_groups<16>(l_run, AddOp()));
 
-  // Merge the waves.  A wave without keys has maximum -inf and weight 0.
+  // Merge the waves.  A wave without keys has the lowest maximum and sum and output 0.  (Where scores are NaN, so is the sum.)
   const int thread = 64 * wave + lane_anew();
   const float l = across_groups<16>(l_run, AddOp());
   float* mg = reinterpret_cast<float*>(smem);  // [wave][column][output[HD], max, sum, -, -]
@@ -682,7 +682,7 @@ __global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(WI
   constexpr int ND = HD / 16;
   const int c = thread >> 4, d0 = (thread & 15) * ND;
   if (c >= w.cols) return;
-  float m = -INFINITY, sum = 0.f, out[ND];
+  float m = kLowestScore, sum = 0.f, out[ND];
 #pragma unroll
   for (int i = 0; i < kTileWaves; ++i) m = fmaxf(m, mg[(i * 16 + c) * kState + HD]);
 #pragma unroll
@@ -690,7 +690,7 @@ __global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(WI
 #pragma unroll
   for (int i = 0; i < kTileWaves; ++i) {
     const float* src = mg + (i * 16 + c) * kState;
-    const float f = src[HD] > -INFINITY ? __builtin_amdgcn_exp2f(src[HD] - m) : 0.f;  // (NaN: its sum is NaN, times anything)
+    const float f = __builtin_amdgcn_exp2f(src[HD] - m);
     sum += src[HD + 1] * f;
 #pragma unroll
     for (int j = 0; j < ND; ++j) out[j] += src[d0 + j] * f;
@@ -734,10 +734,10 @@ __global__ __launch_bounds__(kTileThreads) void tile_combine_kernel(const float*
     n_states = counted + __builtin_amdgcn_readfirstlane(reinterpret_cast<const int*>(src)[counted * kState + HD + 2]);
     if (n_states <= 1) return;
   }
-  float m_run = -INFINITY, l_run = 0.f, out[ND] = {};
+  float m_run = kLowestScore, l_run = 0.f, out[ND] = {};
   for (int s0 = wave; s0 < n_states; s0 += 64 * W) {
     const int n = min((n_states - s0 + W - 1) / W, 64);  // of them in this turn
-    float m = -INFINITY, l = 0.f;
+    float m = kLowestScore, l = 0.f;
     if (lane < n) {
       m = src[(size_t)(s0 + W * lane) * kState + HD];
       l = src[(size_t)(s0 + W * lane) * kState + HD + 1];
@@ -756,8 +756,8 @@ __global__ __launch_bounds__(kTileThreads) void tile_combine_kernel(const float*
     top = lane_op<2>(top, MaxOp());
     top = lane_op<kMirror4>(top, MaxOp());
     top = across_groups<8>(top, MaxOp());
-    const float m_new = fmaxf(m_run, top), alpha = m_run > -INFINITY ? __builtin_amdgcn_exp2f(m_run - m_new) : 0.f;
-    const float f = m > -INFINITY ? __builtin_amdgcn_exp2f(m - m_new) : 0.f;
+    const float m_new = fmaxf(m_run, top), alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+    const float f = __builtin_amdgcn_exp2f(m - m_new);
     l_run = l_run * alpha + wave_sum(l * f);
 #pragma unroll
     for (int j = 0; j < ND; ++j) out[j] *= alpha;
@@ -788,12 +788,12 @@ __global__ __launch_bounds__(kTileThreads) void tile_combine_kernel(const float*
   __syncthreads();
   const int d = threadIdx.x;
   if (d >= HD) return;
-  float m = -INFINITY, sum = 0.f, r = 0.f;
+  float m = kLowestScore, sum = 0.f, r = 0.f;
 #pragma unroll
   for (int i = 0; i < W; ++i) m = fmaxf(m, merge[i][HD]);
 #pragma unroll
   for (int i = 0; i < W; ++i) {
-    const float f = merge[i][HD] > -INFINITY ? __builtin_amdgcn_exp2f(merge[i][HD] - m) : 0.f;
+    const float f = __builtin_amdgcn_exp2f(merge[i][HD] - m);
     sum += merge[i][HD + 1] * f;
     r += merge[i][d] * f;
   }

@@ -90,6 +90,9 @@ __device__ __forceinline__ float within_group(float v, Op op) {
   if constexpr (LANES == 16) v = lane_op<8>(v, op);
   return v;
 }
+// What a running maximum of scores starts from: finite, so that keys whose scores are all below fp32's range (-inf) leave it
+// where it is and weigh exp(-inf - it) = 0, as those do that are not there.  From -inf on they would weigh exp(-inf + inf) = NaN.
+constexpr float kLowestScore = -3.40282347e38f;
 // Sum over the wave, in every lane.
 __device__ __forceinline__ float wave_sum(float v) {
   v = lane_op<32>(v, AddOp());
