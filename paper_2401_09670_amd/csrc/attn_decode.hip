@@ -73,7 +73,7 @@ __global__ __launch_bounds__(kDecThreads) void decode_attention_kernel(
   const int32_t* bt = block_tables + (size_t)seq * max_blocks;
   const size_t page_elems = (size_t)kDecPage * HD;
 
-  float m_run = -INFINITY, l_run = 0.f;
+  float m_run = kLowestScore, l_run = 0.f;
   float acc[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) acc[j] = 0.f;
@@ -113,7 +113,7 @@ __global__ __launch_bounds__(kDecThreads) void decode_attention_kernel(
       tmax = fmaxf(tmax, sc[j]);
     }
     tmax = across_groups<LPT>(tmax, MaxOp());
-    // the first token of a visited page is always < kv_len, so tmax is finite
+    // (tmax is -inf only where every key's score is below fp32's range)
     const float m_new = fmaxf(m_run, tmax);
     const float alpha = exp2f((m_run - m_new) * scale_log2e);
     const float mb = m_new * scale_log2e;
@@ -155,13 +155,13 @@ __global__ __launch_bounds__(kDecThreads) void decode_attention_kernel(
     }
   }
   __syncthreads();
-  // merge the waves (a wave that saw no page has max = -inf, sum = 0 and weight 0)
+  // merge the waves (a wave that saw no page has the lowest maximum, sum = 0 and weight 0)
   if (tid < HD) {
     float m = sm_m[0];
 #pragma unroll
     for (int w = 1; w < kDecWaves; ++w) m = fmaxf(m, sm_m[w]);
     float l = 0.f, a = 0.f;
-    if (m > -INFINITY) {
+    if (m > kLowestScore) {
 #pragma unroll
       for (int w = 0; w < kDecWaves; ++w) {
         const float f = exp2f((sm_m[w] - m) * scale_log2e);
@@ -204,7 +204,7 @@ __global__ __launch_bounds__(HD) void decode_combine_kernel(const float* __restr
     }
   };
   load(0);
-  float m = -INFINITY;
+  float m = kLowestScore;
 #pragma unroll
   for (int u = 0; u < U; ++u) m = fmaxf(m, ms[u]);
   for (int s0 = U; s0 < n_splits; s0 += U) {
@@ -219,7 +219,7 @@ __global__ __launch_bounds__(HD) void decode_combine_kernel(const float* __restr
     if (s0 > 0) load(s0);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      if (s0 + u < n_splits && ms[u] > -INFINITY) {
+      if (s0 + u < n_splits && ms[u] > kLowestScore) {
         const float f = exp2f((ms[u] - m) * scale_log2e);
         l += ls[u] * f;
         a += as[u] * f;
@@ -287,7 +287,7 @@ __global__ __launch_bounds__(kDecThreads) __attribute__((amdgpu_waves_per_eu(2))
   floatx4 acc[HD / 16];  // O^T[d = 16 db + 4 g + r][head = hl]
 #pragma unroll
   for (int db = 0; db < HD / 16; ++db) acc[db] = floatx4{0.f, 0.f, 0.f, 0.f};
-  float m_run = -INFINITY, l_run = 0.f;  // l_run: this lane group's share of the sum
+  float m_run = kLowestScore, l_run = 0.f;  // l_run: this lane group's share of the sum
 
   uint16_t* vst = reinterpret_cast<uint16_t*>(smem) + wave * kStage;
   // K as operand A: lane (key = hl, group g) holds K[key][32 s + 8 g .. + 8) for s = 0..3.
@@ -353,7 +353,7 @@ __global__ __launch_bounds__(kDecThreads) __attribute__((amdgpu_waves_per_eu(2))
       tmax = fmaxf(tmax, fmaxf(sc[r], sc[4 + r]));
     }
     tmax = across_groups<16>(tmax, MaxOp());
-    // the first key of a visited pair is always < kv_len, so tmax is finite
+    // (tmax is -inf only where every key's score is below fp32's range)
     const float m_new = fmaxf(m_run, tmax);
     const float alpha = exp2f((m_run - m_new) * scale_log2e);
     const float mb = m_new * scale_log2e;
@@ -422,16 +422,16 @@ __global__ __launch_bounds__(kDecThreads) __attribute__((amdgpu_waves_per_eu(2))
       for (int r = 0; r < 4; ++r) dst[2 + 16 * db + 4 * g + r] = acc[db][r];
   }
   __syncthreads();
-  // thread -> head tid / 16, d = 8 (tid % 16) .. + 8; a wave that saw no pair has max = -inf and weight 0
+  // thread -> head tid / 16, d = 8 (tid % 16) .. + 8; a wave that saw no pair has the lowest maximum and weight 0
   const int h = tid >> 4, d0 = (tid & 15) * 8;
   if (h < G) {
-    float m = -INFINITY;
+    float m = kLowestScore;
 #pragma unroll
     for (int w = 0; w < kDecWaves; ++w) m = fmaxf(m, mg[(size_t)(w * 16 + h) * (HD + 2)]);
     float l = 0.f, a[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) a[j] = 0.f;
-    if (m > -INFINITY) {
+    if (m > kLowestScore) {
 #pragma unroll
       for (int w = 0; w < kDecWaves; ++w) {
         const float* src = mg + (size_t)(w * 16 + h) * (HD + 2);

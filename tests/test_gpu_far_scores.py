@@ -87,6 +87,20 @@ def test_behind_prefixes(gpu, n, n_kv, s, rows_of, prefix, kind):
         _check(gu.to_f64(o[i]), gu.to_f64(q[i]), [(*c.seq(g), _far(plens[g])), (*c.seq(groups + i), _far(own[i]))], s)
 
 
+@pytest.mark.parametrize("n,n_kv,s", [(4, 4, 64), (8, 2, 64), (8, 8, 128), (8, 2, 128), (40, 1, 128)])
+@pytest.mark.parametrize("lens", [[150, 1, 64, 33, 400, 129], [3000]], ids=["short", "split"])
+def test_the_bf16_cache(gpu, n, n_kv, s, lens):
+    c, B = _cache("bf16", lens, n_kv, s, 3), len(lens)
+    q = gu.to_dev(_queries(np.random.default_rng(1), B, n, s))
+    ctx = binding.Context(n * s, n, s, 64, n_kv_heads=n_kv)
+    o = torch.full_like(q, 9.0)
+    ctx.ds_decode_attention(q, gu.i32_dev(lens), gu.i32_dev(c.table), B, c.table.shape[1], max(lens), c.k, c.v, c.nb, o,
+                            gu.workspace(ctx.ds_decode_workspace_bytes(B, max(lens))))
+    torch.cuda.synchronize()
+    for i, l in enumerate(lens):
+        _check(gu.to_f64(o[i]), gu.to_f64(q[i]), [(*c.seq(i), _far(l))], s)
+
+
 def test_nothing_but_far_keys_is_nothing(gpu):
     n, s, lens = 8, 128, [64, 5]
     k = -(1 + np.random.default_rng(0).random((69, n, s))) * 2.0 ** 70
