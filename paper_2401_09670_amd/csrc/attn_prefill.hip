@@ -162,7 +162,7 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
     for (int d = 0; d < DT; ++d)
 #pragma unroll
       for (int r = 0; r < 16; ++r) oacc[d][r] = 0.f;
-    float m_run = -INFINITY;  // running max of raw scores for query my_q (same in lanes lq and lq+32)
+    float m_run = kLowestScore;  // running max of raw scores for query my_q (same in lanes lq and lq+32)
     float l_run = 0.f;        // this lane's share of the running sum
 
     const int kv_end = min(len, q0 + kAttQ);  // keys any query of this workgroup may see
@@ -249,7 +249,7 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
       // (and the accumulators rescaled) only when some query's maximum grew by more than kSlack in
       // the exponent: probabilities then stay below 2^kSlack and the final quotient is unchanged.
       if (__builtin_amdgcn_ballot_w64(tmax * scale_log2e > m_run * scale_log2e + kSlack) != 0) {
-        const float m_new = fmaxf(m_run, tmax);  // finite: key kv0 is visible to every query of the wave
+        const float m_new = fmaxf(m_run, tmax);
         const float alpha = __builtin_amdgcn_exp2f((m_run - m_new) * scale_log2e);
         l_run *= alpha;
         m_run = m_new;
@@ -314,7 +314,7 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
     // ---- normalise and store: lane holds O[my_q][32d + 8g + 4hl + i] ----
     const float l_tot = lane_op<32>(l_run, AddOp());
     if (my_q < len) {
-      const float inv = 1.f / l_tot;
+      const float inv = l_tot == 0.f ? 0.f : 1.f / l_tot;  // (every score below fp32's range: 0)
       uint16_t* orow = o + ((size_t)start + my_q) * h + (size_t)head * HD + hl * 4;
 #pragma unroll
       for (int d = 0; d < DT; ++d)

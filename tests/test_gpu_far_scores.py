@@ -4,6 +4,7 @@ import numpy as np
 import pytest
 import torch
 
+from oracle import ds_oracle as orc
 from oracle import kv_quant_oracle as kvo
 from paper_2401_09670_amd import binding, synth
 from tests import gpu_util as gu
@@ -99,6 +100,29 @@ def test_the_bf16_cache(gpu, n, n_kv, s, lens):
     torch.cuda.synchronize()
     for i, l in enumerate(lens):
         _check(gu.to_f64(o[i]), gu.to_f64(q[i]), [(*c.seq(i), _far(l))], s)
+
+
+@pytest.mark.parametrize("n,n_kv,s", [(4, 4, 64), (4, 2, 128)])
+def test_prompts(gpu, n, n_kv, s):
+    """Causal, over packed prompts; a query that sees far keys alone gets 0.  The sum counts the rounded probabilities here:
+    2^-8 of the output more."""
+    lens, rng = [400, 1, 129, 64, 150], np.random.default_rng(6)
+    t = sum(lens)
+    qb, kb, vb = _queries(rng, t, n, s), _keys(rng, lens, n_kv, s), _bits(rng.standard_normal((t, n_kv, s)))
+    ctx = binding.Context(n * s, n, s, 64, n_kv_heads=n_kv)
+    q = gu.to_dev(qb)
+    o = torch.full_like(q, 9.0)
+    ctx.ds_prefill_attention(q, gu.to_dev(kb), gu.to_dev(vb), gu.i32_dev(synth.cu_seqlens(lens)), len(lens), t, max(lens), o)
+    torch.cuda.synchronize()
+    got, q, k, v, r0 = gu.to_f64(o), *(orc.from_bf16_bits(x) for x in (qb, kb, vb)), 0
+    for l in lens:
+        far = _far(l)
+        for i in range(l):
+            seen = np.flatnonzero(~far[:i + 1]) + r0
+            want, pav, size = kvo.attend(q[r0 + i], k[seen], v[seen])
+            bound = kvo.attention_bound(want, pav, size, s, i + 1) + 2.0 ** -8 * np.abs(want) * 1.01
+            assert (np.abs(got[r0 + i] - want) <= bound).all(), (l, i)
+        r0 += l
 
 
 def test_nothing_but_far_keys_is_nothing(gpu):
