@@ -277,7 +277,10 @@ ds_status ds_decode_attention(ds_ctx *ctx, const void *q, const int32_t *kv_lens
  * stands for, value times c, is exact in fp32.
  *   k_cache [num_blocks, n_kv, 16, s] bytes; v_cache [num_blocks, n_kv, s, 16] bytes - a feature's 16 tokens together, unlike
  *   the bf16 cache; k_scale, v_scale [num_blocks, n_kv, 16] bf16.  Block tables are those of the bf16 cache.
- * With DS_KV_BF16, where a call takes it, k_cache and v_cache are the bf16 cache and the scales NULL. */
+ * With DS_KV_BF16, where a call takes it, k_cache and v_cache are the bf16 cache and the scales NULL.
+ * The attention's sums, maxima and scales are fp32; a probability is rounded to 2^-16 of itself before it meets V, to 2^-8
+ * where more than 16 queries of a key/value head go over the same pages of 8 bits together (more than 16 query heads on it, or
+ * a group's rows over its prefix). */
 enum { DS_KV_BF16 = 0, DS_KV_E4M3 = 1, DS_KV_INT8 = 2 };
 
 /* ds_kv_migrate into such a cache: every row quantised as it is written.  Slots that no token maps to keep their bytes. */

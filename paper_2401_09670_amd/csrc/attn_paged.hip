@@ -8,8 +8,13 @@
 // In the result of the first a lane has one column (lane % 16) and 4 keys, so the softmax's running maximum and sum are
 // scalars of a lane; with the keys dealt out as below the probabilities are already the second product's operand B.
 // Values of 8 bits go to bf16 exactly; the scales of K multiply the scores, those of V the probabilities, in fp32.
-// Probabilities are rounded to bf16 for the second product (at most 2^-8 of each, in no one direction); the sum is that of
-// the unrounded ones.
+// For the second product a probability (times V's scale) is two bf16 numbers, the nearest and what that leaves: at most 2^-16
+// of it is lost, and what is left of a result's error is its own rounding to bf16.  (The nearest alone, 2^-8: the error against
+// 64 bits is 1.3 to 2.4 % larger over hundreds of tokens, 13 % over 37.  The second product twice costs 1 to 2 % where HBM
+// bounds the kernel, with the append 64 sequences of 545 e4m3 tokens 70.0 -> 71.0 us, 128 of 16 to 2048 109.1 -> 110.0, and 10 %
+// in wide tiles: 7, 40 and 1 rows of 64 heads on 8 behind some 7000 bf16 tokens 40.1 -> 44.2.)  In wide tiles over 8 bits it is
+// the nearest alone: what V itself loses in 8 bits is 4 to 16 times as much, and both would take 41.2 us there instead of 37.2,
+// for an error that is 0.2 % smaller.  The sum is that of the unrounded probabilities.
 //
 // A launch has up to two parts, the groups' prefixes and the rows' own pages, and a workgroup of 4 waves takes one
 // (group, key/value head, block of columns, split of the pages) of either part:
@@ -145,10 +150,17 @@ __device__ __forceinline__ void online_softmax(floatx4 (&s)[N], floatx4 (&acc)[D
     }
   l_run += sum;
 }
-__device__ __forceinline__ u32x4 probabilities(const floatx4* s) {  // of two tiles
-  u32x4 p;
+struct Probabilities {  // operand B of two tiles
+  u32x4 near, rest;
+};
+__device__ __forceinline__ Probabilities probabilities(const floatx4* s) {
+  Probabilities p;
 #pragma unroll
-  for (int w = 0; w < 4; ++w) p[w] = pack_bf16(s[w / 2][2 * (w % 2)], s[w / 2][2 * (w % 2) + 1]);
+  for (int w = 0; w < 4; ++w) {
+    const float a = s[w / 2][2 * (w % 2)], b = s[w / 2][2 * (w % 2) + 1];
+    p.near[w] = pack_bf16(a, b);
+    p.rest[w] = pack_bf16(a - bf16_lo(p.near[w]), b - bf16_hi(p.near[w]));
+  }
   return p;
 }
 template <int T>
@@ -249,7 +261,7 @@ __device__ __forceinline__ void narrow_quant(const TileArgs& a, const TileWork& 
     });
     online_softmax(s, acc, m_run, l_run);
     each(std::make_integer_sequence<int, 8>{}, [&](auto j) { s[j() / 4][j() % 4] *= row_lane<j()>(vs); });
-    const u32x4 pf = probabilities(s);
+    const Probabilities pf = probabilities(s);
     // A load gave the lane 16 keys of one feature, g & 1 choosing between two blocks of 16 features: words 2, 3 of the
     // even rows of lanes against words 0, 1 of the odd ones, and words 0, 1 are 8 keys of the first block in every lane,
     // words 2, 3 of the second.
@@ -268,9 +280,13 @@ __device__ __forceinline__ void narrow_quant(const TileArgs& a, const TileWork& 
       for (int i = 0; i < VL; ++i) vr[i] &= u32x4{keep0, keep1, keep0, keep1};
     }
 #pragma unroll
-    for (int i = 0; i < VL; ++i)
+    for (int i = 0; i < VL; ++i) {
+      const u32x4 v[2] = {values8<T>(vr[i][0], vr[i][1]), values8<T>(vr[i][2], vr[i][3])};
 #pragma unroll
-      for (int h = 0; h < 2; ++h) acc[2 * i + h] = mfma(values8<T>(vr[i][2 * h], vr[i][2 * h + 1]), pf, acc[2 * i + h]);
+      for (int h = 0; h < 2; ++h) acc[2 * i + h] = mfma(v[h], pf.near, acc[2 * i + h]);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) acc[2 * i + h] = mfma(v[h], pf.rest, acc[2 * i + h]);
+    }
     if (more) {
       fetch_v();
       ids(pg + 2 * w.step);
@@ -347,11 +363,17 @@ __device__ __forceinline__ void narrow_bf16(const TileArgs& a, const TileWork& w
 #pragma unroll
       for (int r = 0; r < 4; ++r) s[u][r] = 4 * g + r < there[u] ? s[u][r] * a.scale_log2e : -INFINITY;
     online_softmax(s, acc, m_run, l_run);
-    const u32x4 pf = probabilities(s);
+    const Probabilities pf = probabilities(s);
     __builtin_amdgcn_wave_barrier();  // (a wave's LDS accesses keep their order; the compiler has to keep it too)
     const uint16_t* vfrag = vst + (4 * g + (hl >> 2)) * kVRow<HD> + (hl & 3) * 4;
 #pragma unroll
-    for (int db = 0; db < HD / 16; ++db) acc[db] = mfma(turned<HD>(vfrag, db), pf, acc[db]);
+    for (int db = 0; db < HD / 16; db += 2) {
+      const u32x4 v[2] = {turned<HD>(vfrag, db), turned<HD>(vfrag, db + 1)};
+#pragma unroll
+      for (int h = 0; h < 2; ++h) acc[db + h] = mfma(v[h], pf.near, acc[db + h]);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) acc[db + h] = mfma(v[h], pf.rest, acc[db + h]);
+    }
     __builtin_amdgcn_wave_barrier();
   }
 }
@@ -510,14 +532,15 @@ __device__ __forceinline__ void wide_tiles(const TileArgs& a, const TileWork& w,
     }
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      const u32x4 pf = probabilities(s + 2 * u);
+      const Probabilities pf = probabilities(s + 2 * u);
 #pragma unroll
       for (int db = 0; db < HD / 16; ++db) {
         if constexpr (kQuant) {
           const int d = 16 * db + hl;
-          acc[db] = mfma(ld16(vt + d * kWideKeys + ((4 * u + g) ^ ((d >> 1) & 7)) * 8), pf, acc[db]);
+          acc[db] = mfma(ld16(vt + d * kWideKeys + ((4 * u + g) ^ ((d >> 1) & 7)) * 8), pf.near, acc[db]);
         } else {
-          acc[db] = mfma(turned<HD>(vt + (32 * u + 4 * g + (hl >> 2)) * kVRow<HD> + (hl & 3) * 4, db), pf, acc[db]);
+          const u32x4 v = turned<HD>(vt + (32 * u + 4 * g + (hl >> 2)) * kVRow<HD> + (hl & 3) * 4, db);
+          acc[db] = mfma(v, pf.rest, mfma(v, pf.near, acc[db]));
         }
       }
     }
