@@ -825,11 +825,6 @@ __global__ __launch_bounds__(kTileThreads) void tile_combine_kernel(const float*
 
 // ---- plans ----
 constexpr double kOnceBytes = 256e6;  // of own pages: more than the last-level cache could keep until the next step
-DS_SWITCH(g_tile_own, 0);
-DS_SWITCH(g_tile_prefix, 0);
-DS_SWITCH(g_tile_rank, 1);
-DS_SWITCH(g_tile_solo, -1);
-DS_SWITCH(g_tile_join, -1);
 
 // A key/value head for each wave (`items` of them over all rows) instead of four waves for each: nothing to merge, four times as
 // many at once, but a sequence takes as long as one wave needs.  Of 40 heads (us, four waves and one): 64 sequences of 10
@@ -837,7 +832,6 @@ DS_SWITCH(g_tile_join, -1);
 // and 8.5; 8 key/value heads, 64 of 260 11.4 and 13.0, 128 of 260 17.0 and 15.3.  (256 of 1100 on 8 key/value heads, equal
 // ones, take 118 and 99, but 128 ragged ones up to 2048 on 40 heads 105 and 140.)
 static bool solo_of(long items, long max_len) {
-  if (g_tile_solo >= 0) return g_tile_solo;
   return max_len <= 32 || (items >= 320 && max_len <= 64) || (items >= 1024 && max_len <= 320);
 }
 static int blocks_of(long cols) { return (int)(cols <= kNarrowCols ? 1 : (cols + kWideCols - 1) / kWideCols); }
@@ -891,7 +885,6 @@ static bool joined_of(int splits, int B, int n_heads, int n_kv_heads, int head_d
   const int G = n_heads / n_kv_heads;
   if (G > kNarrowCols || own_bytes > kOnceBytes) return false;
   if (tile_splits((long)B * n_kv_heads, (long)max_len + max_prefix) > 1) return false;
-  if (g_tile_join >= 0) return g_tile_join;
   const double again = (double)B * max_prefix * n_kv_heads * head_dim * (kv_type == kKvBf16 ? 4 : 2);
   return again * 0.1e-6 < 2.4 + 0.25e-3 * B * n_heads * (splits + 1.0);
 }
@@ -905,8 +898,6 @@ TilePlan tile_plan(int B, int n_heads, int n_kv_heads, int head_dim, int kv_type
     p.prefix = prefix_splits(B, n_heads, n_kv_heads, n_groups, max_prefix, own_bytes);
     p.joined = joined_of(p.prefix, B, n_heads, n_kv_heads, head_dim, kv_type, max_len, max_prefix, own_bytes);
   }
-  if (g_tile_own > 0) p.own = g_tile_own;
-  if (g_tile_prefix > 0 && p.prefix > 0) p.prefix = g_tile_prefix;
   return p;
 }
 int tile_most_states(int B, int n_heads, int n_kv_heads, int max_len, int max_prefix) {
@@ -955,7 +946,7 @@ static hipError_t launch_tiles(const TileAttention& t, hipStream_t stream) {
   part(a.part[1], nullptr, t.kv_lens, t.block_tables, t.kv_len_add, t.max_blocks, t.B, G,
        joined ? (long)t.max_kv_len + t.max_prefix : t.max_kv_len, joined ? 1 : t.plan.own, joined ? 0 : t.plan.prefix);
   a.part[1].max_len = t.max_kv_len;
-  a.part[1].rank = g_tile_rank && t.B > 1;
+  a.part[1].rank = t.B > 1;
   const bool wide = a.part[0].wide || a.part[1].wide;
   const bool once = (double)t.B * t.max_kv_len * t.n_kv_heads * HD * (T == kKvBf16 ? 4 : 2) > kOnceBytes;
   const dim3 grid((unsigned)blocks), threads(kTileThreads);
