@@ -274,13 +274,15 @@ ds_status ds_decode_attention(ds_ctx *ctx, const void *q, const int32_t *kv_lens
  *   DS_KV_E4M3  c = 2^e, e the least integer >= -100 with a <= 448 2^e;  values: x_d / c to the nearest e4m3 (OCP), ties to even
  *   DS_KV_INT8  c = the least bf16 >= a / 127 and >= 2^-100;             values: x_d / c to the nearest integer, ties to even
  * a = 0: c = 1.  A row that holds an infinity or a NaN: c = NaN, values 0; all of it then stands for NaN.  What a row
- * stands for, value times c, is exact in fp32.
+ * stands for, value times c, is exact in fp32 (but e4m3 rounds numbers from 248 2^120 on to 2^128, which fp32 does not have).
  *   k_cache [num_blocks, n_kv, 16, s] bytes; v_cache [num_blocks, n_kv, s, 16] bytes - a feature's 16 tokens together, unlike
  *   the bf16 cache; k_scale, v_scale [num_blocks, n_kv, 16] bf16.  Block tables are those of the bf16 cache.
  * With DS_KV_BF16, where a call takes it, k_cache and v_cache are the bf16 cache and the scales NULL.
  * The attention's sums, maxima and scales are fp32; a probability is rounded to 2^-16 of itself before it meets V, to 2^-8
  * where more than 16 queries of a key/value head go over the same pages of 8 bits together (more than 16 query heads on it, or
- * a group's rows over its prefix). */
+ * a group's rows over its prefix).  A token's V on bf16 pages has to be finite: an infinity makes the row NaN.
+ * The bounds max_kv_len, max_ctx and max_prefix_len say what is read and also choose how a call divides its work: results are
+ * equal up to the rounding of the sums, and bounds far above the lengths cost time. */
 enum { DS_KV_BF16 = 0, DS_KV_E4M3 = 1, DS_KV_INT8 = 2 };
 
 /* ds_kv_migrate into such a cache: every row quantised as it is written.  Slots that no token maps to keep their bytes. */

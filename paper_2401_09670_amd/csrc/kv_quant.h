@@ -3,7 +3,8 @@
 //   e4m3  scale c = 2^e, e the least integer >= -100 with a <= 448 2^e;   values RNE(x_d / c)
 //   int8  scale c = the least bf16 >= a / 127, at least 2^-100;           values RNE(x_d / c), |.| <= 127
 // a = 0: c = 1.  An infinity or a NaN in the row: c = NaN, values 0; the row stands for NaN throughout.
-// A value has at most 7, a scale at most 8 significant bits, so what a row stands for (value * c) is exact in fp32.
+// A value has at most 7, a scale at most 8 significant bits, so what a row stands for (value * c) is exact in fp32 (but for the
+// e4m3 numbers from 248 2^120 on, which round to 256 2^120 = 2^128).
 // (The least scale keeps every product above the numbers that bf16 and fp32 hold with fewer bits.)
 //
 // Pages: K [num_blocks, n_kv, 16, s] as the bf16 cache has them; V [num_blocks, n_kv, s, 16], a feature's 16 tokens

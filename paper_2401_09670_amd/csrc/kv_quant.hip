@@ -1,7 +1,7 @@
 // The paged cache of 8 bits as it is written (hand-off, append) and read back.  Formats and layout: kv_quant.h.
 // All three move bytes: what has to be read and written bounds them.  12 ragged prompts of 40 heads, 5197 tokens, int8: 160 MB
-// written off in 30 us (5.4 TB/s) and read back in 26 (6.2); 8 of 2048, 96 heads, e4m3: 1.2 GB in 231 and 209 us (5.3 and 5.8; a
-// large copy reaches 5.15 here).
+// written off in 30 us (5.4 TB/s) and read back in 26 (6.3: that much stays in the last-level cache); 8 of 2048, 96 heads, e4m3,
+// one behind the other: 1.2 GB in 195 and back in 252 us (6.2 and 4.8, together 5.4 TB/s; a large copy reaches 5.15 here).
 #include <type_traits>
 
 #include "kv_quant.h"
