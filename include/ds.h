@@ -357,6 +357,33 @@ ds_status ds_decode_step_shared(ds_ctx *ctx, const ds_layer_weights *w, const vo
                                 void *v_scale, int32_t num_blocks, int32_t kv_type, void *y, void *workspace,
                                 size_t workspace_bytes, void *stream);
 
+/* ---- positions by rotation, attention through a window ----
+ * For layers whose positions are rotations of Q and K and whose attention is a sliding window: the calls between the QKV product
+ * and the out-projection.  They stand beside ds_kv_append_quant, ds_prefill_attention and ds_decode_attention_quant. */
+
+/* New rows of Q, K and V: Q and K turned by their positions, K and V into the paged cache behind the tokens it has, in any kv_type.
+ *   q, k, v     device bf16 [t, n, s], [t, n_kv, s], [t, n_kv, s]; row r starts q_stride * r (k, v: kv_stride * r) elements behind
+ *               them (multiples of 8, at least n s and n_kv s): they may point into the rows of a QKV product
+ *   cu_rows     device [B+1] int32, starts at 0: sequence i has the new rows cu_rows[i] .. cu_rows[i+1]-1, any number of them, 0
+ *               too; rows from cu_rows[B] on are left out.  NULL: one row each, t = B
+ *   ctx_lens    device [B] int32: tokens before them; the j-th new row is token ctx_lens[i] + j, and its page must be in
+ *               block_tables.  -1: a sequence that only pads the batch, of which nothing is read into or written to anything
+ *   positions   device [t] int32: a row's row of the table (outside it: the nearest in it); NULL: the token's number
+ *   table       device fp32 [n_pos, rot]: rot / 2 cosines, then rot / 2 sines.  rot: a multiple of 16 up to s
+ *   adjacent    0: features i and i + rot / 2 of a head are the pair i, else features 2 i and 2 i + 1; those from rot on stay
+ *   q_out       device bf16 [t, n, s]: the turned Q.  It may be q itself where q_stride = n s
+ *   k_out       device bf16 [t, n_kv, s] or NULL: the turned K, as a prefill's attention takes it.  It may be k itself where
+ *               kv_stride = n_kv s
+ * A pair (a, b) becomes (a cos - b sin, b cos + a sin): each product and each sum rounded to fp32, the result to bf16; a cache
+ * of 8 bits holds that bf16 row.  No two sequences of a call may write into one page (the debug validation checks it, and that
+ * the pages written to are there and the positions inside the table). */
+ds_status ds_kv_append_rotary(ds_ctx *ctx, const void *q, int32_t q_stride, const void *k, const void *v, int32_t kv_stride,
+                              const int32_t *cu_rows, int32_t B, int32_t t, const int32_t *ctx_lens,
+                              const int32_t *positions, const float *table, int32_t n_pos, int32_t rot, int32_t adjacent,
+                              const int32_t *block_tables, int32_t max_blocks_per_seq, void *k_cache, void *v_cache,
+                              void *k_scale, void *v_scale, int32_t num_blocks, int32_t kv_type, void *q_out, void *k_out,
+                              void *stream);
+
 /* ---- per-kernel timing (HIP events around every launch; off by default) ---- */
 enum {
   DS_K_LAYERNORM = 0, DS_K_GEMM = 1, DS_K_PREFILL_ATTN = 2, DS_K_KV_MIGRATE = 3,

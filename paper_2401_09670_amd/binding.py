@@ -36,7 +36,7 @@ EXPORTS = ("ds_create", "ds_destroy", "ds_last_error", "ds_set_validate", "ds_pr
            "ds_embed", "ds_next_token_workspace_bytes", "ds_next_token", "ds_profile_enable", "ds_profile_collect",
            "ds_decode_quant_workspace_bytes", "ds_decode_shared_workspace_bytes", "ds_kv_migrate_quant",
            "ds_kv_read_quant", "ds_kv_append_quant", "ds_decode_attention_quant", "ds_decode_attention_shared",
-           "ds_decode_step_quant", "ds_decode_step_shared")
+           "ds_decode_step_quant", "ds_decode_step_shared", "ds_kv_append_rotary")
 
 
 class DsError(RuntimeError):
@@ -61,7 +61,7 @@ class LayerWeights(ctypes.Structure):
 TENSOR_CALLS = ("ds_prefill", "ds_kv_migrate", "ds_decode_step", "ds_decode_step_static", "ds_layernorm", "ds_linear",
                 "ds_prefill_attention", "ds_decode_attention", "ds_embed", "ds_next_token", "ds_kv_migrate_quant",
                 "ds_kv_read_quant", "ds_kv_append_quant", "ds_decode_attention_quant", "ds_decode_attention_shared",
-                "ds_decode_step_quant", "ds_decode_step_shared")
+                "ds_decode_step_quant", "ds_decode_step_shared", "ds_kv_append_rotary")
 
 _lib = None
 
@@ -142,7 +142,8 @@ def load_library() -> ctypes.CDLL:
             ("ds_decode_attention_shared", [vp, *groups, vp, vp, i32, i32, i32, *cache, vp, vp, sz]),
             ("ds_decode_step_quant", [ctypes.POINTER(LayerWeights), vp, vp, vp, i32, i32, i32, *cache, vp, vp, sz]),
             ("ds_decode_step_shared", [ctypes.POINTER(LayerWeights), vp, *groups, vp, vp, i32, i32, i32, *cache, vp, vp,
-                                       sz])):
+                                       sz]),
+            ("ds_kv_append_rotary", [vp, i32, vp, vp, i32, vp, i32, i32, vp, vp, vp, i32, i32, i32, vp, i32, *cache, vp, vp])):
         getattr(lib, name).argtypes = [vp, *args, vp]
         getattr(lib, name).restype = ctypes.c_int
     lib.ds_profile_enable.argtypes = [vp, i32]
@@ -330,6 +331,15 @@ class Context:
             self.handle.value, weights, x, cu_groups, n_groups, max_group_rows, prefix_lens, prefix_tables,
             max_prefix_blocks, max_prefix_len, ctx_lens, block_tables, B, max_blocks_per_seq, max_ctx, k_cache, v_cache,
             k_scale, v_scale, num_blocks, kv_type, y, workspace, workspace, _stream()))
+
+    # ---- positions by rotation, attention through a window ----
+    def ds_kv_append_rotary(self, q, q_stride: int, k, v, kv_stride: int, cu_rows, B: int, t: int, ctx_lens, positions,
+                            table, n_pos: int, rot: int, adjacent: int, block_tables, max_blocks_per_seq: int, k_cache,
+                            v_cache, k_scale, v_scale, num_blocks: int, kv_type: int, q_out, k_out=None):
+        self._check(self.calls.ds_kv_append_rotary(
+            self.handle.value, q, q_stride, k, v, kv_stride, cu_rows, B, t, ctx_lens, positions, table, n_pos, rot, adjacent,
+            block_tables, max_blocks_per_seq, k_cache, v_cache, k_scale, v_scale, num_blocks, kv_type, q_out, k_out,
+            _stream()))
 
     # ---- the two ends of the token loop ----
     def ds_embed(self, token_ids, positions, tok_emb, vocab: int, pos_emb, n_pos: int, rows: int, x):

@@ -1050,6 +1050,51 @@ static ds_status validate_page_owners(ds_ctx* ctx, const char* who, const StepCa
   return DS_OK;
 }
 
+// New rows of sequences: they are all there, the pages they are written into are named and each is written by one sequence, and
+// their positions lie in the table.
+static ds_status validate_new_rows(ds_ctx* ctx, const char* who, const ds::RotaryRows& r, int32_t num_blocks, hipStream_t s) {
+  std::vector<int32_t> cu, before, bt, at;
+  if (r.cu_rows) {
+    if (ds_status st = fetch_i32(ctx, r.cu_rows, (size_t)r.B + 1, s, cu)) return st;
+    if (cu[0] != 0 || cu[r.B] > r.t)
+      return fail(ctx, DS_ERR_BOUNDS, "%s: cu_rows goes from %d to %d, must go from 0 to t = %d or less", who, cu[0], cu[r.B], r.t);
+    for (int i = 0; i < r.B; ++i)
+      if (cu[i + 1] < cu[i]) return fail(ctx, DS_ERR_BOUNDS, "%s: cu_rows decreases at sequence %d", who, i);
+  }
+  if (ds_status st = fetch_i32(ctx, r.ctx_lens, (size_t)r.B, s, before)) return st;
+  if (ds_status st = fetch_i32(ctx, r.block_tables, (size_t)r.B * r.max_blocks, s, bt)) return st;
+  if (r.positions)
+    if (ds_status st = fetch_i32(ctx, r.positions, (size_t)r.t, s, at)) return st;
+  const int page = ctx->cfg.block_size;
+  try {
+    std::unordered_map<int32_t, int> writer;
+    for (int i = 0; i < r.B; ++i) {
+      const long first = r.cu_rows ? cu[i] : i, count = r.cu_rows ? (long)cu[i + 1] - cu[i] : 1;
+      if (before[i] < -1) return fail(ctx, DS_ERR_BOUNDS, "%s: sequence %d has %d tokens", who, i, before[i]);
+      if (before[i] < 0 || count == 0) continue;
+      const long end = before[i] + count;
+      if (end > (long)r.max_blocks * page)
+        return fail(ctx, DS_ERR_BOUNDS, "%s: sequence %d needs %ld tokens' pages > max_blocks_per_seq %d", who, i, end, r.max_blocks);
+      for (long j = before[i] / page; j <= (end - 1) / page; ++j) {
+        const int32_t id = bt[(size_t)i * r.max_blocks + j];
+        if (id < 0 || id >= num_blocks)
+          return fail(ctx, DS_ERR_BOUNDS, "%s: block_tables[%d][%ld] = %d outside [0, %d)", who, i, j, id, num_blocks);
+        const auto had = writer.emplace(id, i);
+        if (!had.second)
+          return fail(ctx, DS_ERR_BOUNDS, "%s: sequences %d and %d both write into block %d", who, had.first->second, i, id);
+      }
+      for (long j = 0; j < count; ++j) {
+        const long p = r.positions ? at[first + j] : before[i] + j;
+        if (p < 0 || p >= r.n_pos)
+          return fail(ctx, DS_ERR_BOUNDS, "%s: row %ld has position %ld outside [0, %d)", who, first + j, p, r.n_pos);
+      }
+    }
+  } catch (const std::exception&) {
+    return fail(ctx, DS_ERR_INVALID_ARG, "%s: no memory for the pages of %d sequences", who, r.B);
+  }
+  return DS_OK;
+}
+
 // Every decode-step entry point: `workspace` is the caller's buffer, or null for the static scratch array
 // of the current device (then the step must fit DS_STATIC_SCRATCH_BYTES).
 static ds_status decode_step(ds_ctx* ctx, const ds_layer_weights* w, const void* x, const int32_t* ctx_lens,
@@ -1389,6 +1434,44 @@ ds_status ds_decode_step_shared(ds_ctx* ctx, const ds_layer_weights* w, const vo
                         n_groups, max_group_rows, max_prefix_blocks, max_prefix_len};
   return decode_step(ctx, w, x, ctx_lens, block_tables, B, max_blocks_per_seq, max_ctx, cache, num_blocks, y, workspace,
                      workspace_bytes, false, stream, who);
+}
+
+// ---- positions by rotation, attention through a window ----
+
+ds_status ds_kv_append_rotary(ds_ctx* ctx, const void* q, int32_t q_stride, const void* k, const void* v, int32_t kv_stride,
+                              const int32_t* cu_rows, int32_t B, int32_t t, const int32_t* ctx_lens,
+                              const int32_t* positions, const float* table, int32_t n_pos, int32_t rot, int32_t adjacent,
+                              const int32_t* block_tables, int32_t max_blocks_per_seq, void* k_cache, void* v_cache,
+                              void* k_scale, void* v_scale, int32_t num_blocks, int32_t kv_type, void* q_out, void* k_out,
+                              void* stream) {
+  const char* who = "ds_kv_append_rotary";
+  if (!ctx) return DS_ERR_INVALID_ARG;
+  const ds_model_cfg& c = ctx->cfg;
+  if (!q || !k || !v || !ctx_lens || !table || !block_tables || !q_out)
+    return fail(ctx, DS_ERR_INVALID_ARG, "%s: NULL pointer", who);
+  if (B <= 0 || t <= 0 || max_blocks_per_seq <= 0 || n_pos <= 0 || (!cu_rows && t != B))
+    return fail(ctx, DS_ERR_INVALID_ARG, "%s: non-positive size, or rows without cu_rows that are not one a sequence", who);
+  if (q_stride < c.hidden || kv_stride < kv_width(c) || q_stride % 8 != 0 || kv_stride % 8 != 0)
+    return fail(ctx, DS_ERR_INVALID_ARG, "%s: a row stride that is below the row's width or no multiple of 8", who);
+  if (rot <= 0 || rot % 16 != 0 || rot > c.head_dim)
+    return fail(ctx, DS_ERR_UNSUPPORTED, "%s: rot %d is no multiple of 16 up to the head size", who, rot);
+  if ((q_out == q && q_stride != c.hidden) || (k_out == k && kv_stride != kv_width(c)))
+    return fail(ctx, DS_ERR_INVALID_ARG, "%s: in place only where rows follow each other", who);
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(table) || !aligned16(q_out) || !aligned16(k_out))
+    return fail(ctx, DS_ERR_INVALID_ARG, "%s: pointers must be 16-byte aligned", who);
+  if (ds_status st = check_cache(ctx, who, k_cache, v_cache, k_scale, v_scale, num_blocks, kv_type, true)) return st;
+  const ds::RotaryRows rows{(const uint16_t*)q, (const uint16_t*)k, (const uint16_t*)v, q_stride, kv_stride, cu_rows, B, t,
+                            ctx_lens, positions, table, n_pos, rot, adjacent != 0, block_tables, max_blocks_per_seq,
+                            (uint16_t*)q_out, (uint16_t*)k_out};
+  if (!ds::rotary_fits(rows, kv_type, c.n_heads, c.n_kv_heads))
+    return fail(ctx, DS_ERR_INVALID_ARG, "%s: more rows than a launch can have", who);
+  if (ds_status st = ensure_device(ctx)) return st;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (ctx->validate)
+    if (ds_status st = validate_new_rows(ctx, who, rows, num_blocks, s)) return st;
+  const ds::KvCache cache{k_cache, v_cache, k_scale, v_scale, kv_type};
+  DS_LAUNCH(ctx, s, DS_K_KV_APPEND, ds::launch_kv_append_rotary(rows, cache, c.n_heads, c.n_kv_heads, c.head_dim, s));
+  return DS_OK;
 }
 
 ds_status ds_profile_enable(ds_ctx* ctx, int32_t on) {

@@ -193,6 +193,24 @@ hipError_t launch_kv_append_quant(const void* k_new, const void* v_new, int row_
                                   const int32_t* block_tables, int B, int max_blocks, const KvCache& cache, int n_heads,
                                   int head_dim, hipStream_t stream);
 
+// New rows with their rotation: Q [t, n, s] (row stride q_stride) -> q_out; K and V (row stride kv_stride) -> the cache, and K
+// -> k_out where that is given.  cu_rows null: row i is sequence i's one new row.  positions null: those in the cache.
+struct RotaryRows {
+  const uint16_t *q, *k, *v;
+  int q_stride, kv_stride;
+  const int32_t* cu_rows;
+  int B, t;
+  const int32_t *ctx_lens, *positions;
+  const float* table;  // [n_pos, rot]: rot / 2 cosines, rot / 2 sines
+  int n_pos, rot, adjacent;
+  const int32_t* block_tables;
+  int max_blocks;
+  uint16_t *q_out, *k_out;
+};
+bool rotary_fits(const RotaryRows& r, int kv_type, int n_heads, int n_kv_heads);  // into a launch
+hipError_t launch_kv_append_rotary(const RotaryRows& r, const KvCache& cache, int n_heads, int n_kv_heads, int head_dim,
+                                   hipStream_t stream);
+
 // One query per (sequence, head) over pages, on the matrix cores whatever the number of heads: over the sequence's own
 // pages, and before them, where n_groups > 0, over the prefix of its group (rows [cu_groups[i], cu_groups[i + 1])).
 struct TilePlan {

@@ -10,46 +10,6 @@ namespace ds {
 
 constexpr int kQuantThreads = 256, kQuantWaves = 4;
 
-// The 16 tokens of a (page, head) in a wave: lane (g = lane / 16, c = lane % 16) has tokens 4 g .. 4 g + 3, and of each of
-// them the E = s / 16 numbers E c .. E c + E - 1.
-template <int HD>
-struct PageRows {
-  static constexpr int E = HD / 16;       // numbers of a token in a lane: 8 or 4
-  static constexpr int W = E / 4;         // words of 4 values
-  uint32_t w[4][2 * W];                   // bf16 pairs
-
-  __device__ __forceinline__ void load(const uint16_t* src, size_t row_stride, int g, int c, int last) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {  // (tokens behind the end: the last one again)
-      const uint16_t* p = src + (size_t)min(4 * g + i, last) * row_stride + E * c;
-      if constexpr (HD == 128) {
-        const u32x4 v = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
-#pragma unroll
-        for (int j = 0; j < 4; ++j) w[i][j] = v[j];
-      } else {
-        const u32x2 v = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(p));
-        w[i][0] = v[0];
-        w[i][1] = v[1];
-      }
-    }
-  }
-};
-
-struct BitsMax {  // of bit patterns without a sign, carried as floats
-  __device__ __forceinline__ float operator()(float a, float b) const {
-    return __uint_as_float(max(__float_as_uint(a), __float_as_uint(b)));
-  }
-};
-
-// Largest magnitude of the row whose numbers the 16 lanes of a group have, as bf16 bits.
-template <int N>
-__device__ __forceinline__ uint32_t row_amax(const uint32_t (&w)[N]) {
-  uint32_t a = 0;
-#pragma unroll
-  for (int j = 0; j < N; ++j) a = max(a, max(w[j] & 0x7fffu, (w[j] >> 16) & 0x7fffu));
-  return __float_as_uint(within_group<16>(__uint_as_float(a), BitsMax()));
-}
-
 // A wave takes one page of one head of K or of V; a workgroup 4 heads, and those of a page follow each other.
 //   Sequence i has the places cu[i] / 16 + i and on, as many as it has pages or more, and there are t / 16 + B of them in all:
 // next to none is for nothing, however unlike the lengths are.  (A grid of the longest sequence's pages times sequences took 8 us
@@ -117,19 +77,8 @@ __global__ __launch_bounds__(kQuantThreads) void kv_migrate_quant_kernel(
     }
     return;
   }
-  // V: first the 4 tokens of a feature into one word, then the 4 words of a feature into one lane
-#pragma unroll
-  for (int j = 0; j < W; ++j) turn_bytes(out[j]);  // out[j][e]: feature E c + 4 j + e, tokens 4 g .. 4 g + 3
   uint32_t f[E];
-#pragma unroll
-  for (int e = 0; e < E; ++e) f[e] = out[e / 4][e % 4];
-#pragma unroll
-  for (int e = 0; e < E / 2; ++e) swap32(f[e], f[e + E / 2]);
-#pragma unroll
-  for (int e = 0; e < W; ++e) {
-    swap16(f[e], f[e + W]);
-    swap16(f[e + E / 2], f[e + E / 2 + W]);
-  }
+  turn_page<HD>(out, f);
   // tokens 0..3, 4..7, 8..11, 12..15 of feature E c + W g + e
   uint8_t* dst = v_cache + page * (kKvPage * HD) + (E * c + W * g) * kKvPage;
 #pragma unroll
