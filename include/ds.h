@@ -384,6 +384,19 @@ ds_status ds_kv_append_rotary(ds_ctx *ctx, const void *q, int32_t q_stride, cons
                               void *k_scale, void *v_scale, int32_t num_blocks, int32_t kv_type, void *q_out, void *k_out,
                               void *stream);
 
+/* ds_decode_attention over the last `window` (>= 1) tokens of each sequence and its first `sinks` (>= 0): with kv_lens[i] = L
+ * the query, which is token L - 1's, sees token j if L - 1 - j < window or j < sinks.  Any kv_type, on its conventions
+ * (roundings, scores beyond fp32's range, kv_lens[i] = 0: output 0).  What it does not see does not count, whatever it holds, and
+ * entries of block_tables whose 16 tokens are all hidden are not read: they may be -1, their pages given back.
+ * Workspace: ds_decode_window_workspace_bytes(B, max_kv_len, window, sinks) (0: none), which serves smaller batches, lengths,
+ * windows and sinks too. */
+size_t ds_decode_window_workspace_bytes(const ds_ctx *ctx, int32_t max_batch, int32_t max_ctx, int32_t window, int32_t sinks);
+ds_status ds_decode_attention_window(ds_ctx *ctx, const void *q, const int32_t *kv_lens, const int32_t *block_tables,
+                                     int32_t B, int32_t max_blocks_per_seq, int32_t max_kv_len, int32_t window, int32_t sinks,
+                                     const void *k_cache, const void *v_cache, const void *k_scale, const void *v_scale,
+                                     int32_t num_blocks, int32_t kv_type, void *o, void *workspace, size_t workspace_bytes,
+                                     void *stream);
+
 /* ---- per-kernel timing (HIP events around every launch; off by default) ---- */
 enum {
   DS_K_LAYERNORM = 0, DS_K_GEMM = 1, DS_K_PREFILL_ATTN = 2, DS_K_KV_MIGRATE = 3,

@@ -36,7 +36,8 @@ EXPORTS = ("ds_create", "ds_destroy", "ds_last_error", "ds_set_validate", "ds_pr
            "ds_embed", "ds_next_token_workspace_bytes", "ds_next_token", "ds_profile_enable", "ds_profile_collect",
            "ds_decode_quant_workspace_bytes", "ds_decode_shared_workspace_bytes", "ds_kv_migrate_quant",
            "ds_kv_read_quant", "ds_kv_append_quant", "ds_decode_attention_quant", "ds_decode_attention_shared",
-           "ds_decode_step_quant", "ds_decode_step_shared", "ds_kv_append_rotary")
+           "ds_decode_step_quant", "ds_decode_step_shared", "ds_kv_append_rotary",
+           "ds_decode_window_workspace_bytes", "ds_decode_attention_window")
 
 
 class DsError(RuntimeError):
@@ -61,7 +62,7 @@ class LayerWeights(ctypes.Structure):
 TENSOR_CALLS = ("ds_prefill", "ds_kv_migrate", "ds_decode_step", "ds_decode_step_static", "ds_layernorm", "ds_linear",
                 "ds_prefill_attention", "ds_decode_attention", "ds_embed", "ds_next_token", "ds_kv_migrate_quant",
                 "ds_kv_read_quant", "ds_kv_append_quant", "ds_decode_attention_quant", "ds_decode_attention_shared",
-                "ds_decode_step_quant", "ds_decode_step_shared", "ds_kv_append_rotary")
+                "ds_decode_step_quant", "ds_decode_step_shared", "ds_kv_append_rotary", "ds_decode_attention_window")
 
 _lib = None
 
@@ -134,6 +135,8 @@ def load_library() -> ctypes.CDLL:
     lib.ds_decode_quant_workspace_bytes.restype = sz
     lib.ds_decode_shared_workspace_bytes.argtypes = [vp, i32, i32, i32]
     lib.ds_decode_shared_workspace_bytes.restype = sz
+    lib.ds_decode_window_workspace_bytes.argtypes = [vp, i32, i32, i32, i32]
+    lib.ds_decode_window_workspace_bytes.restype = sz
     for name, args in (
             ("ds_kv_migrate_quant", [vp, vp, vp, i32, i32, i32, vp, i32, *cache]),
             ("ds_kv_read_quant", [vp, i32, i32, i32, vp, i32, *cache, vp, vp]),
@@ -143,7 +146,8 @@ def load_library() -> ctypes.CDLL:
             ("ds_decode_step_quant", [ctypes.POINTER(LayerWeights), vp, vp, vp, i32, i32, i32, *cache, vp, vp, sz]),
             ("ds_decode_step_shared", [ctypes.POINTER(LayerWeights), vp, *groups, vp, vp, i32, i32, i32, *cache, vp, vp,
                                        sz]),
-            ("ds_kv_append_rotary", [vp, i32, vp, vp, i32, vp, i32, i32, vp, vp, vp, i32, i32, i32, vp, i32, *cache, vp, vp])):
+            ("ds_kv_append_rotary", [vp, i32, vp, vp, i32, vp, i32, i32, vp, vp, vp, i32, i32, i32, vp, i32, *cache, vp, vp]),
+            ("ds_decode_attention_window", [vp, vp, vp, i32, i32, i32, i32, i32, *cache, vp, vp, sz])):
         getattr(lib, name).argtypes = [vp, *args, vp]
         getattr(lib, name).restype = ctypes.c_int
     lib.ds_profile_enable.argtypes = [vp, i32]
@@ -340,6 +344,16 @@ class Context:
             self.handle.value, q, q_stride, k, v, kv_stride, cu_rows, B, t, ctx_lens, positions, table, n_pos, rot, adjacent,
             block_tables, max_blocks_per_seq, k_cache, v_cache, k_scale, v_scale, num_blocks, kv_type, q_out, k_out,
             _stream()))
+
+    def ds_decode_window_workspace_bytes(self, max_batch: int, max_ctx: int, window: int, sinks: int) -> int:
+        return self.lib.ds_decode_window_workspace_bytes(self.handle, max_batch, max_ctx, window, sinks)
+
+    def ds_decode_attention_window(self, q, kv_lens, block_tables, B: int, max_blocks_per_seq: int, max_kv_len: int,
+                                   window: int, sinks: int, k_cache, v_cache, k_scale, v_scale, num_blocks: int,
+                                   kv_type: int, o, workspace=None):
+        self._check(self.calls.ds_decode_attention_window(
+            self.handle.value, q, kv_lens, block_tables, B, max_blocks_per_seq, max_kv_len, window, sinks, k_cache, v_cache,
+            k_scale, v_scale, num_blocks, kv_type, o, workspace, workspace, _stream()))
 
     # ---- the two ends of the token loop ----
     def ds_embed(self, token_ids, positions, tok_emb, vocab: int, pos_emb, n_pos: int, rows: int, x):

@@ -65,6 +65,7 @@ struct TileArgs {
   const uint16_t *k_scale, *v_scale;
   int n_heads, n_kv_heads;
   int n_states;      // of a (row, head); 1: o is written
+  int window, sinks; // (WINDOW)
   float scale_log2e;
   uint16_t* o;
   float* partial;    // [row][head][state][output[HD], max, sum, states of the own pages (in the first of them), -]
@@ -105,7 +106,46 @@ struct TileWork {
   bool whole;  // there is nothing else of the row and head: the result is written, no state
   int step;  // narrow: pages from one chunk of a wave to its next
   const int32_t* bt;
+  int sink_pages, sink_len, gap, low;  // (WINDOW)
 };
+
+// Through a window a sequence is the pages that have something to see: those of its first `sinks` tokens, then those of its last
+// `window`, numbered from 0 as if nothing lay between, and where the first tokens reach the window, all of them.  A page that
+// holds the end of the one and the beginning of the other comes twice, each time with its own part of the tokens.
+struct Seen {
+  int sink_pages, sink_len;
+  int gap;  // pages left out before page sink_pages (-1: one comes twice)
+  int low;  // tokens of that page that are hidden
+};
+__device__ __forceinline__ Seen seen_of(int len, int window, int sinks) {
+  const int hidden = max(len - window, 0);  // tokens before the window
+  Seen v{0, 0, 0, 0};
+  if (sinks < hidden) {
+    v.sink_pages = (sinks + kKvPage - 1) / kKvPage;
+    v.sink_len = sinks;
+    v.gap = hidden / kKvPage - v.sink_pages;
+    v.low = hidden % kKvPage;
+  }
+  return v;
+}
+// Page p of a sequence in its block table; the first slot of it that is seen and the one behind the last (up to 16, or below 0).
+template <bool WINDOW>
+__device__ __forceinline__ int table_entry(const TileWork& w, int p) {
+  return WINDOW && p >= w.sink_pages ? p + w.gap : p;
+}
+template <bool WINDOW>
+__device__ __forceinline__ int slots_from(const TileWork& w, int p) {
+  return WINDOW && p == w.sink_pages ? w.low : 0;
+}
+template <bool WINDOW>
+__device__ __forceinline__ int slots_to(const TileWork& w, int p) {
+  return (WINDOW && p < w.sink_pages ? w.sink_len : w.len) - p * kKvPage;
+}
+// Ones in the bytes n0 .. n1 - 1 of a word (of 4).
+__device__ __forceinline__ uint32_t bytes_of(int n0, int n1) {
+  const uint32_t below = n0 >= 4 ? 0xffffffffu : (1u << (8 * max(n0, 0))) - 1u;
+  return (n1 >= 4 ? 0xffffffffu : (1u << (8 * max(n1, 0))) - 1u) & ~below;
+}
 
 // The r-th longest (by pages, then by number) of up to 64 sequences, one a lane (pages < 0: none): a lane's number.
 __device__ __forceinline__ int ranked(int pages, int r, int bits) {
@@ -204,7 +244,7 @@ struct TileLds {
 //   K is asked for one chunk ahead when this one's scores are made, V when its output is: 16 registers each.  (A chunk of 64
 // keys has twice those and half the waves: 40 heads, 64 sequences of 545 tokens 76 us, of 32 keys 71.)  Loads that no cache
 // keeps: 71 -> 66 there, but one sequence of 700 tokens, which the caches do keep from step to step, 8.6 -> 10.8: kOnceBytes.
-template <int HD, int T, bool ONCE>
+template <int HD, int T, bool ONCE, bool WINDOW>
 __device__ __forceinline__ void narrow_quant(const TileArgs& a, const TileWork& w, const u32x4 (&qf)[HD / 32],
                                              floatx4 (&acc)[HD / 16], float& m_run, float& l_run) {
   constexpr int KL = HD / 64, VL = HD / 32;  // 16-byte loads of a key, of a chunk's V, per lane
@@ -213,8 +253,8 @@ __device__ __forceinline__ void narrow_quant(const TileArgs& a, const TileWork& 
   const uint8_t* vc = static_cast<const uint8_t*>(a.v);
   int kid = 0, vid = 0;
   auto ids = [&](int p) {  // pages of the lane as a row of K and as a column of V (behind the last: the last, without keys)
-    kid = w.bt[min(p + (hl >> 3), w.hi - 1)];
-    vid = w.bt[min(p + (g >> 1), w.hi - 1)];
+    kid = w.bt[table_entry<WINDOW>(w, min(p + (hl >> 3), w.hi - 1))];
+    vid = w.bt[table_entry<WINDOW>(w, min(p + (g >> 1), w.hi - 1))];
   };
   u32x4 kr[2][KL], vr[VL];
   uint16_t ksr, vsr;
@@ -243,8 +283,15 @@ __device__ __forceinline__ void narrow_quant(const TileArgs& a, const TileWork& 
     ids(pg + w.step);
   }
   for (; pg < w.hi; pg += w.step) {
-    // keys of the lane's half page
-    const int there = pg + (g >> 1) < w.hi ? min(w.len - (pg + (g >> 1)) * kKvPage - 8 * (g & 1), 8) : 0;
+    // Keys of the lane's half page.  WINDOW: from the first that is seen, both worked out anew wherever they are used, which is
+    // in chunks that are not whole alone: kept over the chunk they are one register more than there is.
+    const int there = !WINDOW && pg + (g >> 1) < w.hi ? min(w.len - (pg + (g >> 1)) * kKvPage - 8 * (g & 1), 8) : 0;
+    const bool partial = WINDOW && (pg <= w.sink_pages || pg + 1 >= w.hi || w.len - (pg + 1) * kKvPage < kKvPage);
+    auto keys_of = [&](int& n0, int& n1) {
+      const int of = lane_anew() >> 4, page = pg + (of >> 1);
+      n0 = slots_from<WINDOW>(w, page) - 8 * (of & 1);
+      n1 = page < w.hi ? slots_to<WINDOW>(w, page) - 8 * (of & 1) : 0;
+    };
     floatx4 s[2] = {floatx4{0.f, 0.f, 0.f, 0.f}, floatx4{0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
     for (int c = 0; c < KL; ++c)
@@ -253,13 +300,22 @@ __device__ __forceinline__ void narrow_quant(const TileArgs& a, const TileWork& 
 #pragma unroll
         for (int t = 0; t < 2; ++t)
           s[t] = mfma(values8<T>(kr[t][c][2 * h], kr[t][c][2 * h + 1]), qf[2 * c + h], s[t]);
-    const float ks = bf16_lo(ksr) * a.scale_log2e, vs = (hl & 7) < there ? bf16_lo(vsr) : 0.f;
+    const float ks = bf16_lo(ksr) * a.scale_log2e;
+    float vs = WINDOW || (hl & 7) < there ? bf16_lo(vsr) : 0.f;
     const bool more = pg + w.step < w.hi;
     if (more) fetch_k();
     each(std::make_integer_sequence<int, 8>{}, [&](auto j) {
       const float x = s[j() / 4][j() % 4] * row_lane<j()>(ks);
-      s[j() / 4][j() % 4] = j() < there ? x : -INFINITY;  // (whatever the slot holds)
+      s[j() / 4][j() % 4] = WINDOW || j() < there ? x : -INFINITY;  // (whatever the slot holds)
     });
+    if (WINDOW && partial) {
+      int n0, n1;
+      keys_of(n0, n1);
+      vs = (hl & 7) >= n0 && (hl & 7) < n1 ? vs : 0.f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (j < n0 || j >= n1) s[j / 4][j % 4] = -INFINITY;
+    }
     online_softmax(s, acc, m_run, l_run);
     each(std::make_integer_sequence<int, 8>{}, [&](auto j) { s[j() / 4][j() % 4] *= row_lane<j()>(vs); });
     const Probabilities pf = probabilities(s);
@@ -274,7 +330,15 @@ __device__ __forceinline__ void narrow_quant(const TileArgs& a, const TileWork& 
       vr[i] = u32x4{x[0], x[1], x[2], x[3]};
     }
     // slots behind the end may hold NaN, and 0 * NaN is NaN
-    if (__builtin_amdgcn_ballot_w64(there < 8) != 0) {
+    if constexpr (WINDOW) {  // (and hidden ones too)
+      if (partial) {
+        int n0, n1;
+        keys_of(n0, n1);
+        const uint32_t keep0 = bytes_of(n0, n1), keep1 = bytes_of(n0 - 4, n1 - 4);
+#pragma unroll
+        for (int i = 0; i < VL; ++i) vr[i] &= u32x4{keep0, keep1, keep0, keep1};
+      }
+    } else if (__builtin_amdgcn_ballot_w64(there < 8) != 0) {
       const uint32_t keep0 = there >= 4 ? 0xffffffffu : (1u << (8 * max(there, 0))) - 1u;
       const uint32_t keep1 = there >= 8 ? 0xffffffffu : (1u << (8 * max(there - 4, 0))) - 1u;
 #pragma unroll
@@ -296,7 +360,7 @@ __device__ __forceinline__ void narrow_quant(const TileArgs& a, const TileWork& 
 }
 
 // bf16: row i of score tile t is key i of page t; V goes through the wave's own LDS.
-template <int HD, bool ONCE>
+template <int HD, bool ONCE, bool WINDOW>
 __device__ __forceinline__ void narrow_bf16(const TileArgs& a, const TileWork& w, const u32x4 (&qf)[HD / 32],
                                             floatx4 (&acc)[HD / 16], float& m_run, float& l_run, unsigned char* smem) {
   constexpr int CPR = HD / 8, RPL = 64 / CPR;  // 16-byte pieces of a row, rows of a load
@@ -310,7 +374,7 @@ __device__ __forceinline__ void narrow_bf16(const TileArgs& a, const TileWork& w
   int id[2] = {0, 0};
   auto ids = [&](int p) {
 #pragma unroll
-    for (int u = 0; u < 2; ++u) id[u] = w.bt[min(p + u, w.hi - 1)];
+    for (int u = 0; u < 2; ++u) id[u] = w.bt[table_entry<WINDOW>(w, min(p + u, w.hi - 1))];
   };
   u32x4 kr[2][HD / 32], vr[2][NL];
   size_t at[2];
@@ -336,9 +400,12 @@ __device__ __forceinline__ void narrow_bf16(const TileArgs& a, const TileWork& w
     ids(pg + w.step);
   }
   for (; pg < w.hi; pg += w.step) {
-    int there[2];
+    int there[2], hidden[2];
 #pragma unroll
-    for (int u = 0; u < 2; ++u) there[u] = pg + u < w.hi ? min(w.len - (pg + u) * kKvPage, kKvPage) : 0;
+    for (int u = 0; u < 2; ++u) {
+      there[u] = pg + u < w.hi ? min(slots_to<WINDOW>(w, pg + u), kKvPage) : 0;
+      hidden[u] = slots_from<WINDOW>(w, pg + u);
+    }
     floatx4 s[2] = {floatx4{0.f, 0.f, 0.f, 0.f}, floatx4{0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
     for (int st = 0; st < HD / 32; ++st)
@@ -346,14 +413,14 @@ __device__ __forceinline__ void narrow_bf16(const TileArgs& a, const TileWork& w
       for (int u = 0; u < 2; ++u) s[u] = mfma(kr[u][st], qf[st], s[u]);
     const bool more = pg + w.step < w.hi;
     if (more) fetch_k();
-    // (rows behind the end as zeros: what is there may be NaN, and 0 * NaN is NaN)
+    // (rows behind the end, or hidden, as zeros: what is there may be NaN, and 0 * NaN is NaN)
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
       for (int i = 0; i < NL; ++i) {
         const int row = RPL * i + vrow;
         *reinterpret_cast<u32x4*>(vst + (u * kKvPage + row) * kVRow<HD> + vcol) =
-            row < there[u] ? vr[u][i] : u32x4{0, 0, 0, 0};
+            row < there[u] && (!WINDOW || row >= hidden[u]) ? vr[u][i] : u32x4{0, 0, 0, 0};
       }
     if (more) {
       fetch_v();
@@ -362,7 +429,8 @@ __device__ __forceinline__ void narrow_bf16(const TileArgs& a, const TileWork& w
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) s[u][r] = 4 * g + r < there[u] ? s[u][r] * a.scale_log2e : -INFINITY;
+      for (int r = 0; r < 4; ++r)
+        s[u][r] = 4 * g + r < there[u] && (!WINDOW || 4 * g + r >= hidden[u]) ? s[u][r] * a.scale_log2e : -INFINITY;
     online_softmax(s, acc, m_run, l_run);
     const Probabilities pf = probabilities(s);
     __builtin_amdgcn_wave_barrier();  // (a wave's LDS accesses keep their order; the compiler has to keep it too)
@@ -396,7 +464,7 @@ __device__ __forceinline__ int k_swizzle(int row) {
   else return HD == 128 ? (row & 3) | ((row >> 3) & 3) << 2 : ((row >> 1) & 1) | ((row >> 3) & 3) << 1;
 }
 
-template <int HD, int T>
+template <int HD, int T, bool WINDOW>
 __device__ __forceinline__ void wide_tiles(const TileArgs& a, const TileWork& w, const u32x4 (&qf)[HD / 32],
                                            floatx4 (&acc)[HD / 16], float& m_run, float& l_run, bool idle,
                                            unsigned char* smem) {
@@ -418,7 +486,7 @@ __device__ __forceinline__ void wide_tiles(const TileArgs& a, const TileWork& w,
   int id[2] = {0, 0}, pg;
   auto ids = [&](int p) {
 #pragma unroll
-    for (int u = 0; u < 2; ++u) id[u] = w.bt[min(p + 2 * u + odd, w.hi - 1)];
+    for (int u = 0; u < 2; ++u) id[u] = w.bt[table_entry<WINDOW>(w, min(p + 2 * u + odd, w.hi - 1))];
   };
   auto words = [&](uint32_t (&r)[RW], const void* p) {
     if constexpr (RW == 2) {
@@ -453,7 +521,8 @@ __device__ __forceinline__ void wide_tiles(const TileArgs& a, const TileWork& w,
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const int page = 2 * u + odd, row = page * kKvPage + key;
-      const int there = pg + page < w.hi ? min(w.len - (pg + page) * kKvPage, kKvPage) : 0;  // keys of the page
+      const int there = pg + page < w.hi ? min(slots_to<WINDOW>(w, pg + page), kKvPage) : 0;  // keys of the page
+      const int hidden = slots_from<WINDOW>(w, pg + page);                                    // the first of them that is seen
       if constexpr (kQuant) {
 #pragma unroll
         for (int c = 0; c < NCH; ++c)
@@ -464,7 +533,13 @@ __device__ __forceinline__ void wide_tiles(const TileArgs& a, const TileWork& w,
 #pragma unroll
         for (int c = 0; c < NCH; ++c) {
           uint32_t x = vr[u][2 * c], y = vr[u][2 * c + 1];
-          if (there < kKvPage) {  // slots behind the end may hold NaN
+          if constexpr (WINDOW) {  // (and hidden ones too)
+            if (there < kKvPage || hidden > 0) {
+              const int n0 = hidden - t0 - 8 * c, n1 = there - t0 - 8 * c;
+              x &= bytes_of(n0, n1);
+              y &= bytes_of(n0 - 4, n1 - 4);
+            }
+          } else if (there < kKvPage) {  // slots behind the end may hold NaN
             const int n = there - t0 - 8 * c;
             x = n >= 4 ? x : n > 0 ? x & ((1u << (8 * n)) - 1u) : 0;
             y = n >= 8 ? y : n > 4 ? y & ((1u << (8 * (n - 4))) - 1u) : 0;
@@ -474,7 +549,7 @@ __device__ __forceinline__ void wide_tiles(const TileArgs& a, const TileWork& w,
         if (at < 32) {
           const float f = bf16_lo(scale[u]);
           sc[(at < 16 ? 0 : kWideKeys) + page * kKvPage + (at & 15)] =
-              at < 16 ? f * a.scale_log2e : ((at & 15) < there ? f : 0.f);
+              at < 16 ? f * a.scale_log2e : ((at & 15) < there && (!WINDOW || (at & 15) >= hidden) ? f : 0.f);
         }
       } else {
 #pragma unroll
@@ -482,7 +557,7 @@ __device__ __forceinline__ void wide_tiles(const TileArgs& a, const TileWork& w,
           *reinterpret_cast<u32x4*>(kt + row * HD + ((NCH * piece + c) ^ k_swizzle<HD, T>(row)) * 8) =
               u32x4{kr[u][4 * c], kr[u][4 * c + 1], kr[u][4 * c + 2], kr[u][4 * c + 3]};
           *reinterpret_cast<u32x4*>(vt + row * kVRow<HD> + (NCH * piece + c) * 8) =
-              key < there ? u32x4{vr[u][4 * c], vr[u][4 * c + 1], vr[u][4 * c + 2], vr[u][4 * c + 3]} : u32x4{0, 0, 0, 0};
+              key < there && (!WINDOW || key >= hidden) ? u32x4{vr[u][4 * c], vr[u][4 * c + 1], vr[u][4 * c + 2], vr[u][4 * c + 3]} : u32x4{0, 0, 0, 0};
         }
       }
     }
@@ -518,7 +593,17 @@ __device__ __forceinline__ void wide_tiles(const TileArgs& a, const TileWork& w,
       if constexpr (kQuant) s[t] *= *reinterpret_cast<const floatx4*>(sc + 32 * (t / 2) + 8 * g + 4 * (t % 2));
       else s[t] *= a.scale_log2e;
     }
-    if (here < kWideKeys) {
+    if (WINDOW && pg <= w.sink_pages) {  // (a tile may have pages of the first tokens, and where the window begins)
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const int key = 32 * (t / 2) + (kQuant ? 8 * g + 4 * (t % 2) : 16 * (t % 2) + 4 * g), page = pg + key / kKvPage;
+        const int from = slots_from<WINDOW>(w, page) - key % kKvPage;
+        const int to = page < w.hi ? slots_to<WINDOW>(w, page) - key % kKvPage : 0;
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (r < from || r >= to) s[t][r] = -INFINITY;
+      }
+    } else if (here < kWideKeys) {
 #pragma unroll
       for (int t = 0; t < 4; ++t)
 #pragma unroll
@@ -575,7 +660,8 @@ __device__ __forceinline__ void store_columns(const TileArgs& a, const TileWork&
 
 // WIDE: either part may be wide (a part of up to 16 columns is narrow all the same).  ONCE: the rows' own pages are read
 // with loads that no cache keeps.  JOINED: part 0 has no workgroups, a row's take its group's prefix and then its own pages.
-template <int HD, int T, bool WIDE, bool ONCE, bool JOINED>
+// WINDOW: of a row's own pages those that its window and its first tokens are in.
+template <int HD, int T, bool WIDE, bool ONCE, bool JOINED, bool WINDOW = false>
 __global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(WIDE || (JOINED && T == kKvBf16) ? 3 : 4))) void tile_attention_kernel(
     const TileArgs a) {
   constexpr int DB = HD / 16, kSteps = HD / 32, kState = HD + kStatePad;
@@ -605,13 +691,23 @@ __global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(WI
     // Longest first among every n-th sequence, so that no long one starts among the last and ends the launch by itself.
     const int n = (p.groups + 63) / 64, other = group % n + n * lane;
     const int len = other < p.groups ? max(p.lens[other] + p.len_add, 0) : -2 * kKvPage;
-    const int at = ranked(min((len + kKvPage - 1) / kKvPage, p.max_pages), group / n, 32 - __builtin_clz(p.max_pages));
+    int seen = (len + kKvPage - 1) / kKvPage;
+    if constexpr (WINDOW) seen -= seen_of(min(len, p.max_len), a.window, a.sinks).gap;
+    const int at = ranked(min(seen, p.max_pages), group / n, 32 - __builtin_clz(p.max_pages));
     group = group % n + n * at;
     w.len = __builtin_amdgcn_readlane(len, at);
   } else {
     w.len = p.lens[group] + p.len_add;
   }
   w.len = min(w.len, p.max_len);
+  if constexpr (WINDOW) {
+    const Seen v = seen_of(w.len, a.window, a.sinks);
+    w.sink_pages = v.sink_pages;
+    w.sink_len = v.sink_len;
+    w.gap = v.gap;
+    w.low = v.low;
+    w.len -= v.gap * kKvPage;
+  }
   w.row0 = p.cu_rows ? p.cu_rows[group] : group;
   w.cols = (p.cu_rows ? p.cu_rows[group + 1] - w.row0 : 1) * G;
   if (w.c0 >= w.cols) return;
@@ -625,7 +721,12 @@ __global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(WI
     float all = 0.f;
     for (int i0 = 0; i0 < p.groups; i0 += 64) {
       const int i = i0 + lane;
-      if (i < p.groups) all += (float)((max(min(p.lens[i] + p.len_add, p.max_len), 0) + kKvPage - 1) / kKvPage);
+      if (i < p.groups) {
+        const int len = max(min(p.lens[i] + p.len_add, p.max_len), 0);
+        int of = (len + kKvPage - 1) / kKvPage;
+        if constexpr (WINDOW) of -= seen_of(len, a.window, a.sinks).gap;
+        all += (float)of;
+      }
     }
     const int fair = (int)fminf(wave_sum(all) * (float)p.blocks_x * (1.f / 384.f), 1e9f);
     const int most = __builtin_amdgcn_readfirstlane(max(fair, kLeastPiece));
@@ -663,7 +764,7 @@ __global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(WI
 
   if constexpr (WIDE) {
     if (wide) {
-      wide_tiles<HD, T>(a, w, qf, acc, m_run, l_run, my_c0 >= w.cols, smem);
+      wide_tiles<HD, T, WINDOW>(a, w, qf, acc, m_run, l_run, my_c0 >= w.cols, smem);
       return store_columns<HD>(a, w, col, acc, m_run, across_groups<16>(l_run, AddOp()));
     }
   }
@@ -683,8 +784,8 @@ __global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(WI
   }
 #pragma unroll 1
   for (int seg = JOINED ? 0 : 1; seg < 2; ++seg) {
-    if constexpr (kQuant) narrow_quant<HD, T, ONCE>(a, w, qf, acc, m_run, l_run);
-    else narrow_bf16<HD, ONCE>(a, w, qf, acc, m_run, l_run, smem);
+    if constexpr (kQuant) narrow_quant<HD, T, ONCE, WINDOW>(a, w, qf, acc, m_run, l_run);
+    else narrow_bf16<HD, ONCE, WINDOW>(a, w, qf, acc, m_run, l_run, smem);
     if constexpr (JOINED) w = next;
   }
   if (p.solo) return store_columns<HD>(a, w, lane_anew() & 15, acc, m_run, across_groups<16>(l_run, AddOp()));
@@ -890,6 +991,13 @@ static bool joined_of(int splits, int B, int n_heads, int n_kv_heads, int head_d
   return again * 0.1e-6 < 2.4 + 0.25e-3 * B * n_heads * (splits + 1.0);
 }
 
+// Tokens of the pages that a window and the first tokens of sequences of up to max_len are in, at most: those of the window
+// begin and end inside a page, and one page may come twice.
+int tile_window_tokens(int max_len, int window, int sinks) {
+  auto pages = [](long tokens) { return (tokens + kKvPage - 1) / kKvPage; };
+  return (int)(kKvPage * std::min(pages(max_len) + 1, pages(sinks) + pages((long)window + kKvPage - 1)));
+}
+
 TilePlan tile_plan(int B, int n_heads, int n_kv_heads, int head_dim, int kv_type, int max_len, int n_groups, int max_prefix) {
   TilePlan p;
   p.own = tile_splits((long)B * n_kv_heads * blocks_of(n_heads / n_kv_heads), max_len);
@@ -935,6 +1043,7 @@ static hipError_t launch_tiles(const TileAttention& t, hipStream_t stream) {
     blocks += (long)p.blocks_x * groups * splits;
   };
   const bool joined = t.plan.joined;
+  const int most_seen = t.window > 0 ? tile_window_tokens(t.max_kv_len, t.window, t.sinks) : t.max_kv_len;
   if (joined) {
     TilePart& p = a.part[0];
     p.cu_rows = t.cu_groups; p.lens = t.prefix_lens; p.tables = t.prefix_tables;
@@ -945,13 +1054,22 @@ static hipError_t launch_tiles(const TileAttention& t, hipStream_t stream) {
     a.first_blocks = (int)blocks;
   }
   part(a.part[1], nullptr, t.kv_lens, t.block_tables, t.kv_len_add, t.max_blocks, t.B, G,
-       joined ? (long)t.max_kv_len + t.max_prefix : t.max_kv_len, joined ? 1 : t.plan.own, joined ? 0 : t.plan.prefix);
+       joined ? (long)t.max_kv_len + t.max_prefix : most_seen, joined ? 1 : t.plan.own, joined ? 0 : t.plan.prefix);
   a.part[1].max_len = t.max_kv_len;
   a.part[1].rank = t.B > 1;
+  a.window = t.window; a.sinks = t.sinks;
   const bool wide = a.part[0].wide || a.part[1].wide;
-  const bool once = (double)t.B * t.max_kv_len * t.n_kv_heads * HD * (T == kKvBf16 ? 4 : 2) > kOnceBytes;
+  const bool once = (double)t.B * most_seen * t.n_kv_heads * HD * (T == kKvBf16 ? 4 : 2) > kOnceBytes;
   const dim3 grid((unsigned)blocks), threads(kTileThreads);
-  if (joined) {
+  if (t.window > 0) {
+    if (T == kKvBf16 || wide) {
+      if (once) hipLaunchKernelGGL((tile_attention_kernel<HD, T, true, true, false, true>), grid, threads, 0, stream, a);
+      else hipLaunchKernelGGL((tile_attention_kernel<HD, T, true, false, false, true>), grid, threads, 0, stream, a);
+    } else if constexpr (T != kKvBf16) {
+      if (once) hipLaunchKernelGGL((tile_attention_kernel<HD, T, false, true, false, true>), grid, threads, 0, stream, a);
+      else hipLaunchKernelGGL((tile_attention_kernel<HD, T, false, false, false, true>), grid, threads, 0, stream, a);
+    }
+  } else if (joined) {
     hipLaunchKernelGGL((tile_attention_kernel<HD, T, false, false, true>), grid, threads, 0, stream, a);
   } else if (T == kKvBf16 || wide) {
     if (once) hipLaunchKernelGGL((tile_attention_kernel<HD, T, true, true, false>), grid, threads, 0, stream, a);

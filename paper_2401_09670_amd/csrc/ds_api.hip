@@ -406,9 +406,10 @@ ds_status validate_cu(ds_ctx* ctx, const char* who, const int32_t* cu_dev, int B
   return DS_OK;
 }
 
-// the first ceil(tokens[i] / page) entries of every row of block_tables name a block in [0, num_blocks)
+// the first ceil(tokens[i] / page) entries of every row of block_tables name a block in [0, num_blocks); with a window those
+// that hold one of its tokens or one of the first `sinks`
 ds_status validate_tables(ds_ctx* ctx, const char* who, const int32_t* bt_dev, int B, int max_blocks,
-                          int num_blocks, const std::vector<int32_t>& tokens, hipStream_t s) {
+                          int num_blocks, const std::vector<int32_t>& tokens, hipStream_t s, int window = 0, int sinks = 0) {
   std::vector<int32_t> bt;
   ds_status st = fetch_i32(ctx, bt_dev, (size_t)B * max_blocks, s, bt);
   if (st != DS_OK) return st;
@@ -419,6 +420,7 @@ ds_status validate_tables(ds_ctx* ctx, const char* who, const int32_t* bt_dev, i
       return fail(ctx, DS_ERR_BOUNDS, "%s: sequence %d needs %ld pages > max_blocks_per_seq %d", who, i, pages,
                   max_blocks);
     for (long j = 0; j < pages; ++j) {
+      if (window > 0 && j * page >= sinks && (j + 1) * page <= (long)tokens[i] - window) continue;
       const int32_t id = bt[(size_t)i * max_blocks + j];
       if (id < 0 || id >= num_blocks)
         return fail(ctx, DS_ERR_BOUNDS, "%s: block_tables[%d][%ld] = %d outside [0, %d)", who, i, j, id, num_blocks);
@@ -999,6 +1001,7 @@ struct StepCache {
   bool tiles;
   const int32_t *cu_groups = nullptr, *prefix_lens = nullptr, *prefix_tables = nullptr;
   int n_groups = 0, max_group_rows = 0, max_prefix_blocks = 0, max_prefix = 0;
+  int window = 0, sinks = 0;  // window > 0: only the last `window` and the first `sinks` tokens of a sequence are seen
 };
 
 static ds::TileAttention tile_attention(const ds_ctx* ctx, const StepCache& cache, const void* q, int q_stride,
@@ -1014,7 +1017,9 @@ static ds::TileAttention tile_attention(const ds_ctx* ctx, const StepCache& cach
   t.kv_len_add = kv_len_add; t.B = B; t.max_blocks = max_blocks; t.max_kv_len = max_kv_len;
   t.cache = cache.kv;
   t.n_heads = c.n_heads; t.n_kv_heads = c.n_kv_heads; t.head_dim = c.head_dim;
-  t.plan = ds::tile_plan(B, c.n_heads, c.n_kv_heads, c.head_dim, cache.kv.type, max_kv_len, cache.n_groups, cache.max_prefix);
+  t.window = cache.window; t.sinks = cache.sinks;
+  const int most = cache.window > 0 ? ds::tile_window_tokens(max_kv_len, cache.window, cache.sinks) : max_kv_len;
+  t.plan = ds::tile_plan(B, c.n_heads, c.n_kv_heads, c.head_dim, cache.kv.type, most, cache.n_groups, cache.max_prefix);
   t.o = o; t.states = states;
   return t;
 }
@@ -1361,7 +1366,9 @@ static ds_status paged_attention(ds_ctx* ctx, const char* who, const void* q, co
   if (ctx->validate) {
     std::vector<int32_t> lens;
     if (ds_status st = validate_lens(ctx, who, kv_lens, B, 0, 0, max_kv_len, s, lens)) return st;
-    if (ds_status st = validate_tables(ctx, who, block_tables, B, max_blocks_per_seq, num_blocks, lens, s)) return st;
+    if (ds_status st = validate_tables(ctx, who, block_tables, B, max_blocks_per_seq, num_blocks, lens, s, cache.window,
+                                       cache.sinks))
+      return st;
     if (cache.n_groups > 0)
       if (ds_status st = validate_groups(ctx, who, cache.cu_groups, cache.n_groups, cache.max_group_rows, B,
                                          cache.prefix_lens, cache.prefix_tables, cache.max_prefix_blocks, cache.max_prefix,
@@ -1472,6 +1479,28 @@ ds_status ds_kv_append_rotary(ds_ctx* ctx, const void* q, int32_t q_stride, cons
   const ds::KvCache cache{k_cache, v_cache, k_scale, v_scale, kv_type};
   DS_LAUNCH(ctx, s, DS_K_KV_APPEND, ds::launch_kv_append_rotary(rows, cache, c.n_heads, c.n_kv_heads, c.head_dim, s));
   return DS_OK;
+}
+
+size_t ds_decode_window_workspace_bytes(const ds_ctx* ctx, int32_t max_batch, int32_t max_ctx, int32_t window, int32_t sinks) {
+  if (!ctx || max_batch <= 0 || max_ctx <= 0 || max_ctx > kMostTokens || window <= 0 || sinks < 0) return 0;
+  return tile_states(ctx, max_batch, ds::tile_window_tokens(max_ctx, window, sinks), 0);
+}
+
+ds_status ds_decode_attention_window(ds_ctx* ctx, const void* q, const int32_t* kv_lens, const int32_t* block_tables,
+                                     int32_t B, int32_t max_blocks_per_seq, int32_t max_kv_len, int32_t window, int32_t sinks,
+                                     const void* k_cache, const void* v_cache, const void* k_scale, const void* v_scale,
+                                     int32_t num_blocks, int32_t kv_type, void* o, void* workspace, size_t workspace_bytes,
+                                     void* stream) {
+  const char* who = "ds_decode_attention_window";
+  if (!ctx) return DS_ERR_INVALID_ARG;
+  if (window <= 0 || sinks < 0) return fail(ctx, DS_ERR_INVALID_ARG, "%s: a window below 1 or sinks below 0", who);
+  if (ds_status st = check_cache(ctx, who, k_cache, v_cache, k_scale, v_scale, num_blocks, kv_type, true)) return st;
+  StepCache cache{{const_cast<void*>(k_cache), const_cast<void*>(v_cache), const_cast<void*>(k_scale),
+                   const_cast<void*>(v_scale), kv_type}, true};
+  cache.window = window;
+  cache.sinks = sinks;
+  return paged_attention(ctx, who, q, cache, kv_lens, block_tables, B, max_blocks_per_seq, max_kv_len, num_blocks, o,
+                         workspace, workspace_bytes, stream);
 }
 
 ds_status ds_profile_enable(ds_ctx* ctx, int32_t on) {

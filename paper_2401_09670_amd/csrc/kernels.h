@@ -233,7 +233,9 @@ struct TileAttention {
   int n_heads, n_kv_heads, head_dim;
   TilePlan plan;
   void *o, *states;
+  int window, sinks;  // window > 0: over the last `window` and the first `sinks` tokens of each sequence alone (no prefixes)
 };
+int tile_window_tokens(int max_len, int window, int sinks);  // what a plan goes by then
 bool tile_attention_fits(const TileAttention& t);  // into a launch
 hipError_t launch_tile_attention(const TileAttention& t, hipStream_t stream);
 

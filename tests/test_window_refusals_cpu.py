@@ -1,4 +1,7 @@
 """What the calls for positions by rotation and for attention through a window refuse before anything touches a device."""
+import random
+import re
+
 import pytest
 
 from paper_2401_09670_amd import binding
@@ -19,6 +22,8 @@ CALLS = {  # arguments in their order, without the context and the stream
     "ds_kv_append_rotary": dict(q=P, q_stride=1536, k=P, v=P, kv_stride=1536, cu_rows=P, B=2, t=40, ctx_lens=P, positions=P,
                                 table=P, n_pos=100, rot=64, adjacent=0, block_tables=P, max_blocks=4, **CACHE, q_out=2 * P,
                                 k_out=2 * P),
+    "ds_decode_attention_window": dict(q=P, kv_lens=P, block_tables=P, B=4, max_blocks=128, max_kv_len=2000, window=1900,
+                                       sinks=4, **CACHE, o=P, workspace=P, workspace_bytes=1 << 30),
 }
 MAY_BE_NULL = ("cu_rows", "positions", "k_out")
 INDICES = ("cu_rows", "cu_seqlens", "ctx_lens", "positions", "block_tables", "kv_lens")
@@ -50,6 +55,16 @@ def _cases():
                 yield name, dict(kv_type=kind), UNSUPPORTED
             yield name, dict(kv_type=0), INVALID               # bf16 pages come without scales
             yield name, dict(kv_type=0, k_scale=None), INVALID
+        if "window" in args:
+            yield name, dict(window=-2 ** 31), INVALID
+            yield name, dict(sinks=-1), INVALID
+        if "workspace" in args:
+            yield name, dict(workspace=None), WORKSPACE
+            yield name, dict(workspace_bytes=64), WORKSPACE
+            yield name, dict(workspace=P + 8), INVALID
+            yield name, dict(max_kv_len=16 * args["max_blocks"] + 1), INVALID
+            yield name, dict(B=65536), INVALID                 # more than a launch can have
+            yield name, dict(max_kv_len=2 ** 31 - 1, max_blocks=2 ** 27), INVALID
     name = "ds_kv_append_rotary"
     for stride in (dict(q_stride=1016), dict(kv_stride=248), dict(q_stride=1028), dict(kv_stride=260)):
         yield name, stride, INVALID                            # below a row's width, rows that would not be aligned
@@ -72,3 +87,44 @@ def test_refused(ctx, name, change, want):
 @pytest.mark.parametrize("name", list(CALLS))
 def test_no_context(name):
     assert getattr(binding.load_library(), name)(None, *CALLS[name].values(), None) == INVALID
+
+
+SHAPES = [(256, 4, 64, 0), (5120, 40, 128, 0), (8192, 64, 128, 8), (2048, 16, 128, 1), (4096, 32, 128, 1)]
+
+
+@pytest.mark.parametrize("hidden,n,s,n_kv", SHAPES)
+def test_a_decode_call_needs_no_more_than_was_promised(hidden, n, s, n_kv):
+    """A workspace for the largest batch, length, window and first tokens serves every smaller call."""
+    c = binding.Context(hidden, n, s, 1024, n_kv_heads=n_kv)
+    rng, asked = random.Random(hidden), 0
+    for _ in range(1500):
+        B, L = int(2 ** rng.uniform(0, 8.5)), int(2 ** rng.uniform(0, 16))
+        window, sinks = int(2 ** rng.uniform(0, 15)), int(2 ** rng.uniform(0, 10)) - 1
+        most = [x + rng.randrange(x + 1) for x in (B, L, window, sinks)]
+        kind = rng.randrange(3)
+        scales = (None, None) if kind == 0 else (P, P)
+        promised = c.ds_decode_window_workspace_bytes(*most)
+        st = c.lib.ds_decode_attention_window(c.handle, P, P, P, B, -(-L // 16), L, window, sinks, P, P, *scales, 1 << 20, kind,
+                                              P, None, 0, None) if _splits(c, B, L, window, sinks) else None
+        if st is not None:
+            assert st == WORKSPACE
+            asked += 1
+            text = c.lib.ds_last_error(c.handle).decode()
+            assert int(re.search(r"workspace 0 < (\d+)", text).group(1)) <= promised
+    assert asked >= 5
+    c.close()
+
+
+def _splits(c, B, L, window, sinks):
+    """Whether such a call surely asks for a workspace (else it would be launched): 96 pages or more, few rows."""
+    seen = min(-(-L // 16), window // 16)
+    return seen >= 96 and B * (c.cfg.n_kv_heads or c.cfg.n_heads) <= 128
+
+
+def test_sizes_of_nothing():
+    c = binding.Context(256, 4, 64, 1024)
+    for args in ((0, 5, 5, 5), (5, 0, 5, 5), (5, 5, 0, 5), (5, 5, 5, -1), (5, 2 ** 31 - 1, 5, 5)):
+        assert c.ds_decode_window_workspace_bytes(*args) == 0
+    assert c.ds_decode_window_workspace_bytes(4, 2 ** 30, 2 ** 31 - 1, 2 ** 31 - 1) > 0
+    assert binding.load_library().ds_decode_window_workspace_bytes(None, 1, 1, 1, 1) == 0
+    c.close()
