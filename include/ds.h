@@ -384,6 +384,16 @@ ds_status ds_kv_append_rotary(ds_ctx *ctx, const void *q, int32_t q_stride, cons
                               void *k_scale, void *v_scale, int32_t num_blocks, int32_t kv_type, void *q_out, void *k_out,
                               void *stream);
 
+/* ds_prefill_attention through a window: the query of token i sees token j <= i of its sequence if i - j < window (>= 1) or
+ * j < sinks (>= 0: first tokens that stay visible).  Rows of q, k and v start their strides (in elements, multiples of 8 up to
+ * 2^24, at least a row's width) apart: k and q as ds_kv_append_rotary leaves them, v in the rows of the QKV product.  o is
+ * [t, n, s].  Sequences may be empty (the debug validation, which is ds_prefill_attention's, takes none); rows from
+ * cu_seqlens[B] on are left as they are.  What a query does not see does not count, whatever it holds.  Scores are fp32: a key
+ * whose score is below its range weighs nothing (all of them: output 0).  A probability is rounded to bf16 before it meets V. */
+ds_status ds_prefill_attention_window(ds_ctx *ctx, const void *q, int32_t q_stride, const void *k, int32_t k_stride,
+                                      const void *v, int32_t v_stride, const int32_t *cu_seqlens, int32_t B, int32_t t,
+                                      int32_t max_seqlen, int32_t window, int32_t sinks, void *o, void *stream);
+
 /* ds_decode_attention over the last `window` (>= 1) tokens of each sequence and its first `sinks` (>= 0): with kv_lens[i] = L
  * the query, which is token L - 1's, sees token j if L - 1 - j < window or j < sinks.  Any kv_type, on its conventions
  * (roundings, scores beyond fp32's range, kv_lens[i] = 0: output 0).  What it does not see does not count, whatever it holds, and

@@ -37,7 +37,7 @@ EXPORTS = ("ds_create", "ds_destroy", "ds_last_error", "ds_set_validate", "ds_pr
            "ds_decode_quant_workspace_bytes", "ds_decode_shared_workspace_bytes", "ds_kv_migrate_quant",
            "ds_kv_read_quant", "ds_kv_append_quant", "ds_decode_attention_quant", "ds_decode_attention_shared",
            "ds_decode_step_quant", "ds_decode_step_shared", "ds_kv_append_rotary",
-           "ds_decode_window_workspace_bytes", "ds_decode_attention_window")
+           "ds_decode_window_workspace_bytes", "ds_decode_attention_window", "ds_prefill_attention_window")
 
 
 class DsError(RuntimeError):
@@ -62,7 +62,8 @@ class LayerWeights(ctypes.Structure):
 TENSOR_CALLS = ("ds_prefill", "ds_kv_migrate", "ds_decode_step", "ds_decode_step_static", "ds_layernorm", "ds_linear",
                 "ds_prefill_attention", "ds_decode_attention", "ds_embed", "ds_next_token", "ds_kv_migrate_quant",
                 "ds_kv_read_quant", "ds_kv_append_quant", "ds_decode_attention_quant", "ds_decode_attention_shared",
-                "ds_decode_step_quant", "ds_decode_step_shared", "ds_kv_append_rotary", "ds_decode_attention_window")
+                "ds_decode_step_quant", "ds_decode_step_shared", "ds_kv_append_rotary", "ds_decode_attention_window",
+                "ds_prefill_attention_window")
 
 _lib = None
 
@@ -147,6 +148,7 @@ def load_library() -> ctypes.CDLL:
             ("ds_decode_step_shared", [ctypes.POINTER(LayerWeights), vp, *groups, vp, vp, i32, i32, i32, *cache, vp, vp,
                                        sz]),
             ("ds_kv_append_rotary", [vp, i32, vp, vp, i32, vp, i32, i32, vp, vp, vp, i32, i32, i32, vp, i32, *cache, vp, vp]),
+            ("ds_prefill_attention_window", [vp, i32, vp, i32, vp, i32, vp, i32, i32, i32, i32, i32, vp]),
             ("ds_decode_attention_window", [vp, vp, vp, i32, i32, i32, i32, i32, *cache, vp, vp, sz])):
         getattr(lib, name).argtypes = [vp, *args, vp]
         getattr(lib, name).restype = ctypes.c_int
@@ -344,6 +346,11 @@ class Context:
             self.handle.value, q, q_stride, k, v, kv_stride, cu_rows, B, t, ctx_lens, positions, table, n_pos, rot, adjacent,
             block_tables, max_blocks_per_seq, k_cache, v_cache, k_scale, v_scale, num_blocks, kv_type, q_out, k_out,
             _stream()))
+
+    def ds_prefill_attention_window(self, q, q_stride: int, k, k_stride: int, v, v_stride: int, cu_seqlens, B: int, t: int,
+                                    max_seqlen: int, window: int, sinks: int, o):
+        self._check(self.calls.ds_prefill_attention_window(self.handle.value, q, q_stride, k, k_stride, v, v_stride,
+                                                           cu_seqlens, B, t, max_seqlen, window, sinks, o, _stream()))
 
     def ds_decode_window_workspace_bytes(self, max_batch: int, max_ctx: int, window: int, sinks: int) -> int:
         return self.lib.ds_decode_window_workspace_bytes(self.handle, max_batch, max_ctx, window, sinks)

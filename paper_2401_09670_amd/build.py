@@ -11,7 +11,7 @@ CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "libds.so")
 SOURCES = ["gemm.hip", "gemm_tiles.hip", "gemm_skinny.hip", "ds_api.hip", "layernorm.hip", "kv_cache.hip",
            "attn_prefill.hip", "attn_decode.hip", "token_io.hip",
-           "kv_quant.hip", "attn_paged.hip", "kv_rotary.hip"]
+           "kv_quant.hip", "attn_paged.hip", "kv_rotary.hip", "attn_window.hip"]
 CALLS_PATH = os.path.join(PKG_DIR, "_calls.so")
 CXX = os.environ.get("CXX", "g++")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

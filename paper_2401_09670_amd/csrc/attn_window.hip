@@ -1,0 +1,365 @@
+// Causal attention of packed prompts through a sliding window that leaves the first tokens visible: query i sees key j <= i if
+// i - j < window or j < sinks.
+//
+// A workgroup owns 64 rows a wave of one key/value head: a row is a (query, query head), a power of two of the heads that share
+// the key/value head for each query, so that the more heads share it the fewer queries a workgroup has, and the less its windows
+// reach beyond each other.  It goes over one list of keys: the first tokens before its first query's window, then from there to
+// its last query.  Key number v of that list (all its rows') is seen by a row if v <= top and (v >= low or v < sinks), with
+// top and low the numbers of the row's own token and of its window's first.
+//
+// Scores are computed transposed, S^T[key, row] = K Q^T, so that a lane holds scores of one row (lane % 32 of each of the two
+// blocks of 32 that a wave has): running maximum and sum are scalars of a lane, and the probabilities are the column operand of
+// O^T[d, row] = V^T P^T as they are.  K and V tiles of 64 keys land row-major in one of two LDS buffers by direct loads while
+// the other is multiplied; V^T comes out through the transposing LDS read.  Each operand read from LDS meets both blocks.
+#include <algorithm>
+
+#include "common.h"
+#include "kernels.h"
+
+namespace ds {
+
+constexpr int kWinKeys = 64;       // of a tile
+constexpr float kWinSlack = 8.f;   // exponent headroom before the softmax's reference point is moved
+
+struct WindowArgs {
+  WindowRows r;
+  int kv_group;      // query heads on a key/value head
+  int pack_log2;     // of the heads of a row's query
+  int head_blocks;   // n_heads >> pack_log2
+  int places;        // of a head block: t / queries + B
+  int blocks, per_xcd;
+  float scale_log2e;
+};
+
+__device__ __forceinline__ bf16x8 as_bf16(u32x4 v) { return __builtin_bit_cast(bf16x8, v); }
+
+template <int HD, int NW>
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(HD == 128 ? 1 : 2))) void window_attention_kernel(
+    const WindowArgs a) {
+  constexpr int DSTEPS = HD / 16, DT = HD / 32, CPR = HD / 8;
+  constexpr int TILE = kWinKeys * HD, BUF = 2 * TILE;
+  constexpr int RPL = 64 / CPR;                 // tile rows of a wave-level load
+  constexpr int NLD = kWinKeys / (RPL * NW);    // loads of a wave, tile and operand
+  extern __shared__ __attribute__((aligned(1024))) uint16_t win_lds[];
+
+  // Workgroups reach the chip's eight partitions in turn; each takes a run of the list (key/value head, place, block of its
+  // heads), so that neighbours on one partition share keys.
+  const int id = (blockIdx.x & 7) * a.per_xcd + (blockIdx.x >> 3);
+  if (id >= a.blocks) return;
+  const WindowRows& in = a.r;
+  const int n_sub = a.kv_group >> a.pack_log2;
+  const int sub = id % n_sub, kv = id / n_sub / a.places;
+  const int place = id / n_sub % a.places;
+  const int pack = 1 << a.pack_log2, queries = (64 * NW) >> a.pack_log2;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  int upto = 0;  // sequences that begin at this place or before
+  for (int i0 = 0; i0 < in.B; i0 += 64) {
+    const int i = i0 + lane;
+    upto += __builtin_popcountll(__builtin_amdgcn_ballot_w64(i < in.B && in.cu_seqlens[min(i, in.B - 1)] / queries + i <= place));
+  }
+  if (upto == 0) return;
+  const int seq = upto - 1, start = in.cu_seqlens[seq];
+  const int len = min(in.cu_seqlens[seq + 1] - start, in.max_seqlen);
+  const int q0 = (place - start / queries - seq) * queries;
+  if (q0 >= len) return;
+
+  // the list of keys
+  const int q_end = min(q0 + queries, len);
+  const int band = max(q0 - in.window + 1, 0);
+  const int first = min(in.sinks, band);        // number `first` is key `band`
+  const int total = q_end - band + first;
+  const int n_tiles = (total + kWinKeys - 1) / kWinKeys;
+
+  const int hl = lane >> 5, lq = lane & 31;
+  const uint16_t* kbase = in.k + (size_t)start * in.k_stride + (size_t)kv * HD;
+  const uint16_t* vbase = in.v + (size_t)start * in.v_stride + (size_t)kv * HD;
+
+  // Chunk c of 16 bytes of row r of a tile lies at c ^ swizzle(r), by the source address of the load.  K (16-byte reads of 32
+  // rows at one chunk number): rows of 256 bytes r & 15, of 128 bytes (r >> 1) & 7.  V (transposing 8-byte reads of 4 rows, 4
+  // chunks for each half of a wave): (r & 3) << 2, ((r >> 1) & 1) << 2.
+  const int ld_sub = lane / CPR, ld_c = lane % CPR;
+  const int ld_row0 = wave * NLD * RPL + ld_sub;
+  auto k_col = [&](int row) { return (ld_c ^ (CPR == 16 ? row & 15 : (row >> 1) & 7)) * 8; };
+  const int v_col = (ld_c ^ (CPR == 16 ? ld_sub << 2 : ((ld_sub >> 1) & 1) << 2)) * 8;
+  auto to_lds = [&](const uint16_t* from, uint16_t* to) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
+                                     (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+  };
+  auto request = [&](int v0, int buf) {
+    uint16_t* dst = win_lds + buf * BUF + wave * NLD * 512;
+    if ((v0 >= first || v0 + kWinKeys <= first) && v0 + kWinKeys <= total) {
+      const int key0 = v0 >= first ? v0 - first + band : v0;
+      const uint16_t* kt = kbase + (size_t)key0 * in.k_stride;
+      const uint16_t* vt = vbase + (size_t)key0 * in.v_stride;
+#pragma unroll
+      for (int j = 0; j < NLD; ++j) {
+        const int row = ld_row0 + j * RPL;
+        to_lds(kt + (uint32_t)(row * in.k_stride + k_col(row)), dst + j * 512);
+        to_lds(vt + (uint32_t)(row * in.v_stride + v_col), dst + TILE + j * 512);
+      }
+    } else {  // (rows behind the end: the last key again)
+#pragma unroll
+      for (int j = 0; j < NLD; ++j) {
+        const int row = ld_row0 + j * RPL, v = min(v0 + row, total - 1);
+        const size_t key = v >= first ? v - first + band : v;
+        to_lds(kbase + key * in.k_stride + k_col(row), dst + j * 512);
+        to_lds(vbase + key * in.v_stride + v_col, dst + TILE + j * 512);
+      }
+    }
+  };
+  auto wait_loads = [] { __builtin_amdgcn_s_waitcnt((0x7 << 4) | (0xf << 8)); };  // vmcnt(0) alone
+
+  // the lane's rows
+  const int row_q = lq >> a.pack_log2, row_head = (kv * n_sub + sub) * pack + (lq & (pack - 1));
+  const int block_q = 32 >> a.pack_log2;        // queries of a block of rows
+  const int wave_q = q0 + 2 * wave * block_q;
+  const bool idle = wave_q >= len;
+  bf16x8 qf[2][DSTEPS];
+  int top[2], low[2];
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+    const int i = wave_q + b * block_q + row_q;
+    const uint16_t* qrow = in.q + ((size_t)start + min(i, len - 1)) * in.q_stride + (size_t)row_head * HD + hl * 8;
+#pragma unroll
+    for (int st = 0; st < DSTEPS; ++st) qf[b][st] = as_bf16(ld16(qrow + st * 16));
+    top[b] = i - band + first;
+    low[b] = top[b] - in.window + 1;
+  }
+  // of the wave: the last number that any of its rows sees, the one up to which all do; where the first row's window begins
+  // and where the last one's does
+  const int wave_top = wave_q + 2 * block_q - 1 - band + first, least_top = wave_q - band + first;
+  const int wave_low = least_top - in.window + 1, most_low = wave_top - in.window + 1;
+
+  floatx16 oacc[2][DT];
+  float m_run[2], l_run[2];
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+    m_run[b] = kLowestScore;
+    l_run[b] = 0.f;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) oacc[b][d][r] = 0.f;
+  }
+
+  request(0, 0);
+  wait_loads();
+  __syncthreads();
+  const int kswz = CPR == 16 ? (lq & 15) : ((lq >> 1) & 7);
+  const int i16 = lane & 15;
+  const int vswz = CPR == 16 ? ((i16 >> 2) << 2) : (((i16 >> 3) & 1) << 2);
+  const int vchunk = 2 * ((lane >> 4) & 1) + ((i16 & 3) >> 1);
+  for (int tile = 0; tile < n_tiles; ++tile) {
+    const int v0 = tile * kWinKeys;
+    const uint16_t* ks = win_lds + (tile & 1) * BUF;
+    const uint16_t* vs = ks + TILE;
+    if (tile + 1 < n_tiles) request(v0 + kWinKeys, (tile + 1) & 1);
+    const bool none = idle || v0 > wave_top || (v0 + kWinKeys <= wave_low && v0 >= in.sinks);
+    if (!none) {
+      // ---- S^T = K Q^T ----
+      floatx16 s[2][2];
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[b][u][r] = 0.f;
+#pragma unroll
+      for (int st = 0; st < DSTEPS; ++st)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const bf16x8 kf = as_bf16(ld16(ks + (32 * u + lq) * HD + ((2 * st + hl) ^ kswz) * 8));
+#pragma unroll
+          for (int b = 0; b < 2; ++b) s[b][u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[b][st], s[b][u], 0, 0, 0);
+        }
+      // ---- masks; element r of half u is number v0 + 32 u + 8 (r / 4) + 4 hl + r % 4 ----
+      if (v0 + kWinKeys - 1 > least_top || (v0 < most_low && v0 + kWinKeys > in.sinks)) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              const int v = v0 + u * 32 + (r >> 2) * 8 + hl * 4 + (r & 3);
+              if (v > top[b] || (v < low[b] && v >= in.sinks)) s[b][u][r] = -INFINITY;
+            }
+      }
+      u32x4 pw[2][4];  // pw[b][2 u + x]: column operand of the step over 16 keys
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        float most = -INFINITY;
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) most = fmaxf(most, s[b][u][r]);
+        most = lane_op<32>(most, MaxOp());
+        // The reference point only has to keep the exponentials in range: it moves when some row's maximum grew by more than
+        // kWinSlack in the exponent.
+        if (__builtin_amdgcn_ballot_w64(most * a.scale_log2e > m_run[b] * a.scale_log2e + kWinSlack) != 0) {
+          const float m_new = fmaxf(m_run[b], most);
+          const float alpha = __builtin_amdgcn_exp2f((m_run[b] - m_new) * a.scale_log2e);
+          l_run[b] *= alpha;
+          m_run[b] = m_new;
+#pragma unroll
+          for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) oacc[b][d][r] *= alpha;
+        }
+        const float mb = m_run[b] * a.scale_log2e;
+        float sum = 0.f;
+        bf16x2 ones;
+        ones[0] = (__bf16)1.f;
+        ones[1] = (__bf16)1.f;
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int r = 0; r < 16; r += 2) {
+            bf16x2 p;  // (rounded to bf16, 2^-9 of each at most: the sum counts what the second product multiplies)
+            p[0] = (__bf16)__builtin_amdgcn_exp2f(s[b][u][r] * a.scale_log2e - mb);
+            p[1] = (__bf16)__builtin_amdgcn_exp2f(s[b][u][r + 1] * a.scale_log2e - mb);
+            sum = __builtin_amdgcn_fdot2_f32_bf16(p, ones, sum, false);
+            pw[b][2 * u + (r >> 3)][(r & 7) >> 1] = __builtin_bit_cast(uint32_t, p);
+          }
+        l_run[b] += sum;
+      }
+      // ---- O^T += V^T P^T; step x of half u contracts keys 32 u + 16 x + {0..3, 8..11} + 4 hl ----
+      const uint16_t* vfrag = vs + (4 * hl + (i16 >> 2)) * HD + (i16 & 1) * 4;
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          typedef short short4v __attribute__((ext_vector_type(4)));
+          typedef __attribute__((address_space(3))) short4v* lds_short4_ptr;
+          const int col = ((4 * d + vchunk) ^ vswz) * 8;
+          const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_ptr)(vfrag + x * 16 * HD + col)));
+          const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_ptr)(vfrag + (x * 16 + 8) * HD + col)));
+          const bf16x8 vf = as_bf16(u32x4{lo[0], lo[1], hi[0], hi[1]});
+#pragma unroll
+          for (int b = 0; b < 2; ++b) oacc[b][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, as_bf16(pw[b][x]), oacc[b][d], 0, 0, 0);
+        }
+    }
+    wait_loads();
+    __syncthreads();
+  }
+  if (idle) return;
+
+  // ---- the quotient; lane holds O[row][32 d + 8 g + 4 hl + i] ----
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+    const int i = wave_q + b * block_q + row_q;
+    const float l = lane_op<32>(l_run[b], AddOp());
+    const float inv = l == 0.f ? 0.f : 1.f / l;  // (every score below fp32's range: 0)
+    bool nan = false;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        oacc[b][d][r] *= inv;
+        nan = nan || oacc[b][d][r] != oacc[b][d][r];
+      }
+    if (i < len) {
+      uint16_t* orow = in.o + (((size_t)start + i) * in.n_heads + row_head) * HD + hl * 4;
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+          *reinterpret_cast<u32x2*>(orow + d * 32 + g * 8) =
+              u32x2{pack_bf16(oacc[b][d][4 * g], oacc[b][d][4 * g + 1]), pack_bf16(oacc[b][d][4 * g + 2], oacc[b][d][4 * g + 3])};
+    }
+    // A hidden key's V that is not finite has made NaN of the rows that share a tile with it (0 times it): rows with NaN are done
+    // again, key by key over what they see, 64 scores at a time.  NaN that they see stays.
+    uint64_t again = __builtin_amdgcn_ballot_w64(nan && i < len);
+    again = (again | again >> 32) & 0xffffffffu;
+    while (again) {
+      const int row = __builtin_ctzll(again);
+      again &= again - 1;
+      const int at = wave_q + b * block_q + (row >> a.pack_log2), head = (kv * n_sub + sub) * pack + (row & (pack - 1));
+      const uint16_t* qr = in.q + ((size_t)start + at) * in.q_stride + (size_t)head * HD;
+      const int begin = max(at - in.window + 1, 0), before = min(in.sinks, begin), n = at + 1 - begin + before;
+      constexpr int ND = HD / 64;
+      float m = kLowestScore, sum = 0.f, out[ND] = {};
+      for (int c0 = 0; c0 < n; c0 += 64) {
+        const int v = min(c0 + lane, n - 1);
+        const uint16_t* kr = kbase + (size_t)(v < before ? v : v - before + begin) * in.k_stride;
+        float dot = 0.f;
+#pragma unroll 4
+        for (int d = 0; d < HD; d += 2) {
+          const uint32_t x = *reinterpret_cast<const uint32_t*>(qr + d), y = *reinterpret_cast<const uint32_t*>(kr + d);
+          dot = fmaf(bf16_lo(x), bf16_lo(y), dot);
+          dot = fmaf(bf16_hi(x), bf16_hi(y), dot);
+        }
+        dot = c0 + lane < n ? dot * a.scale_log2e : -INFINITY;
+        float most = dot;
+        most = lane_op<1>(most, MaxOp());
+        most = lane_op<2>(most, MaxOp());
+        most = lane_op<kMirror4>(most, MaxOp());
+        most = across_groups<8>(most, MaxOp());
+        const float m_new = fmaxf(m, most), alpha = __builtin_amdgcn_exp2f(m - m_new), p = __builtin_amdgcn_exp2f(dot - m_new);
+        m = m_new;
+        sum = sum * alpha + wave_sum(p);
+#pragma unroll
+        for (int j = 0; j < ND; ++j) out[j] *= alpha;
+        const int count = min(64, n - c0);
+        for (int j = 0; j < count; ++j) {
+          const float pj = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(p), j));
+          const int vj = c0 + j;
+          const uint16_t* vr = vbase + (size_t)(vj < before ? vj : vj - before + begin) * in.v_stride + ND * lane;
+#pragma unroll
+          for (int e = 0; e < ND; ++e) out[e] = fmaf(pj, __uint_as_float((uint32_t)vr[e] << 16), out[e]);
+        }
+      }
+      __bf16* to = reinterpret_cast<__bf16*>(in.o) + (((size_t)start + at) * in.n_heads + head) * HD + ND * lane;
+#pragma unroll
+      for (int e = 0; e < ND; ++e) to[e] = (__bf16)(sum == 0.f ? 0.f : out[e] / sum);
+    }
+  }
+}
+
+// Heads of a query that a row block has together: the largest power of two that divides the group, up to 32.
+static int pack_log2_of(int kv_group) {
+  int p = 0;
+  while (p < 5 && kv_group % (2 << p) == 0) ++p;
+  return p;
+}
+
+struct WindowPlan {
+  int waves, pack_log2;
+  long places, blocks;
+};
+static WindowPlan window_plan(const WindowRows& r) {
+  WindowPlan p;
+  p.waves = 2;
+  p.pack_log2 = pack_log2_of(r.n_heads / r.n_kv_heads);
+  p.places = (long)r.t / ((64 * p.waves) >> p.pack_log2) + r.B;
+  p.blocks = p.places * (r.n_heads >> p.pack_log2);
+  return p;
+}
+bool window_attention_fits(const WindowRows& r) { return window_plan(r).blocks <= 0x7fffffffL / 256 - 8; }
+
+template <int HD, int NW>
+static hipError_t launch_window(const WindowArgs& a, hipStream_t stream) {
+  constexpr int kLds = 2 * 2 * kWinKeys * HD * (int)sizeof(uint16_t);
+  (void)KernelAttrReg<window_attention_kernel<HD, NW>, kLds>::done;
+  hipLaunchKernelGGL((window_attention_kernel<HD, NW>), dim3((unsigned)(8 * a.per_xcd)), dim3(64 * NW), kLds, stream, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_window_attention(const WindowRows& r, int head_dim, hipStream_t stream) {
+  if (!window_attention_fits(r)) return hipErrorInvalidValue;
+  const WindowPlan p = window_plan(r);
+  WindowArgs a{};
+  a.r = r;
+  a.kv_group = r.n_heads / r.n_kv_heads;
+  a.pack_log2 = p.pack_log2;
+  a.head_blocks = r.n_heads >> p.pack_log2;
+  a.places = (int)p.places;
+  a.blocks = (int)p.blocks;
+  a.per_xcd = (int)((p.blocks + 7) / 8);
+  a.scale_log2e = 1.4426950408889634f / sqrtf((float)head_dim);
+  if (head_dim == 128) return launch_window<128, 2>(a, stream);
+  if (head_dim == 64) return launch_window<64, 2>(a, stream);
+  return hipErrorInvalidValue;
+}
+
+}  // namespace ds

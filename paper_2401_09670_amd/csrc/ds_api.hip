@@ -937,6 +937,7 @@ static ds_status check_cache(ds_ctx* ctx, const char* who, const void* k, const 
   return DS_OK;
 }
 
+constexpr int32_t kMostStride = 1 << 24;  // of rows, in elements: 64 of them are within 32 bits' reach of each other
 constexpr int32_t kMostTokens = INT32_MAX - 1024;  // of a sequence or prefix on pages in tiles: their positions are 32 bits
 
 // Packed rows and the pages of their sequences.
@@ -1478,6 +1479,36 @@ ds_status ds_kv_append_rotary(ds_ctx* ctx, const void* q, int32_t q_stride, cons
     if (ds_status st = validate_new_rows(ctx, who, rows, num_blocks, s)) return st;
   const ds::KvCache cache{k_cache, v_cache, k_scale, v_scale, kv_type};
   DS_LAUNCH(ctx, s, DS_K_KV_APPEND, ds::launch_kv_append_rotary(rows, cache, c.n_heads, c.n_kv_heads, c.head_dim, s));
+  return DS_OK;
+}
+
+ds_status ds_prefill_attention_window(ds_ctx* ctx, const void* q, int32_t q_stride, const void* k, int32_t k_stride,
+                                      const void* v, int32_t v_stride, const int32_t* cu_seqlens, int32_t B, int32_t t,
+                                      int32_t max_seqlen, int32_t window, int32_t sinks, void* o, void* stream) {
+  const char* who = "ds_prefill_attention_window";
+  if (!ctx) return DS_ERR_INVALID_ARG;
+  const ds_model_cfg& c = ctx->cfg;
+  if (!q || !k || !v || !cu_seqlens || !o) return fail(ctx, DS_ERR_INVALID_ARG, "%s: NULL pointer", who);
+  if (B <= 0 || t <= 0 || max_seqlen <= 0 || max_seqlen > t)
+    return fail(ctx, DS_ERR_INVALID_ARG, "%s: non-positive or inconsistent size", who);
+  if (window <= 0 || sinks < 0) return fail(ctx, DS_ERR_INVALID_ARG, "%s: a window below 1 or sinks below 0", who);
+  for (const int32_t stride : {q_stride, k_stride, v_stride})
+    if (stride % 8 != 0 || stride > kMostStride)
+      return fail(ctx, DS_ERR_INVALID_ARG, "%s: a row stride that is no multiple of 8 or above %d", who, kMostStride);
+  if (q_stride < c.hidden || k_stride < kv_width(c) || v_stride < kv_width(c))
+    return fail(ctx, DS_ERR_INVALID_ARG, "%s: a row stride that is below the row's width", who);
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(o))
+    return fail(ctx, DS_ERR_INVALID_ARG, "%s: pointers must be 16-byte aligned", who);
+  const ds::WindowRows rows{(const uint16_t*)q, (const uint16_t*)k, (const uint16_t*)v, q_stride, k_stride, v_stride,
+                            cu_seqlens, B, t, max_seqlen, window, sinks, c.n_heads, c.n_kv_heads, (uint16_t*)o};
+  if (!ds::window_attention_fits(rows)) return fail(ctx, DS_ERR_INVALID_ARG, "%s: more rows than a launch can have", who);
+  if (ds_status st = ensure_device(ctx)) return st;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (ctx->validate) {
+    std::vector<int32_t> cu;
+    if (ds_status st = validate_cu(ctx, who, cu_seqlens, B, t, max_seqlen, s, cu)) return st;
+  }
+  DS_LAUNCH(ctx, s, DS_K_PREFILL_ATTN, ds::launch_window_attention(rows, c.head_dim, s));
   return DS_OK;
 }
 

@@ -149,6 +149,17 @@ hipError_t launch_prefill_attention(const void* q, const void* k, const void* v,
                                     int B, int t, int max_seqlen, int n_heads, int n_kv_heads, int head_dim, void* o,
                                     hipStream_t stream);
 
+// The same through a window: query i sees key j <= i if i - j < window or j < sinks.  Rows of q, k, v a stride apart.
+struct WindowRows {
+  const uint16_t *q, *k, *v;
+  int q_stride, k_stride, v_stride;
+  const int32_t* cu_seqlens;
+  int B, t, max_seqlen, window, sinks, n_heads, n_kv_heads;
+  uint16_t* o;
+};
+bool window_attention_fits(const WindowRows& r);  // into a launch
+hipError_t launch_window_attention(const WindowRows& r, int head_dim, hipStream_t stream);
+
 // contiguous [t,n,s] -> paged [num_blocks,n,16,s] for K and V in one launch
 hipError_t launch_kv_migrate(const void* k_src, const void* v_src, const int32_t* cu_seqlens, int B,
                              int max_seqlen, const int32_t* block_tables, int max_blocks, void* k_cache,

@@ -126,7 +126,7 @@ PyMethodDef entries[] = {DS_ENTRY(ds_prefill),          DS_ENTRY(ds_kv_migrate),
                          DS_ENTRY(ds_kv_append_quant),  DS_ENTRY(ds_decode_attention_quant),
                          DS_ENTRY(ds_decode_attention_shared), DS_ENTRY(ds_decode_step_quant),
                          DS_ENTRY(ds_decode_step_shared),       DS_ENTRY(ds_kv_append_rotary),
-                         DS_ENTRY(ds_decode_attention_window)};
+                         DS_ENTRY(ds_decode_attention_window), DS_ENTRY(ds_prefill_attention_window)};
 
 // bind(name, address, LayerWeights) -> the entry point of that name whose code lies at `address`
 PyObject* bind(PyObject*, PyObject* args) {

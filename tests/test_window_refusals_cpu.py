@@ -22,6 +22,8 @@ CALLS = {  # arguments in their order, without the context and the stream
     "ds_kv_append_rotary": dict(q=P, q_stride=1536, k=P, v=P, kv_stride=1536, cu_rows=P, B=2, t=40, ctx_lens=P, positions=P,
                                 table=P, n_pos=100, rot=64, adjacent=0, block_tables=P, max_blocks=4, **CACHE, q_out=2 * P,
                                 k_out=2 * P),
+    "ds_prefill_attention_window": dict(q=P, q_stride=1536, k=P, k_stride=256, v=P, v_stride=1536, cu_seqlens=P, B=2, t=40,
+                                        max_seqlen=30, window=8, sinks=4, o=P),
     "ds_decode_attention_window": dict(q=P, kv_lens=P, block_tables=P, B=4, max_blocks=128, max_kv_len=2000, window=1900,
                                        sinks=4, **CACHE, o=P, workspace=P, workspace_bytes=1 << 30),
 }
@@ -55,6 +57,12 @@ def _cases():
                 yield name, dict(kv_type=kind), UNSUPPORTED
             yield name, dict(kv_type=0), INVALID               # bf16 pages come without scales
             yield name, dict(kv_type=0, k_scale=None), INVALID
+        for a in ("q_stride", "k_stride", "v_stride") if "max_seqlen" in args else ():
+            for stride in (248, args[a] + 4, 2 ** 24 + 8):     # below a row's width, not aligned, too far apart
+                yield name, {a: stride}, INVALID
+        if "max_seqlen" in args:
+            yield name, dict(max_seqlen=41), INVALID
+            yield name, dict(B=2 ** 31 - 1), INVALID           # more than a launch can have
         if "window" in args:
             yield name, dict(window=-2 ** 31), INVALID
             yield name, dict(sinks=-1), INVALID
