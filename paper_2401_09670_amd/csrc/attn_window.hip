@@ -12,6 +12,7 @@
 // O^T[d, row] = V^T P^T as they are.  K and V tiles of 64 keys land row-major in one of two LDS buffers by direct loads while
 // the other is multiplied; V^T comes out through the transposing LDS read.  Each operand read from LDS meets both blocks.
 #include <algorithm>
+#include <type_traits>
 
 #include "common.h"
 #include "kernels.h"
@@ -33,14 +34,22 @@ struct WindowArgs {
 
 __device__ __forceinline__ bf16x8 as_bf16(u32x4 v) { return __builtin_bit_cast(bf16x8, v); }
 
+template <int N>
+__device__ __forceinline__ void wait_all_but() {  // vmcnt(N) alone: N in bits 3:0 and 15:14
+  static_assert(N < 64);
+  __builtin_amdgcn_s_waitcnt((N & 0xf) | (N >> 4) << 14 | 0x7 << 4 | 0xf << 8);
+}
+
 template <int HD, int NW>
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(HD == 128 ? 1 : 2))) void window_attention_kernel(
     const WindowArgs a) {
   constexpr int DSTEPS = HD / 16, DT = HD / 32, CPR = HD / 8;
-  constexpr int TILE = kWinKeys * HD, BUF = 2 * TILE;
+  constexpr int TILE = kWinKeys * HD;
   constexpr int RPL = 64 / CPR;                 // tile rows of a wave-level load
   constexpr int NLD = kWinKeys / (RPL * NW);    // loads of a wave, tile and operand
-  extern __shared__ __attribute__((aligned(1024))) uint16_t win_lds[];
+  // Two buffers for K and two for V.  Each is a variable of its own, and which one an access means is known when it is compiled:
+  // the compiler then sees that a load into one need not have landed before another is read.
+  __shared__ __attribute__((aligned(1024))) uint16_t k_lds0[TILE], k_lds1[TILE], v_lds0[TILE], v_lds1[TILE];
 
   // Workgroups reach the chip's eight partitions in turn; each takes a run of the list (key/value head, place, block of its
   // heads), so that neighbours on one partition share keys.
@@ -80,35 +89,36 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(HD == 1
   // chunks for each half of a wave): (r & 3) << 2, ((r >> 1) & 1) << 2.
   const int ld_sub = lane / CPR, ld_c = lane % CPR;
   const int ld_row0 = wave * NLD * RPL + ld_sub;
-  auto k_col = [&](int row) { return (ld_c ^ (CPR == 16 ? row & 15 : (row >> 1) & 7)) * 8; };
+  auto k_col = [&](int row) __attribute__((always_inline)) { return (ld_c ^ (CPR == 16 ? row & 15 : (row >> 1) & 7)) * 8; };
   const int v_col = (ld_c ^ (CPR == 16 ? ld_sub << 2 : ((ld_sub >> 1) & 1) << 2)) * 8;
-  auto to_lds = [&](const uint16_t* from, uint16_t* to) {
+  auto to_lds = [&](const uint16_t* from, uint16_t* to) __attribute__((always_inline)) {
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
                                      (__attribute__((address_space(3))) void*)to, 16, 0, 0);
   };
-  auto request = [&](int v0, int buf) {
-    uint16_t* dst = win_lds + buf * BUF + wave * NLD * 512;
+  // Tile `tile` of K or of V into its buffer; behind the last tile nothing.  Always NLD loads or none.
+  auto request = [&](int tile, auto of_v, uint16_t* dst) __attribute__((always_inline)) {
+    constexpr bool kV = decltype(of_v)::value;
+    const uint16_t* base = kV ? vbase : kbase;
+    const int stride = kV ? in.v_stride : in.k_stride, v0 = tile * kWinKeys;
+    if (tile >= n_tiles) return;
+    dst += wave * NLD * 512;
     if ((v0 >= first || v0 + kWinKeys <= first) && v0 + kWinKeys <= total) {
-      const int key0 = v0 >= first ? v0 - first + band : v0;
-      const uint16_t* kt = kbase + (size_t)key0 * in.k_stride;
-      const uint16_t* vt = vbase + (size_t)key0 * in.v_stride;
+      const uint16_t* from = base + (size_t)(v0 >= first ? v0 - first + band : v0) * stride;
 #pragma unroll
       for (int j = 0; j < NLD; ++j) {
         const int row = ld_row0 + j * RPL;
-        to_lds(kt + (uint32_t)(row * in.k_stride + k_col(row)), dst + j * 512);
-        to_lds(vt + (uint32_t)(row * in.v_stride + v_col), dst + TILE + j * 512);
+        to_lds(from + (uint32_t)(row * stride + (kV ? v_col : k_col(row))), dst + j * 512);
       }
     } else {  // (rows behind the end: the last key again)
 #pragma unroll
       for (int j = 0; j < NLD; ++j) {
         const int row = ld_row0 + j * RPL, v = min(v0 + row, total - 1);
-        const size_t key = v >= first ? v - first + band : v;
-        to_lds(kbase + key * in.k_stride + k_col(row), dst + j * 512);
-        to_lds(vbase + key * in.v_stride + v_col, dst + TILE + j * 512);
+        to_lds(base + (size_t)(v >= first ? v - first + band : v) * stride + (kV ? v_col : k_col(row)), dst + j * 512);
       }
     }
   };
-  auto wait_loads = [] { __builtin_amdgcn_s_waitcnt((0x7 << 4) | (0xf << 8)); };  // vmcnt(0) alone
+  const std::false_type of_k;
+  const std::true_type of_v;
 
   // the lane's rows
   const int row_q = lq >> a.pack_log2, row_head = (kv * n_sub + sub) * pack + (lq & (pack - 1));
@@ -116,7 +126,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(HD == 1
   const int wave_q = q0 + 2 * wave * block_q;
   const bool idle = wave_q >= len;
   bf16x8 qf[2][DSTEPS];
-  int top[2], low[2];
+  int top[2];
 #pragma unroll
   for (int b = 0; b < 2; ++b) {
     const int i = wave_q + b * block_q + row_q;
@@ -124,7 +134,6 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(HD == 1
 #pragma unroll
     for (int st = 0; st < DSTEPS; ++st) qf[b][st] = as_bf16(ld16(qrow + st * 16));
     top[b] = i - band + first;
-    low[b] = top[b] - in.window + 1;
   }
   // of the wave: the last number that any of its rows sees, the one up to which all do; where the first row's window begins
   // and where the last one's does
@@ -143,104 +152,162 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(HD == 1
       for (int r = 0; r < 16; ++r) oacc[b][d][r] = 0.f;
   }
 
-  request(0, 0);
-  wait_loads();
-  __syncthreads();
   const int kswz = CPR == 16 ? (lq & 15) : ((lq >> 1) & 7);
   const int i16 = lane & 15;
   const int vswz = CPR == 16 ? ((i16 >> 2) << 2) : (((i16 >> 3) & 1) << 2);
   const int vchunk = 2 * ((lane >> 4) & 1) + ((i16 & 3) >> 1);
-  for (int tile = 0; tile < n_tiles; ++tile) {
-    const int v0 = tile * kWinKeys;
-    const uint16_t* ks = win_lds + (tile & 1) * BUF;
-    const uint16_t* vs = ks + TILE;
-    if (tile + 1 < n_tiles) request(v0 + kWinKeys, (tile + 1) & 1);
-    const bool none = idle || v0 > wave_top || (v0 + kWinKeys <= wave_low && v0 >= in.sinks);
-    if (!none) {
-      // ---- S^T = K Q^T ----
-      floatx16 s[2][2];
+  const int k_at = lq * HD, v_at = (4 * hl + (i16 >> 2)) * HD + (i16 & 1) * 4;
+  // The scores of a half tile (32 keys) are made while the half before it is brought to probabilities and multiplied with V: a
+  // matrix instruction takes the matrix unit 32 cycles and its wave 4, in the others the wave's vector instructions go on.
+  // There is one wave a SIMD (its rows' registers are 400), so nothing else would.  Each slot below is a matrix instruction,
+  // the LDS reads of one that follows and a piece of the softmax, and fences keep the compiler from undoing it.
+  float most[2];
+  auto read_k = [&](const uint16_t* buf, int from, int st) __attribute__((always_inline)) {
+    return as_bf16(ld16(buf + (k_at + ((2 * st + hl) ^ kswz) * 8 + from * HD)));
+  };
+  auto read_v = [&](uint16_t* buf, int from, int x, int d) __attribute__((always_inline)) {
+    typedef short short4v __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) short4v* lds_short4_ptr;
+    const int at = v_at + ((4 * d + vchunk) ^ vswz) * 8 + (from + x * 16) * HD;
+    const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_ptr)(buf + at)));
+    const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_ptr)(buf + (at + 8 * HD))));
+    return as_bf16(u32x4{lo[0], lo[1], hi[0], hi[1]});
+  };
+  const floatx16 zero = {};
+  auto step = [&](floatx16 (&cur)[2], floatx16 (&nxt)[2], const uint16_t* k_buf, int k_from, uint16_t* v_buf, int v_from) __attribute__((always_inline)) {
+    constexpr int NS = 2 * DSTEPS, NP = 4 * DT;   // slots of either product
+    constexpr int kAhead = 3;                     // operands
+    constexpr int kPairSlots = NS + 2 * DT;       // all of P is there before the slots of its second half
+    bf16x8 kf[DSTEPS], vf[2 * DT];
+    u32x4 pw[2][2];  // pw[b][x]: column operand of the step over 16 keys
+    float sum[2] = {0.f, 0.f};
+    const float mb[2] = {m_run[0] * a.scale_log2e, m_run[1] * a.scale_log2e};
+    bf16x2 ones;
+    ones[0] = (__bf16)1.f;
+    ones[1] = (__bf16)1.f;
+    auto pair = [&](int p) __attribute__((always_inline)) {  // probabilities 2 (p % 4) and the next of keys 16 x .. of block b; rounded to bf16, 2^-9 of each at
+      const int x = p / 8, b = p / 4 % 2, r = 8 * x + 2 * (p % 4);  // most: the sum counts what the second product multiplies
+      bf16x2 v;
+      v[0] = (__bf16)__builtin_amdgcn_exp2f(cur[b][r] * a.scale_log2e - mb[b]);
+      v[1] = (__bf16)__builtin_amdgcn_exp2f(cur[b][r + 1] * a.scale_log2e - mb[b]);
+      sum[b] = __builtin_amdgcn_fdot2_f32_bf16(v, ones, sum[b], false);
+      pw[b][x][p % 4] = __builtin_bit_cast(uint32_t, v);
+    };
 #pragma unroll
-      for (int b = 0; b < 2; ++b)
+    for (int st = 0; st < kAhead; ++st) kf[st] = read_k(k_buf, k_from, st);
+    __builtin_amdgcn_sched_barrier(0);
+    pair(0);
+    __builtin_amdgcn_sched_barrier(0);
+    float top_of[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) s[b][u][r] = 0.f;
-#pragma unroll
-      for (int st = 0; st < DSTEPS; ++st)
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          const bf16x8 kf = as_bf16(ld16(ks + (32 * u + lq) * HD + ((2 * st + hl) ^ kswz) * 8));
-#pragma unroll
-          for (int b = 0; b < 2; ++b) s[b][u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[b][st], s[b][u], 0, 0, 0);
-        }
-      // ---- masks; element r of half u is number v0 + 32 u + 8 (r / 4) + 4 hl + r % 4 ----
-      if (v0 + kWinKeys - 1 > least_top || (v0 < most_low && v0 + kWinKeys > in.sinks)) {
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-          for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-              const int v = v0 + u * 32 + (r >> 2) * 8 + hl * 4 + (r & 3);
-              if (v > top[b] || (v < low[b] && v >= in.sinks)) s[b][u][r] = -INFINITY;
-            }
+    for (int slot = 0; slot < NS + NP; ++slot) {
+      const int b = slot % 2;
+      if (slot < NS) {
+        const int st = slot / 2;
+        nxt[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[st], qf[b][st], st == 0 ? zero : nxt[b], 0, 0, 0);
+        if (b == 0 && st + kAhead < DSTEPS) kf[st + kAhead] = read_k(k_buf, k_from, st + kAhead);
+      } else {
+        const int f = (slot - NS) / 2, x = f / DT, d = f % DT;
+        oacc[b][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[f], as_bf16(pw[b][x]), oacc[b][d], 0, 0, 0);
       }
-      u32x4 pw[2][4];  // pw[b][2 u + x]: column operand of the step over 16 keys
+      if (b == 0) {
+        const int f = (slot - NS + 2 * kAhead) / 2;
+        if (slot - NS + 2 * kAhead >= 0 && f < 2 * DT) vf[f] = read_v(v_buf, v_from, f / DT, f % DT);
+      }
+#pragma unroll
+      for (int p = 1; p < 16; ++p)
+        if ((p - 1) * kPairSlots / 15 == slot) pair(p);
+      if (slot >= kPairSlots) {  // the maximum of the new scores in the last slots
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (e * (2 * DT) / 16 == slot - kPairSlots)
+            top_of[e / 8] = fmaxf(fmaxf(top_of[e / 8], nxt[e / 8][2 * (e % 8)]), nxt[e / 8][2 * (e % 8) + 1]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      l_run[b] += sum[b];
+      most[b] = top_of[b];
+    }
+  };
+  // What the next half's scores still need: masks (element r is number v0 + 8 (r / 4) + 4 hl + r % 4) and, now and then, another
+  // reference point.  It only has to keep the exponentials in range, so it moves when some row's maximum grew by more than
+  // kWinSlack in the exponent.
+  auto settle = [&](floatx16 (&nxt)[2], int half) __attribute__((always_inline)) {
+    const int v0 = 32 * half;
+    if (v0 + 31 > least_top || (v0 < most_low && v0 + 32 > in.sinks)) {
+      const int at = v0 + 4 * hl, sinks = in.sinks - at;
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
-        float most = -INFINITY;
+        const int last = top[b] - at, from = last - in.window + 1;
+        most[b] = -INFINITY;
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) most = fmaxf(most, s[b][u][r]);
-        most = lane_op<32>(most, MaxOp());
-        // The reference point only has to keep the exponentials in range: it moves when some row's maximum grew by more than
-        // kWinSlack in the exponent.
-        if (__builtin_amdgcn_ballot_w64(most * a.scale_log2e > m_run[b] * a.scale_log2e + kWinSlack) != 0) {
-          const float m_new = fmaxf(m_run[b], most);
-          const float alpha = __builtin_amdgcn_exp2f((m_run[b] - m_new) * a.scale_log2e);
-          l_run[b] *= alpha;
-          m_run[b] = m_new;
-#pragma unroll
-          for (int d = 0; d < DT; ++d)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) oacc[b][d][r] *= alpha;
+        for (int r = 0; r < 16; ++r) {
+          const int v = (r >> 2) * 8 + (r & 3);
+          const bool hidden = (v > last) | ((v < from) & (v >= sinks));
+          nxt[b][r] = hidden ? -INFINITY : nxt[b][r];
+          most[b] = fmaxf(most[b], nxt[b][r]);
         }
-        const float mb = m_run[b] * a.scale_log2e;
-        float sum = 0.f;
-        bf16x2 ones;
-        ones[0] = (__bf16)1.f;
-        ones[1] = (__bf16)1.f;
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-          for (int r = 0; r < 16; r += 2) {
-            bf16x2 p;  // (rounded to bf16, 2^-9 of each at most: the sum counts what the second product multiplies)
-            p[0] = (__bf16)__builtin_amdgcn_exp2f(s[b][u][r] * a.scale_log2e - mb);
-            p[1] = (__bf16)__builtin_amdgcn_exp2f(s[b][u][r + 1] * a.scale_log2e - mb);
-            sum = __builtin_amdgcn_fdot2_f32_bf16(p, ones, sum, false);
-            pw[b][2 * u + (r >> 3)][(r & 7) >> 1] = __builtin_bit_cast(uint32_t, p);
-          }
-        l_run[b] += sum;
       }
-      // ---- O^T += V^T P^T; step x of half u contracts keys 32 u + 16 x + {0..3, 8..11} + 4 hl ----
-      const uint16_t* vfrag = vs + (4 * hl + (i16 >> 2)) * HD + (i16 & 1) * 4;
-#pragma unroll
-      for (int x = 0; x < 4; ++x)
-#pragma unroll
-        for (int d = 0; d < DT; ++d) {
-          typedef short short4v __attribute__((ext_vector_type(4)));
-          typedef __attribute__((address_space(3))) short4v* lds_short4_ptr;
-          const int col = ((4 * d + vchunk) ^ vswz) * 8;
-          const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_ptr)(vfrag + x * 16 * HD + col)));
-          const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_ptr)(vfrag + (x * 16 + 8) * HD + col)));
-          const bf16x8 vf = as_bf16(u32x4{lo[0], lo[1], hi[0], hi[1]});
-#pragma unroll
-          for (int b = 0; b < 2; ++b) oacc[b][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, as_bf16(pw[b][x]), oacc[b][d], 0, 0, 0);
-        }
     }
-    wait_loads();
-    __syncthreads();
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const float m = lane_op<32>(most[b], MaxOp());
+      if (__builtin_amdgcn_ballot_w64(m * a.scale_log2e > m_run[b] * a.scale_log2e + kWinSlack) != 0) {
+        const float m_new = fmaxf(m_run[b], m);
+        const float alpha = __builtin_amdgcn_exp2f((m_run[b] - m_new) * a.scale_log2e);
+        l_run[b] *= alpha;
+        m_run[b] = m_new;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) oacc[b][d][r] *= alpha;
+      }
+    }
+  };
+  // Loads: in turn K of the tile after next, when this tile's K is done with (in the middle of an iteration), and V of the next
+  // one, when the last one's is (at its beginning).  Each is waited for an iteration later, with the other still on its way.
+  floatx16 even[2], odd[2];
+  request(0, of_k, k_lds0);
+  request(0, of_v, v_lds0);
+  request(1, of_k, k_lds1);
+  wait_all_but<0>();
+  lds_barrier();
+#pragma unroll
+  for (int st = 0; st < DSTEPS; ++st) {
+    const bf16x8 kf = read_k(k_lds0, 0, st);
+#pragma unroll
+    for (int b = 0; b < 2; ++b) even[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[b][st], st == 0 ? zero : even[b], 0, 0, 0);
+  }
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+    most[b] = -INFINITY;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) most[b] = fmaxf(most[b], even[b][r]);
+  }
+  settle(even, 0);
+  auto one_tile = [&](int tile, uint16_t* k_now, uint16_t* k_then, uint16_t* v_now, uint16_t* v_then) __attribute__((always_inline)) {
+    // V of this tile is there (and K of the next on its way)
+    if (tile + 1 < n_tiles) wait_all_but<NLD>();
+    else wait_all_but<0>();
+    lds_barrier();
+    request(tile + 1, of_v, v_then);
+    step(even, odd, k_now, 32, v_now, 0);
+    settle(odd, 2 * tile + 1);
+    // K of the next is there (and V of the next on its way)
+    if (tile + 1 < n_tiles) wait_all_but<NLD>();
+    lds_barrier();
+    request(tile + 2, of_k, k_now);
+    // (behind the last tile: of what the buffer holds, and nobody uses it)
+    step(odd, even, k_then, 0, v_now, 32);
+    settle(even, 2 * tile + 2);
+  };
+  for (int tile = 0;; tile += 2) {
+    one_tile(tile, k_lds0, k_lds1, v_lds0, v_lds1);
+    if (tile + 1 >= n_tiles) break;
+    one_tile(tile + 1, k_lds1, k_lds0, v_lds1, v_lds0);
+    if (tile + 2 >= n_tiles) break;
   }
   if (idle) return;
 
@@ -339,9 +406,7 @@ bool window_attention_fits(const WindowRows& r) { return window_plan(r).blocks <
 
 template <int HD, int NW>
 static hipError_t launch_window(const WindowArgs& a, hipStream_t stream) {
-  constexpr int kLds = 2 * 2 * kWinKeys * HD * (int)sizeof(uint16_t);
-  (void)KernelAttrReg<window_attention_kernel<HD, NW>, kLds>::done;
-  hipLaunchKernelGGL((window_attention_kernel<HD, NW>), dim3((unsigned)(8 * a.per_xcd)), dim3(64 * NW), kLds, stream, a);
+  hipLaunchKernelGGL((window_attention_kernel<HD, NW>), dim3((unsigned)(8 * a.per_xcd)), dim3(64 * NW), 0, stream, a);
   return hipGetLastError();
 }
 
