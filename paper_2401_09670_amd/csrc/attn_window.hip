@@ -40,8 +40,8 @@ __device__ __forceinline__ void wait_all_but() {  // vmcnt(N) alone: N in bits 3
   __builtin_amdgcn_s_waitcnt((N & 0xf) | (N >> 4) << 14 | 0x7 << 4 | 0xf << 8);
 }
 
-template <int HD, int NW>
-__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(HD == 128 ? 1 : 2))) void window_attention_kernel(
+template <int HD, int NW, int RB>
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(RB == 2 && HD == 128 ? 1 : 2))) void window_attention_kernel(
     const WindowArgs a) {
   constexpr int DSTEPS = HD / 16, DT = HD / 32, CPR = HD / 8;
   constexpr int TILE = kWinKeys * HD;
@@ -59,7 +59,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(HD == 1
   const int n_sub = a.kv_group >> a.pack_log2;
   const int sub = id % n_sub, kv = id / n_sub / a.places;
   const int place = id / n_sub % a.places;
-  const int pack = 1 << a.pack_log2, queries = (64 * NW) >> a.pack_log2;
+  const int pack = 1 << a.pack_log2, queries = (32 * RB * NW) >> a.pack_log2;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   int upto = 0;  // sequences that begin at this place or before
@@ -78,7 +78,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(HD == 1
   const int band = max(q0 - in.window + 1, 0);
   const int first = min(in.sinks, band);        // number `first` is key `band`
   const int total = q_end - band + first;
-  const int n_tiles = (total + kWinKeys - 1) / kWinKeys;
+  const int n_halves = (total + 31) / 32;
 
   const int hl = lane >> 5, lq = lane & 31;
   const uint16_t* kbase = in.k + (size_t)start * in.k_stride + (size_t)kv * HD;
@@ -91,23 +91,29 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(HD == 1
   const int ld_row0 = wave * NLD * RPL + ld_sub;
   auto k_col = [&](int row) __attribute__((always_inline)) { return (ld_c ^ (CPR == 16 ? row & 15 : (row >> 1) & 7)) * 8; };
   const int v_col = (ld_c ^ (CPR == 16 ? ld_sub << 2 : ((ld_sub >> 1) & 1) << 2)) * 8;
-  auto to_lds = [&](const uint16_t* from, uint16_t* to) __attribute__((always_inline)) {
+  uint32_t k_off[NLD];  // bytes from the first row of a load
+#pragma unroll
+  for (int j = 0; j < NLD; ++j) k_off[j] = 2 * (uint32_t)(ld_sub * in.k_stride + k_col(ld_row0 + j * RPL));
+  const uint32_t v_off = 2 * (uint32_t)(ld_sub * in.v_stride + v_col);
+  auto to_lds = [&](const void* from, uint16_t* to) __attribute__((always_inline)) {
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
                                      (__attribute__((address_space(3))) void*)to, 16, 0, 0);
   };
-  // Tile `tile` of K or of V into its buffer; behind the last tile nothing.  Always NLD loads or none.
+  // Tile `tile` of K or of V into its buffer, in NLD loads; behind the last tile there are none, and all others are waited for:
+  // whoever waits for all but NLD has then waited for what came before.
   auto request = [&](int tile, auto of_v, uint16_t* dst) __attribute__((always_inline)) {
     constexpr bool kV = decltype(of_v)::value;
     const uint16_t* base = kV ? vbase : kbase;
     const int stride = kV ? in.v_stride : in.k_stride, v0 = tile * kWinKeys;
-    if (tile >= n_tiles) return;
+    if (v0 >= total) return wait_all_but<0>();
     dst += wave * NLD * 512;
-    if ((v0 >= first || v0 + kWinKeys <= first) && v0 + kWinKeys <= total) {
-      const uint16_t* from = base + (size_t)(v0 >= first ? v0 - first + band : v0) * stride;
+    if ((v0 >= first || v0 + kWinKeys <= first) && v0 + kWinKeys <= total) {  // a scalar base and 32 bits a lane
+      const char* from = reinterpret_cast<const char*>(base) + 2 * (size_t)((v0 >= first ? v0 - first + band : v0) + wave * NLD * RPL) * stride;
 #pragma unroll
       for (int j = 0; j < NLD; ++j) {
-        const int row = ld_row0 + j * RPL;
-        to_lds(from + (uint32_t)(row * stride + (kV ? v_col : k_col(row))), dst + j * 512);
+        uint32_t off = kV ? v_off : k_off[j];
+        asm("" : "+v"(off));  // (else its sum with the base is kept for the loop, in 64 bits a lane)
+        to_lds(from + 2 * (size_t)(j * RPL) * stride + off, dst + j * 512);
       }
     } else {  // (rows behind the end: the last key again)
 #pragma unroll
@@ -123,12 +129,12 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(HD == 1
   // the lane's rows
   const int row_q = lq >> a.pack_log2, row_head = (kv * n_sub + sub) * pack + (lq & (pack - 1));
   const int block_q = 32 >> a.pack_log2;        // queries of a block of rows
-  const int wave_q = q0 + 2 * wave * block_q;
+  const int wave_q = q0 + RB * wave * block_q;
   const bool idle = wave_q >= len;
-  bf16x8 qf[2][DSTEPS];
-  int top[2];
+  bf16x8 qf[RB][DSTEPS];
+  int top[RB];
 #pragma unroll
-  for (int b = 0; b < 2; ++b) {
+  for (int b = 0; b < RB; ++b) {
     const int i = wave_q + b * block_q + row_q;
     const uint16_t* qrow = in.q + ((size_t)start + min(i, len - 1)) * in.q_stride + (size_t)row_head * HD + hl * 8;
 #pragma unroll
@@ -137,13 +143,17 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(HD == 1
   }
   // of the wave: the last number that any of its rows sees, the one up to which all do; where the first row's window begins
   // and where the last one's does
-  const int wave_top = wave_q + 2 * block_q - 1 - band + first, least_top = wave_q - band + first;
+  const int wave_top = wave_q + RB * block_q - 1 - band + first, least_top = wave_q - band + first;
   const int wave_low = least_top - in.window + 1, most_low = wave_top - in.window + 1;
+  auto half_seen = [&](int half) __attribute__((always_inline)) {  // whether any of the rows sees any of the 32 keys
+    const int v0 = 32 * half;
+    return v0 <= wave_top && (v0 + 32 > wave_low || v0 < in.sinks) && half < n_halves && !idle;
+  };
 
-  floatx16 oacc[2][DT];
-  float m_run[2], l_run[2];
+  floatx16 oacc[RB][DT];
+  float m_run[RB], l_run[RB];
 #pragma unroll
-  for (int b = 0; b < 2; ++b) {
+  for (int b = 0; b < RB; ++b) {
     m_run[b] = kLowestScore;
     l_run[b] = 0.f;
 #pragma unroll
@@ -161,7 +171,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(HD == 1
   // matrix instruction takes the matrix unit 32 cycles and its wave 4, in the others the wave's vector instructions go on.
   // There is one wave a SIMD (its rows' registers are 400), so nothing else would.  Each slot below is a matrix instruction,
   // the LDS reads of one that follows and a piece of the softmax, and fences keep the compiler from undoing it.
-  float most[2];
+  float most[RB];
   auto read_k = [&](const uint16_t* buf, int from, int st) __attribute__((always_inline)) {
     return as_bf16(ld16(buf + (k_at + ((2 * st + hl) ^ kswz) * 8 + from * HD)));
   };
@@ -174,59 +184,71 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(HD == 1
     return as_bf16(u32x4{lo[0], lo[1], hi[0], hi[1]});
   };
   const floatx16 zero = {};
-  auto step = [&](floatx16 (&cur)[2], floatx16 (&nxt)[2], const uint16_t* k_buf, int k_from, uint16_t* v_buf, int v_from) __attribute__((always_inline)) {
-    constexpr int NS = 2 * DSTEPS, NP = 4 * DT;   // slots of either product
-    constexpr int kAhead = 3;                     // operands
-    constexpr int kPairSlots = NS + 2 * DT;       // all of P is there before the slots of its second half
-    bf16x8 kf[DSTEPS], vf[2 * DT];
-    u32x4 pw[2][2];  // pw[b][x]: column operand of the step over 16 keys
-    float sum[2] = {0.f, 0.f};
-    const float mb[2] = {m_run[0] * a.scale_log2e, m_run[1] * a.scale_log2e};
-    bf16x2 ones;
-    ones[0] = (__bf16)1.f;
-    ones[1] = (__bf16)1.f;
-    auto pair = [&](int p) __attribute__((always_inline)) {  // probabilities 2 (p % 4) and the next of keys 16 x .. of block b; rounded to bf16, 2^-9 of each at
-      const int x = p / 8, b = p / 4 % 2, r = 8 * x + 2 * (p % 4);  // most: the sum counts what the second product multiplies
-      bf16x2 v;
-      v[0] = (__bf16)__builtin_amdgcn_exp2f(cur[b][r] * a.scale_log2e - mb[b]);
-      v[1] = (__bf16)__builtin_amdgcn_exp2f(cur[b][r + 1] * a.scale_log2e - mb[b]);
-      sum[b] = __builtin_amdgcn_fdot2_f32_bf16(v, ones, sum[b], false);
-      pw[b][x][p % 4] = __builtin_bit_cast(uint32_t, v);
+  auto step = [&](floatx16 (&cur)[RB], floatx16 (&nxt)[RB], const uint16_t* k_buf, int k_from, uint16_t* v_buf,
+                  int v_from) __attribute__((always_inline)) {
+    constexpr int NS = RB * DSTEPS, NP = 2 * RB * DT, kPairs = 8 * RB;  // slots of either product, pairs of probabilities
+    constexpr int kGroup = 4;                  // operands that are read, and waited for, together
+    constexpr int kFirst = 2;                  // pairs before the first slot
+    constexpr int kPairSlots = NS + RB * DT;   // all of P is there before the slots of its second half
+    bf16x8 op[DSTEPS + 2 * DT];
+    u32x4 pw[RB][2];  // pw[b][x]: column operand of the step over 16 keys
+    float sum[RB], mb[RB], top_of[RB];
+#pragma unroll
+    for (int b = 0; b < RB; ++b) {
+      sum[b] = 0.f;
+      mb[b] = m_run[b] * a.scale_log2e;
+      top_of[b] = -INFINITY;
+    }
+    auto read = [&](int f) __attribute__((always_inline)) {
+      op[f] = f < DSTEPS ? read_k(k_buf, k_from, f) : read_v(v_buf, v_from, (f - DSTEPS) / DT, (f - DSTEPS) % DT);
+    };
+    // Probabilities 2 (p % 4) and the next of keys 16 x .. of block b; rounded to bf16, 2^-9 of each at most.
+    auto pair = [&](int p) __attribute__((always_inline)) {
+      const int x = p / (4 * RB), b = p / 4 % RB, r = 8 * x + 2 * (p % 4);
+      const float p0 = __builtin_amdgcn_exp2f(cur[b][r] * a.scale_log2e - mb[b]);
+      const float p1 = __builtin_amdgcn_exp2f(cur[b][r + 1] * a.scale_log2e - mb[b]);
+      sum[b] += p0;
+      sum[b] += p1;
+      asm volatile("" : "+v"(sum[b]));  // (here, not where the sum is used)
+      pw[b][x][p % 4] = pack_bf16(p0, p1);
     };
 #pragma unroll
-    for (int st = 0; st < kAhead; ++st) kf[st] = read_k(k_buf, k_from, st);
+    for (int f = 0; f < kGroup; ++f) read(f);
     __builtin_amdgcn_sched_barrier(0);
-    pair(0);
+#pragma unroll
+    for (int p = 0; p < kFirst; ++p) pair(p);
     __builtin_amdgcn_sched_barrier(0);
-    float top_of[2] = {-INFINITY, -INFINITY};
 #pragma unroll
     for (int slot = 0; slot < NS + NP; ++slot) {
-      const int b = slot % 2;
+      const int b = slot % RB, f = slot / RB;
       if (slot < NS) {
-        const int st = slot / 2;
-        nxt[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[st], qf[b][st], st == 0 ? zero : nxt[b], 0, 0, 0);
-        if (b == 0 && st + kAhead < DSTEPS) kf[st + kAhead] = read_k(k_buf, k_from, st + kAhead);
+        nxt[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[f], qf[b][f], f == 0 ? zero : nxt[b], 0, 0, 0);
       } else {
-        const int f = (slot - NS) / 2, x = f / DT, d = f % DT;
-        oacc[b][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[f], as_bf16(pw[b][x]), oacc[b][d], 0, 0, 0);
+        const int x = (f - DSTEPS) / DT, d = (f - DSTEPS) % DT;
+        oacc[b][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[f], as_bf16(pw[b][x]), oacc[b][d], 0, 0, 0);
       }
-      if (b == 0) {
-        const int f = (slot - NS + 2 * kAhead) / 2;
-        if (slot - NS + 2 * kAhead >= 0 && f < 2 * DT) vf[f] = read_v(v_buf, v_from, f / DT, f % DT);
+      if (b == 0 && f % kGroup < 2) {  // the next group's operands, half of them each time
+#pragma unroll
+        for (int e = 0; e < kGroup / 2; ++e) {
+          const int g = (f / kGroup + 1) * kGroup + f % kGroup * (kGroup / 2) + e;
+          if (g < DSTEPS + 2 * DT) read(g);
+        }
       }
 #pragma unroll
-      for (int p = 1; p < 16; ++p)
-        if ((p - 1) * kPairSlots / 15 == slot) pair(p);
+      for (int p = kFirst; p < kPairs; ++p)
+        if ((p - kFirst) * kPairSlots / (kPairs - kFirst) == slot) pair(p);
       if (slot >= kPairSlots) {  // the maximum of the new scores in the last slots
 #pragma unroll
-        for (int e = 0; e < 16; ++e)
-          if (e * (2 * DT) / 16 == slot - kPairSlots)
+        for (int e = 0; e < kPairs; ++e)
+          if (e * (RB * DT) / kPairs == slot - kPairSlots) {
             top_of[e / 8] = fmaxf(fmaxf(top_of[e / 8], nxt[e / 8][2 * (e % 8)]), nxt[e / 8][2 * (e % 8) + 1]);
+            asm volatile("" : "+v"(top_of[e / 8]));
+          }
       }
       __builtin_amdgcn_sched_barrier(0);
     }
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
+    for (int b = 0; b < RB; ++b) {
       l_run[b] += sum[b];
       most[b] = top_of[b];
     }
@@ -234,12 +256,12 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(HD == 1
   // What the next half's scores still need: masks (element r is number v0 + 8 (r / 4) + 4 hl + r % 4) and, now and then, another
   // reference point.  It only has to keep the exponentials in range, so it moves when some row's maximum grew by more than
   // kWinSlack in the exponent.
-  auto settle = [&](floatx16 (&nxt)[2], int half) __attribute__((always_inline)) {
+  auto settle = [&](floatx16 (&nxt)[RB], int half) __attribute__((always_inline)) {
     const int v0 = 32 * half;
     if (v0 + 31 > least_top || (v0 < most_low && v0 + 32 > in.sinks)) {
       const int at = v0 + 4 * hl, sinks = in.sinks - at;
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
+      for (int b = 0; b < RB; ++b) {
         const int last = top[b] - at, from = last - in.window + 1;
         most[b] = -INFINITY;
 #pragma unroll
@@ -252,7 +274,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(HD == 1
       }
     }
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
+    for (int b = 0; b < RB; ++b) {
       const float m = lane_op<32>(most[b], MaxOp());
       if (__builtin_amdgcn_ballot_w64(m * a.scale_log2e > m_run[b] * a.scale_log2e + kWinSlack) != 0) {
         const float m_new = fmaxf(m_run[b], m);
@@ -268,52 +290,68 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(HD == 1
   };
   // Loads: in turn K of the tile after next, when this tile's K is done with (in the middle of an iteration), and V of the next
   // one, when the last one's is (at its beginning).  Each is waited for an iteration later, with the other still on its way.
-  floatx16 even[2], odd[2];
+  floatx16 even[RB], odd[RB];
   request(0, of_k, k_lds0);
   request(0, of_v, v_lds0);
   request(1, of_k, k_lds1);
   wait_all_but<0>();
   lds_barrier();
+  const floatx16 none = {-INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY,
+                         -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY};
+  auto scores = [&](floatx16 (&to)[RB]) __attribute__((always_inline)) {
 #pragma unroll
-  for (int st = 0; st < DSTEPS; ++st) {
-    const bf16x8 kf = read_k(k_lds0, 0, st);
+    for (int st = 0; st < DSTEPS; ++st) {
+      const bf16x8 kf = read_k(k_lds0, 0, st);
 #pragma unroll
-    for (int b = 0; b < 2; ++b) even[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[b][st], st == 0 ? zero : even[b], 0, 0, 0);
-  }
+      for (int b = 0; b < RB; ++b) to[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[b][st], st == 0 ? zero : to[b], 0, 0, 0);
+    }
 #pragma unroll
-  for (int b = 0; b < 2; ++b) {
-    most[b] = -INFINITY;
+    for (int b = 0; b < RB; ++b) {
+      most[b] = -INFINITY;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) most[b] = fmaxf(most[b], even[b][r]);
-  }
-  settle(even, 0);
-  auto one_tile = [&](int tile, uint16_t* k_now, uint16_t* k_then, uint16_t* v_now, uint16_t* v_then) __attribute__((always_inline)) {
-    // V of this tile is there (and K of the next on its way)
-    if (tile + 1 < n_tiles) wait_all_but<NLD>();
-    else wait_all_but<0>();
-    lds_barrier();
-    request(tile + 1, of_v, v_then);
-    step(even, odd, k_now, 32, v_now, 0);
-    settle(odd, 2 * tile + 1);
-    // K of the next is there (and V of the next on its way)
-    if (tile + 1 < n_tiles) wait_all_but<NLD>();
-    lds_barrier();
-    request(tile + 2, of_k, k_now);
-    // (behind the last tile: of what the buffer holds, and nobody uses it)
-    step(odd, even, k_then, 0, v_now, 32);
-    settle(even, 2 * tile + 2);
+      for (int r = 0; r < 16; ++r) most[b] = fmaxf(most[b], to[b][r]);
+    }
   };
-  for (int tile = 0;; tile += 2) {
-    one_tile(tile, k_lds0, k_lds1, v_lds0, v_lds1);
-    if (tile + 1 >= n_tiles) break;
-    one_tile(tile + 1, k_lds1, k_lds0, v_lds1, v_lds0);
-    if (tile + 2 >= n_tiles) break;
+  // Half `half` from scores to output, and the scores of the next; where the wave's rows see neither, the next are scores of
+  // nothing.
+  auto advance = [&](floatx16 (&cur)[RB], floatx16 (&nxt)[RB], int half, const uint16_t* k_buf, int k_from, uint16_t* v_buf,
+                     int v_from) __attribute__((always_inline)) {
+    if (half_seen(half) || half_seen(half + 1)) {
+      step(cur, nxt, k_buf, k_from, v_buf, v_from);
+      settle(nxt, half + 1);
+    } else {
+#pragma unroll
+      for (int b = 0; b < RB; ++b) nxt[b] = none;
+    }
+  };
+  scores(even);
+  settle(even, 0);
+  auto one_tile = [&](int half, uint16_t* k_now, uint16_t* k_then, uint16_t* v_now, uint16_t* v_then) __attribute__((always_inline)) {
+    // V of this tile is there (and K of the next on its way)
+    wait_all_but<NLD>();
+    lds_barrier();
+    request(half / 2 + 1, of_v, v_then);
+    advance(even, odd, half, k_now, 32, v_now, 0);
+    if (half + 1 >= n_halves) return;
+    // K of the next is there (and V of the next on its way)
+    wait_all_but<NLD>();
+    lds_barrier();
+    request(half / 2 + 2, of_k, k_now);
+    // (behind the last tile: of what the buffer holds, and all of it is masked)
+    advance(odd, even, half + 1, k_then, 0, v_now, 32);
+  };
+  for (int half = 0;; half += 4) {
+    one_tile(half, k_lds0, k_lds1, v_lds0, v_lds1);
+    if (half + 2 >= n_halves) break;
+    one_tile(half + 2, k_lds1, k_lds0, v_lds1, v_lds0);
+    if (half + 4 >= n_halves) break;
   }
+  wait_all_but<0>();  // (nothing may land when others have the memory)
   if (idle) return;
 
   // ---- the quotient; lane holds O[row][32 d + 8 g + 4 hl + i] ----
 #pragma unroll
-  for (int b = 0; b < 2; ++b) {
+  for (int b = 0; b < RB; ++b) {
     const int i = wave_q + b * block_q + row_q;
     const float l = lane_op<32>(l_run[b], AddOp());
     const float inv = l == 0.f ? 0.f : 1.f / l;  // (every score below fp32's range: 0)
@@ -391,22 +429,23 @@ static int pack_log2_of(int kv_group) {
 }
 
 struct WindowPlan {
-  int waves, pack_log2;
+  int waves, row_blocks, pack_log2;
   long places, blocks;
 };
 static WindowPlan window_plan(const WindowRows& r) {
   WindowPlan p;
-  p.waves = 2;
+  p.waves = 4;
+  p.row_blocks = 1;
   p.pack_log2 = pack_log2_of(r.n_heads / r.n_kv_heads);
-  p.places = (long)r.t / ((64 * p.waves) >> p.pack_log2) + r.B;
+  p.places = (long)r.t / ((32 * p.row_blocks * p.waves) >> p.pack_log2) + r.B;
   p.blocks = p.places * (r.n_heads >> p.pack_log2);
   return p;
 }
 bool window_attention_fits(const WindowRows& r) { return window_plan(r).blocks <= 0x7fffffffL / 256 - 8; }
 
-template <int HD, int NW>
+template <int HD, int NW, int RB>
 static hipError_t launch_window(const WindowArgs& a, hipStream_t stream) {
-  hipLaunchKernelGGL((window_attention_kernel<HD, NW>), dim3((unsigned)(8 * a.per_xcd)), dim3(64 * NW), 0, stream, a);
+  hipLaunchKernelGGL((window_attention_kernel<HD, NW, RB>), dim3((unsigned)(8 * a.per_xcd)), dim3(64 * NW), 0, stream, a);
   return hipGetLastError();
 }
 
@@ -422,8 +461,8 @@ hipError_t launch_window_attention(const WindowRows& r, int head_dim, hipStream_
   a.blocks = (int)p.blocks;
   a.per_xcd = (int)((p.blocks + 7) / 8);
   a.scale_log2e = 1.4426950408889634f / sqrtf((float)head_dim);
-  if (head_dim == 128) return launch_window<128, 2>(a, stream);
-  if (head_dim == 64) return launch_window<64, 2>(a, stream);
+  if (head_dim == 128) return launch_window<128, 4, 1>(a, stream);
+  if (head_dim == 64) return launch_window<64, 4, 1>(a, stream);
   return hipErrorInvalidValue;
 }
 
