@@ -58,18 +58,24 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(RB == 2
   const WindowRows& in = a.r;
   const int n_sub = a.kv_group >> a.pack_log2;
   const int sub = id % n_sub, kv = id / n_sub / a.places;
-  const int place = id / n_sub % a.places;
+  const int place = a.places - 1 - id / n_sub % a.places;  // (late ones first: their windows are full)
   const int pack = 1 << a.pack_log2, queries = (32 * RB * NW) >> a.pack_log2;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  int upto = 0;  // sequences that begin at this place or before
+  // The sequence whose place this is: the last that begins here or before.  (Its bounds out of the lanes that looked for it: not
+  // another load to wait for.)
+  int seq = -1, start = 0, end = 0;
   for (int i0 = 0; i0 < in.B; i0 += 64) {
-    const int i = i0 + lane;
-    upto += __builtin_popcountll(__builtin_amdgcn_ballot_w64(i < in.B && in.cu_seqlens[min(i, in.B - 1)] / queries + i <= place));
+    const int i = min(i0 + lane, in.B - 1), from = in.cu_seqlens[i], upto = in.cu_seqlens[i + 1];
+    const uint64_t here = __builtin_amdgcn_ballot_w64(i0 + lane < in.B && from / queries + i <= place);
+    if (here == 0) break;
+    const int at = 63 - __builtin_clzll(here);
+    seq = i0 + at;
+    start = __builtin_amdgcn_readlane(from, at);
+    end = __builtin_amdgcn_readlane(upto, at);
   }
-  if (upto == 0) return;
-  const int seq = upto - 1, start = in.cu_seqlens[seq];
-  const int len = min(in.cu_seqlens[seq + 1] - start, in.max_seqlen);
+  if (seq < 0) return;
+  const int len = min(end - start, in.max_seqlen);
   const int q0 = (place - start / queries - seq) * queries;
   if (q0 >= len) return;
 
@@ -99,15 +105,14 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(RB == 2
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
                                      (__attribute__((address_space(3))) void*)to, 16, 0, 0);
   };
-  // Tile `tile` of K or of V into its buffer, in NLD loads; behind the last tile there are none, and all others are waited for:
-  // whoever waits for all but NLD has then waited for what came before.
-  auto request = [&](int tile, auto of_v, uint16_t* dst) __attribute__((always_inline)) {
+  // 64 keys from number v0 on, of K or of V, into a buffer.
+  auto request = [&](int v0, auto of_v, uint16_t* dst) __attribute__((always_inline)) {
     constexpr bool kV = decltype(of_v)::value;
     const uint16_t* base = kV ? vbase : kbase;
-    const int stride = kV ? in.v_stride : in.k_stride, v0 = tile * kWinKeys;
-    if (v0 >= total) return wait_all_but<0>();
+    const int stride = kV ? in.v_stride : in.k_stride;
+    if (v0 >= total) return;
     dst += wave * NLD * 512;
-    if ((v0 >= first || v0 + kWinKeys <= first) && v0 + kWinKeys <= total) {  // a scalar base and 32 bits a lane
+    if ((v0 >= first || v0 + kWinKeys <= first) && v0 >= 0 && v0 + kWinKeys <= total) {  // a scalar base and 32 bits a lane
       const char* from = reinterpret_cast<const char*>(base) + 2 * (size_t)((v0 >= first ? v0 - first + band : v0) + wave * NLD * RPL) * stride;
 #pragma unroll
       for (int j = 0; j < NLD; ++j) {
@@ -115,10 +120,10 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(RB == 2
         asm("" : "+v"(off));  // (else its sum with the base is kept for the loop, in 64 bits a lane)
         to_lds(from + 2 * (size_t)(j * RPL) * stride + off, dst + j * 512);
       }
-    } else {  // (rows behind the end: the last key again)
+    } else {  // (rows before the first and behind the last: those again)
 #pragma unroll
       for (int j = 0; j < NLD; ++j) {
-        const int row = ld_row0 + j * RPL, v = min(v0 + row, total - 1);
+        const int row = ld_row0 + j * RPL, v = min(max(v0 + row, 0), total - 1);
         to_lds(base + (size_t)(v >= first ? v - first + band : v) * stride + (kV ? v_col : k_col(row)), dst + j * 512);
       }
     }
@@ -141,14 +146,14 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(RB == 2
     for (int st = 0; st < DSTEPS; ++st) qf[b][st] = as_bf16(ld16(qrow + st * 16));
     top[b] = i - band + first;
   }
-  // of the wave: the last number that any of its rows sees, the one up to which all do; where the first row's window begins
-  // and where the last one's does
+  // Of the wave: the last number that any of its rows sees, the one up to which all do; where the first row's window begins
+  // and where the last one's does.  Then the halves (of a tile: 32 keys) that any of the rows sees, [0, sink_halves) and
+  // [from_half, upto_half), and those that need masks: from tail_half on, and in [sinks / 32, clear_half).
   const int wave_top = wave_q + RB * block_q - 1 - band + first, least_top = wave_q - band + first;
   const int wave_low = least_top - in.window + 1, most_low = wave_top - in.window + 1;
-  auto half_seen = [&](int half) __attribute__((always_inline)) {  // whether any of the rows sees any of the 32 keys
-    const int v0 = 32 * half;
-    return v0 <= wave_top && (v0 + 32 > wave_low || v0 < in.sinks) && half < n_halves && !idle;
-  };
+  const int sink_halves = idle ? 0 : (min(in.sinks, total) + 31) >> 5, from_half = wave_low >> 5;
+  const int upto_half = idle ? 0 : min((wave_top >> 5) + 1, n_halves);
+  const int tail_half = (least_top + 1) >> 5, clear_half = (most_low + 31) >> 5, seen_sinks = in.sinks >> 5;
 
   floatx16 oacc[RB][DT];
   float m_run[RB], l_run[RB];
@@ -258,7 +263,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(RB == 2
   // kWinSlack in the exponent.
   auto settle = [&](floatx16 (&nxt)[RB], int half) __attribute__((always_inline)) {
     const int v0 = 32 * half;
-    if (v0 + 31 > least_top || (v0 < most_low && v0 + 32 > in.sinks)) {
+    if (half >= tail_half || (half < clear_half && half >= seen_sinks)) {
       const int at = v0 + 4 * hl, sinks = in.sinks - at;
 #pragma unroll
       for (int b = 0; b < RB; ++b) {
@@ -288,12 +293,13 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(RB == 2
       }
     }
   };
-  // Loads: in turn K of the tile after next, when this tile's K is done with (in the middle of an iteration), and V of the next
-  // one, when the last one's is (at its beginning).  Each is waited for an iteration later, with the other still on its way.
+  // In an iteration a half's probabilities meet V while the scores of the half behind it are made, twice: so it reads halves
+  // 2 i and 2 i + 1 of V and 2 i + 1 and 2 i + 2 of K, and K's tiles lie half a tile behind V's.  Both land in the iteration
+  // before.  A barrier each.
   floatx16 even[RB], odd[RB];
-  request(0, of_k, k_lds0);
+  request(-32, of_k, k_lds1);
   request(0, of_v, v_lds0);
-  request(1, of_k, k_lds1);
+  request(32, of_k, k_lds0);
   wait_all_but<0>();
   lds_barrier();
   const floatx16 none = {-INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY,
@@ -301,7 +307,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(RB == 2
   auto scores = [&](floatx16 (&to)[RB]) __attribute__((always_inline)) {
 #pragma unroll
     for (int st = 0; st < DSTEPS; ++st) {
-      const bf16x8 kf = read_k(k_lds0, 0, st);
+      const bf16x8 kf = read_k(k_lds1, 32, st);
 #pragma unroll
       for (int b = 0; b < RB; ++b) to[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[b][st], st == 0 ? zero : to[b], 0, 0, 0);
     }
@@ -313,10 +319,10 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(RB == 2
     }
   };
   // Half `half` from scores to output, and the scores of the next; where the wave's rows see neither, the next are scores of
-  // nothing.
+  // nothing.  (Behind the last half they are of what the buffer holds, and all are masked.)
   auto advance = [&](floatx16 (&cur)[RB], floatx16 (&nxt)[RB], int half, const uint16_t* k_buf, int k_from, uint16_t* v_buf,
                      int v_from) __attribute__((always_inline)) {
-    if (half_seen(half) || half_seen(half + 1)) {
+    if (half < sink_halves || (half + 1 >= from_half && half < upto_half)) {
       step(cur, nxt, k_buf, k_from, v_buf, v_from);
       settle(nxt, half + 1);
     } else {
@@ -326,19 +332,14 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(RB == 2
   };
   scores(even);
   settle(even, 0);
+  lds_barrier();  // (the first iteration's loads land where these scores' keys were)
   auto one_tile = [&](int half, uint16_t* k_now, uint16_t* k_then, uint16_t* v_now, uint16_t* v_then) __attribute__((always_inline)) {
-    // V of this tile is there (and K of the next on its way)
-    wait_all_but<NLD>();
+    request(32 * half + 96, of_k, k_then);
+    request(32 * half + 64, of_v, v_then);
+    advance(even, odd, half, k_now, 0, v_now, 0);
+    advance(odd, even, half + 1, k_now, 32, v_now, 32);
+    wait_all_but<0>();
     lds_barrier();
-    request(half / 2 + 1, of_v, v_then);
-    advance(even, odd, half, k_now, 32, v_now, 0);
-    if (half + 1 >= n_halves) return;
-    // K of the next is there (and V of the next on its way)
-    wait_all_but<NLD>();
-    lds_barrier();
-    request(half / 2 + 2, of_k, k_now);
-    // (behind the last tile: of what the buffer holds, and all of it is masked)
-    advance(odd, even, half + 1, k_then, 0, v_now, 32);
   };
   for (int half = 0;; half += 4) {
     one_tile(half, k_lds0, k_lds1, v_lds0, v_lds1);
@@ -346,7 +347,6 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(RB == 2
     one_tile(half + 2, k_lds1, k_lds0, v_lds1, v_lds0);
     if (half + 4 >= n_halves) break;
   }
-  wait_all_but<0>();  // (nothing may land when others have the memory)
   if (idle) return;
 
   // ---- the quotient; lane holds O[row][32 d + 8 g + 4 hl + i] ----
