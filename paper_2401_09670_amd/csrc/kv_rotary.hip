@@ -3,7 +3,9 @@
 // A pair (a, b) of a head's features at position p becomes (a cos - b sin, b cos + a sin), cos and sin from row p of a table.  In
 // fp32, products and sums rounded one by one (no fused multiply-add: the result is the definition's bit by bit, whichever of a
 // pair a lane computes), then to bf16 once; a cache of 8 bits holds that bf16 row rounded again (kv_quant.h).
-// Bytes bound it: every row is read once and written once or (K) twice, the table's rows come out of the caches.
+// Bytes bound it: every row is read once and written once or (K) twice, the table's rows come out of the caches.  12 prompts, 6800
+// rows of 40 heads, into bf16 pages 80 us = 6.1 TB/s; pieces of 20000 rows of 64 heads on 8 into int8 pages 141 us = 5.9.  One row
+// of 64 sequences of 64 heads on 8: 3.8 us on the GPU, 5.3 from call to call, which is the host.
 //
 // A launch has up to two parts:
 //  * rows: a wave has 4 rows, 16 lanes each, and some of the heads of Q, of K and, for a bf16 cache, of V.  The rows' table entries
@@ -49,11 +51,22 @@ __device__ __forceinline__ void load_words(uint32_t (&w)[N], const uint16_t* p) 
     w[1] = v[1];
   }
 }
+// Rows into the pages go past the caches, and the turned rows where there are more of them than the last-level cache keeps for
+// whoever reads them next.  (us, none past, all past, by this rule: 20000 rows of 64 heads, 320 MB of Q, 159, 144 and 141;
+// 6800 of 40, 139 MB of Q and K and as much into bf16 pages, 97, 91 and 80, and with the attention of 8000 of 40 behind it
+// 248, 251 and 239; one row of 64 sequences of 40 and its attention 115.8, 113.1 and 113.6.)
 template <int N>
-__device__ __forceinline__ void store_words(void* p, const uint32_t (&w)[N]) {
-  if constexpr (N == 4) st16(p, u32x4{w[0], w[1], w[2], w[3]});
-  else if constexpr (N == 2) *reinterpret_cast<u32x2*>(p) = u32x2{w[0], w[1]};
-  else *reinterpret_cast<uint32_t*>(p) = w[0];
+__device__ __forceinline__ void store_past(void* p, const uint32_t (&w)[N]) {
+  if constexpr (N == 4) __builtin_nontemporal_store(u32x4{w[0], w[1], w[2], w[3]}, reinterpret_cast<u32x4*>(p));
+  else if constexpr (N == 2) __builtin_nontemporal_store(u32x2{w[0], w[1]}, reinterpret_cast<u32x2*>(p));
+  else __builtin_nontemporal_store(w[0], reinterpret_cast<uint32_t*>(p));
+  asm volatile("");  // (else this store and the ordinary one of another branch become a single ordinary one)
+}
+template <bool PAST, int N>
+__device__ __forceinline__ void store_row(void* p, const uint32_t (&w)[N]) {
+  if constexpr (PAST) store_past(p, w);
+  else if constexpr (N == 4) st16(p, u32x4{w[0], w[1], w[2], w[3]});
+  else *reinterpret_cast<u32x2*>(p) = u32x2{w[0], w[1]};
 }
 
 // What turns the E numbers of a lane: halves, E cosines and E sines (negative in the first half); adjacent, E / 2 of each.
@@ -116,8 +129,8 @@ struct Turn {
   }
 };
 
-// 4 rows, U heads of [Q | K | V where it is bf16].
-template <int HD, int T, int U>
+// 4 rows, U heads of [Q | K | V where it is bf16].  PAST: q_out and k_out past the caches.
+template <int HD, int T, int U, bool PAST>
 __device__ __forceinline__ void rows_part(const RotaryArgs& a, int wave) {
   constexpr int E = HD / 16;
   const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
@@ -156,15 +169,15 @@ __device__ __forceinline__ void rows_part(const RotaryArgs& a, int wave) {
     if (h >= heads) return;
     if (h < n + n_kv) t.apply(w[u], in.adjacent);
     if (h < n) {
-      if (there) store_words(in.q_out + ((size_t)row * n + h) * HD + E * c, w[u]);
+      if (there) store_row<PAST>(in.q_out + ((size_t)row * n + h) * HD + E * c, w[u]);
       continue;
     }
     const bool is_v = h >= n + n_kv;
     const int kv = is_v ? h - n - n_kv : h - n;
-    if (!is_v && in.k_out && there) store_words(in.k_out + ((size_t)row * n_kv + kv) * HD + E * c, w[u]);
+    if (!is_v && in.k_out && there) store_row<PAST>(in.k_out + ((size_t)row * n_kv + kv) * HD + E * c, w[u]);
     const size_t to = (page + kv) * kKvPage + slot;
     if constexpr (T == kKvBf16) {
-      if (there) store_words(static_cast<uint16_t*>(is_v ? a.cache.v : a.cache.k) + to * HD + E * c, w[u]);
+      if (there) store_past(static_cast<uint16_t*>(is_v ? a.cache.v : a.cache.k) + to * HD + E * c, w[u]);
     } else {
       const uint32_t sc = scale_bits<T>(row_amax(w[u]));
       const float inv = scale_inverse(sc);
@@ -172,7 +185,7 @@ __device__ __forceinline__ void rows_part(const RotaryArgs& a, int wave) {
 #pragma unroll
       for (int j = 0; j < E / 4; ++j) b[j] = quantise4<T>(w[u][2 * j], w[u][2 * j + 1], sc, inv);
       if (there) {
-        store_words(static_cast<uint8_t*>(a.cache.k) + to * HD + E * c, b);
+        store_past(static_cast<uint8_t*>(a.cache.k) + to * HD + E * c, b);
         if (c == 0) static_cast<uint16_t*>(a.cache.k_scale)[to] = (uint16_t)sc;
       }
     }
@@ -272,10 +285,10 @@ __device__ __forceinline__ void v_pages_part(const RotaryArgs& a, int wave) {
   }
 }
 
-template <int HD, int T, int U>
+template <int HD, int T, int U, bool PAST>
 __global__ __launch_bounds__(kRotThreads) void kv_append_rotary_kernel(const RotaryArgs a) {
   const int wave = (int)blockIdx.x * kRotWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (wave < a.row_waves) return rows_part<HD, T, U>(a, wave);
+  if (wave < a.row_waves) return rows_part<HD, T, U, PAST>(a, wave);
   if constexpr (T != kKvBf16) {
     __shared__ __attribute__((aligned(16))) uint8_t rows[kRotThreads / 16][HD];
     if (wave >= a.row_waves + a.v_waves) return;
@@ -284,15 +297,20 @@ __global__ __launch_bounds__(kRotThreads) void kv_append_rotary_kernel(const Rot
   }
 }
 
+constexpr double kKeptBytes = 200e6;  // what is left of the last-level cache beside what is read
+
+// Heads of a wave, where that leaves two waves a SIMD or more; else 1.  (8: the 6800 rows above 80 instead of 78 us, the 20000 157
+// instead of 153.)
+constexpr int kHeads = 4;
+
 struct RotaryPlan {
-  int heads;  // of a wave
+  int heads;
   long head_blocks, row_waves, v_waves;
 };
 static RotaryPlan rotary_plan(const RotaryRows& r, int kv_type, int n_heads, int n_kv_heads) {
   RotaryPlan p;
   const long heads = n_heads + (kv_type == kKvBf16 ? 2l : 1l) * n_kv_heads, groups = ((long)r.t + 3) / 4;
-  p.heads = 8;
-  while (p.heads > 1 && groups * ((heads + p.heads - 1) / p.heads) < 2048) p.heads /= 8;
+  p.heads = groups * ((heads + kHeads - 1) / kHeads) < 2048 ? 1 : kHeads;
   p.head_blocks = (heads + p.heads - 1) / p.heads;
   p.row_waves = groups * p.head_blocks;
   p.v_waves = kv_type == kKvBf16 ? 0
@@ -311,11 +329,13 @@ hipError_t launch_kv_append_rotary(const RotaryRows& r, const KvCache& cache, in
   if (!rotary_fits(r, cache.type, n_heads, n_kv_heads)) return hipErrorInvalidValue;
   const RotaryPlan p = rotary_plan(r, cache.type, n_heads, n_kv_heads);
   const RotaryArgs a{r, cache, n_heads, n_kv_heads, (int)p.head_blocks, (int)p.row_waves, (int)p.v_waves};
+  const bool past = 2.0 * r.t * head_dim * (n_heads + (r.k_out ? n_kv_heads : 0)) > kKeptBytes;
   const dim3 grid((unsigned)rotary_blocks(p)), threads(kRotThreads);
   using std::integral_constant;
   auto sized = [&](auto hd, auto type) {
-    if (p.heads == 8) hipLaunchKernelGGL((kv_append_rotary_kernel<hd(), type(), 8>), grid, threads, 0, stream, a);
-    else hipLaunchKernelGGL((kv_append_rotary_kernel<hd(), type(), 1>), grid, threads, 0, stream, a);
+    if (p.heads == 1) hipLaunchKernelGGL((kv_append_rotary_kernel<hd(), type(), 1, false>), grid, threads, 0, stream, a);
+    else if (past) hipLaunchKernelGGL((kv_append_rotary_kernel<hd(), type(), kHeads, true>), grid, threads, 0, stream, a);
+    else hipLaunchKernelGGL((kv_append_rotary_kernel<hd(), type(), kHeads, false>), grid, threads, 0, stream, a);
     return hipGetLastError();
   };
   auto typed = [&](auto hd) {
