@@ -1,16 +1,16 @@
 // Causal attention of packed prompts through a sliding window that leaves the first tokens visible: query i sees key j <= i if
 // i - j < window or j < sinks.
 //
-// A workgroup owns 64 rows a wave of one key/value head: a row is a (query, query head), a power of two of the heads that share
+// A workgroup owns 128 rows of one key/value head, 32 a wave: a row is a (query, query head), a power of two of the heads that share
 // the key/value head for each query, so that the more heads share it the fewer queries a workgroup has, and the less its windows
 // reach beyond each other.  It goes over one list of keys: the first tokens before its first query's window, then from there to
 // its last query.  Key number v of that list (all its rows') is seen by a row if v <= top and (v >= low or v < sinks), with
 // top and low the numbers of the row's own token and of its window's first.
 //
-// Scores are computed transposed, S^T[key, row] = K Q^T, so that a lane holds scores of one row (lane % 32 of each of the two
-// blocks of 32 that a wave has): running maximum and sum are scalars of a lane, and the probabilities are the column operand of
-// O^T[d, row] = V^T P^T as they are.  K and V tiles of 64 keys land row-major in one of two LDS buffers by direct loads while
-// the other is multiplied; V^T comes out through the transposing LDS read.  Each operand read from LDS meets both blocks.
+// Scores are computed transposed, S^T[key, row] = K Q^T, so that a lane holds scores of one row (lane % 32): running maximum and
+// sum are scalars of a lane, and the probabilities are the column operand of O^T[d, row] = V^T P^T as they are.  K and V tiles
+// of 64 keys land row-major in one of two LDS buffers by direct loads while the other is multiplied; V^T comes out through the
+// transposing LDS read.
 #include <algorithm>
 #include <type_traits>
 
@@ -19,14 +19,14 @@
 
 namespace ds {
 
-constexpr int kWinKeys = 64;       // of a tile
-constexpr float kWinSlack = 8.f;   // exponent headroom before the softmax's reference point is moved
+constexpr int kWinWaves = 4, kWinRows = 32;  // of a workgroup, of a wave
+constexpr int kWinKeys = 64;                // of a tile
+constexpr float kWinSlack = 8.f;            // exponent headroom before the softmax's reference point is moved
 
 struct WindowArgs {
   WindowRows r;
   int kv_group;      // query heads on a key/value head
   int pack_log2;     // of the heads of a row's query
-  int head_blocks;   // n_heads >> pack_log2
   int places;        // of a head block: t / queries + B
   int blocks, per_xcd;
   float scale_log2e;
@@ -40,13 +40,13 @@ __device__ __forceinline__ void wait_all_but() {  // vmcnt(N) alone: N in bits 3
   __builtin_amdgcn_s_waitcnt((N & 0xf) | (N >> 4) << 14 | 0x7 << 4 | 0xf << 8);
 }
 
-template <int HD, int NW, int RB>
-__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(RB == 2 && HD == 128 ? 1 : 2))) void window_attention_kernel(
+template <int HD>
+__global__ __launch_bounds__(64 * kWinWaves) __attribute__((amdgpu_waves_per_eu(2))) void window_attention_kernel(
     const WindowArgs a) {
   constexpr int DSTEPS = HD / 16, DT = HD / 32, CPR = HD / 8;
   constexpr int TILE = kWinKeys * HD;
   constexpr int RPL = 64 / CPR;                 // tile rows of a wave-level load
-  constexpr int NLD = kWinKeys / (RPL * NW);    // loads of a wave, tile and operand
+  constexpr int NLD = kWinKeys / (RPL * kWinWaves);    // loads of a wave, tile and operand
   // Two buffers for K and two for V.  Each is a variable of its own, and which one an access means is known when it is compiled:
   // the compiler then sees that a load into one need not have landed before another is read.
   __shared__ __attribute__((aligned(1024))) uint16_t k_lds0[TILE], k_lds1[TILE], v_lds0[TILE], v_lds1[TILE];
@@ -59,7 +59,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(RB == 2
   const int n_sub = a.kv_group >> a.pack_log2;
   const int sub = id % n_sub, kv = id / n_sub / a.places;
   const int place = a.places - 1 - id / n_sub % a.places;  // (late ones first: their windows are full)
-  const int pack = 1 << a.pack_log2, queries = (32 * RB * NW) >> a.pack_log2;
+  const int pack = 1 << a.pack_log2, queries = (kWinRows * kWinWaves) >> a.pack_log2;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   // The sequence whose place this is: the last that begins here or before.  (Its bounds out of the lanes that looked for it: not
@@ -133,39 +133,30 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(RB == 2
 
   // the lane's rows
   const int row_q = lq >> a.pack_log2, row_head = (kv * n_sub + sub) * pack + (lq & (pack - 1));
-  const int block_q = 32 >> a.pack_log2;        // queries of a block of rows
-  const int wave_q = q0 + RB * wave * block_q;
+  const int wave_q = q0 + wave * (kWinRows >> a.pack_log2);
   const bool idle = wave_q >= len;
-  bf16x8 qf[RB][DSTEPS];
-  int top[RB];
+  const int query = wave_q + row_q, top = query - band + first;
+  bf16x8 qf[DSTEPS];
+  {
+    const uint16_t* qrow = in.q + ((size_t)start + min(query, len - 1)) * in.q_stride + (size_t)row_head * HD + hl * 8;
 #pragma unroll
-  for (int b = 0; b < RB; ++b) {
-    const int i = wave_q + b * block_q + row_q;
-    const uint16_t* qrow = in.q + ((size_t)start + min(i, len - 1)) * in.q_stride + (size_t)row_head * HD + hl * 8;
-#pragma unroll
-    for (int st = 0; st < DSTEPS; ++st) qf[b][st] = as_bf16(ld16(qrow + st * 16));
-    top[b] = i - band + first;
+    for (int st = 0; st < DSTEPS; ++st) qf[st] = as_bf16(ld16(qrow + st * 16));
   }
   // Of the wave: the last number that any of its rows sees, the one up to which all do; where the first row's window begins
   // and where the last one's does.  Then the halves (of a tile: 32 keys) that any of the rows sees, [0, sink_halves) and
   // [from_half, upto_half), and those that need masks: from tail_half on, and in [sinks / 32, clear_half).
-  const int wave_top = wave_q + RB * block_q - 1 - band + first, least_top = wave_q - band + first;
+  const int wave_top = wave_q + (kWinRows >> a.pack_log2) - 1 - band + first, least_top = wave_q - band + first;
   const int wave_low = least_top - in.window + 1, most_low = wave_top - in.window + 1;
   const int sink_halves = idle ? 0 : (min(in.sinks, total) + 31) >> 5, from_half = wave_low >> 5;
   const int upto_half = idle ? 0 : min((wave_top >> 5) + 1, n_halves);
   const int tail_half = (least_top + 1) >> 5, clear_half = (most_low + 31) >> 5, seen_sinks = in.sinks >> 5;
 
-  floatx16 oacc[RB][DT];
-  float m_run[RB], l_run[RB];
+  floatx16 oacc[DT];
+  float m_run = kLowestScore, l_run = 0.f;
 #pragma unroll
-  for (int b = 0; b < RB; ++b) {
-    m_run[b] = kLowestScore;
-    l_run[b] = 0.f;
+  for (int d = 0; d < DT; ++d)
 #pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) oacc[b][d][r] = 0.f;
-  }
+    for (int r = 0; r < 16; ++r) oacc[d][r] = 0.f;
 
   const int kswz = CPR == 16 ? (lq & 15) : ((lq >> 1) & 7);
   const int i16 = lane & 15;
@@ -173,10 +164,14 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(RB == 2
   const int vchunk = 2 * ((lane >> 4) & 1) + ((i16 & 3) >> 1);
   const int k_at = lq * HD, v_at = (4 * hl + (i16 >> 2)) * HD + (i16 & 1) * 4;
   // The scores of a half tile (32 keys) are made while the half before it is brought to probabilities and multiplied with V: a
-  // matrix instruction takes the matrix unit 32 cycles and its wave 4, in the others the wave's vector instructions go on.
-  // There is one wave a SIMD (its rows' registers are 400), so nothing else would.  Each slot below is a matrix instruction,
-  // the LDS reads of one that follows and a piece of the softmax, and fences keep the compiler from undoing it.
-  float most[RB];
+  // matrix instruction takes the matrix unit 32 cycles and its wave 4, and in the others the vector instructions go on, its own
+  // wave's and those of the other wave that a SIMD has.  Each slot below is a matrix instruction, the LDS reads of one that
+  // follows and a piece of the softmax, and fences keep the compiler from undoing it.
+  //   A wave has 32 rows.  (64, with one wave a SIMD and half the LDS reads: their scores have to be in the accumulation registers
+  // then, and are copied out of them; 64 heads on 8, 16383 tokens, window 2048 1325 us instead of 1150.  256 rows a workgroup
+  // 1125 instead of 1097; three workgroups a compute unit, with 32 keys a tile in three buffers, 1131 instead of 1052, 12 prompts
+  // of 40 heads 95 instead of 99.)
+  float most;
   auto read_k = [&](const uint16_t* buf, int from, int st) __attribute__((always_inline)) {
     return as_bf16(ld16(buf + (k_at + ((2 * st + hl) ^ kswz) * 8 + from * HD)));
   };
@@ -189,33 +184,28 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(RB == 2
     return as_bf16(u32x4{lo[0], lo[1], hi[0], hi[1]});
   };
   const floatx16 zero = {};
-  auto step = [&](floatx16 (&cur)[RB], floatx16 (&nxt)[RB], const uint16_t* k_buf, int k_from, uint16_t* v_buf,
+  auto step = [&](floatx16& cur, floatx16& nxt, const uint16_t* k_buf, int k_from, uint16_t* v_buf,
                   int v_from) __attribute__((always_inline)) {
-    constexpr int NS = RB * DSTEPS, NP = 2 * RB * DT, kPairs = 8 * RB;  // slots of either product, pairs of probabilities
+    constexpr int kOps = DSTEPS + 2 * DT;      // matrix instructions: of K, of V's first 16 keys, of its others
     constexpr int kGroup = 4;                  // operands that are read, and waited for, together
-    constexpr int kFirst = 2;                  // pairs before the first slot
-    constexpr int kPairSlots = NS + RB * DT;   // all of P is there before the slots of its second half
-    bf16x8 op[DSTEPS + 2 * DT];
-    u32x4 pw[RB][2];  // pw[b][x]: column operand of the step over 16 keys
-    float sum[RB], mb[RB], top_of[RB];
-#pragma unroll
-    for (int b = 0; b < RB; ++b) {
-      sum[b] = 0.f;
-      mb[b] = m_run[b] * a.scale_log2e;
-      top_of[b] = -INFINITY;
-    }
+    constexpr int kFirst = 2;                  // pairs of probabilities before the first slot
+    constexpr int kPairSlots = DSTEPS + DT;    // all of them are there before the slots of the last 16 keys
+    bf16x8 op[kOps];
+    u32x4 pw[2];  // column operands of 16 keys each
+    const float mb = m_run * a.scale_log2e;
+    float sum = 0.f, top_of = -INFINITY;
     auto read = [&](int f) __attribute__((always_inline)) {
       op[f] = f < DSTEPS ? read_k(k_buf, k_from, f) : read_v(v_buf, v_from, (f - DSTEPS) / DT, (f - DSTEPS) % DT);
     };
-    // Probabilities 2 (p % 4) and the next of keys 16 x .. of block b; rounded to bf16, 2^-9 of each at most.
+    // Probabilities 2 p and the next; rounded to bf16, 2^-9 of each at most, for the product, and as they are in the sum.  (Dot
+    // products of pairs with (1, 1) are half as many instructions as additions, but they wait for the matrix unit.)
     auto pair = [&](int p) __attribute__((always_inline)) {
-      const int x = p / (4 * RB), b = p / 4 % RB, r = 8 * x + 2 * (p % 4);
-      const float p0 = __builtin_amdgcn_exp2f(cur[b][r] * a.scale_log2e - mb[b]);
-      const float p1 = __builtin_amdgcn_exp2f(cur[b][r + 1] * a.scale_log2e - mb[b]);
-      sum[b] += p0;
-      sum[b] += p1;
-      asm volatile("" : "+v"(sum[b]));  // (here, not where the sum is used)
-      pw[b][x][p % 4] = pack_bf16(p0, p1);
+      const float p0 = __builtin_amdgcn_exp2f(cur[2 * p] * a.scale_log2e - mb);
+      const float p1 = __builtin_amdgcn_exp2f(cur[2 * p + 1] * a.scale_log2e - mb);
+      sum += p0;
+      sum += p1;
+      asm volatile("" : "+v"(sum));  // (here, not where the sum is used)
+      pw[p / 4][p % 4] = pack_bf16(p0, p1);
     };
 #pragma unroll
     for (int f = 0; f < kGroup; ++f) read(f);
@@ -224,79 +214,68 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(RB == 2
     for (int p = 0; p < kFirst; ++p) pair(p);
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int slot = 0; slot < NS + NP; ++slot) {
-      const int b = slot % RB, f = slot / RB;
-      if (slot < NS) {
-        nxt[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[f], qf[b][f], f == 0 ? zero : nxt[b], 0, 0, 0);
+    for (int slot = 0; slot < kOps; ++slot) {
+      if (slot < DSTEPS) {
+        nxt = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[slot], qf[slot], slot == 0 ? zero : nxt, 0, 0, 0);
       } else {
-        const int x = (f - DSTEPS) / DT, d = (f - DSTEPS) % DT;
-        oacc[b][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[f], as_bf16(pw[b][x]), oacc[b][d], 0, 0, 0);
+        const int x = (slot - DSTEPS) / DT, d = (slot - DSTEPS) % DT;
+        oacc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[slot], as_bf16(pw[x]), oacc[d], 0, 0, 0);
       }
-      if (b == 0 && f % kGroup < 2) {  // the next group's operands, half of them each time
+      if (slot % kGroup < 2) {  // the next group's operands, half of them each time
 #pragma unroll
         for (int e = 0; e < kGroup / 2; ++e) {
-          const int g = (f / kGroup + 1) * kGroup + f % kGroup * (kGroup / 2) + e;
-          if (g < DSTEPS + 2 * DT) read(g);
+          const int g = (slot / kGroup + 1) * kGroup + slot % kGroup * (kGroup / 2) + e;
+          if (g < kOps) read(g);
         }
       }
 #pragma unroll
-      for (int p = kFirst; p < kPairs; ++p)
-        if ((p - kFirst) * kPairSlots / (kPairs - kFirst) == slot) pair(p);
+      for (int p = kFirst; p < 8; ++p)
+        if ((p - kFirst) * kPairSlots / (8 - kFirst) == slot) pair(p);
       if (slot >= kPairSlots) {  // the maximum of the new scores in the last slots
 #pragma unroll
-        for (int e = 0; e < kPairs; ++e)
-          if (e * (RB * DT) / kPairs == slot - kPairSlots) {
-            top_of[e / 8] = fmaxf(fmaxf(top_of[e / 8], nxt[e / 8][2 * (e % 8)]), nxt[e / 8][2 * (e % 8) + 1]);
-            asm volatile("" : "+v"(top_of[e / 8]));
+        for (int e = 0; e < 8; ++e)
+          if (e * DT / 8 == slot - kPairSlots) {
+            top_of = fmaxf(fmaxf(top_of, nxt[2 * e]), nxt[2 * e + 1]);
+            asm volatile("" : "+v"(top_of));
           }
       }
       __builtin_amdgcn_sched_barrier(0);
     }
-#pragma unroll
-    for (int b = 0; b < RB; ++b) {
-      l_run[b] += sum[b];
-      most[b] = top_of[b];
-    }
+    l_run += sum;
+    most = top_of;
   };
   // What the next half's scores still need: masks (element r is number v0 + 8 (r / 4) + 4 hl + r % 4) and, now and then, another
   // reference point.  It only has to keep the exponentials in range, so it moves when some row's maximum grew by more than
   // kWinSlack in the exponent.
-  auto settle = [&](floatx16 (&nxt)[RB], int half) __attribute__((always_inline)) {
+  auto settle = [&](floatx16& nxt, int half) __attribute__((always_inline)) {
     const int v0 = 32 * half;
     if (half >= tail_half || (half < clear_half && half >= seen_sinks)) {
-      const int at = v0 + 4 * hl, sinks = in.sinks - at;
+      const int at = v0 + 4 * hl, sinks = in.sinks - at, last = top - at, from = last - in.window + 1;
+      most = -INFINITY;
 #pragma unroll
-      for (int b = 0; b < RB; ++b) {
-        const int last = top[b] - at, from = last - in.window + 1;
-        most[b] = -INFINITY;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int v = (r >> 2) * 8 + (r & 3);
-          const bool hidden = (v > last) | ((v < from) & (v >= sinks));
-          nxt[b][r] = hidden ? -INFINITY : nxt[b][r];
-          most[b] = fmaxf(most[b], nxt[b][r]);
-        }
+      for (int r = 0; r < 16; ++r) {
+        const int v = (r >> 2) * 8 + (r & 3);
+        const bool hidden = (v > last) | ((v < from) & (v >= sinks));
+        nxt[r] = hidden ? -INFINITY : nxt[r];
+        most = fmaxf(most, nxt[r]);
       }
     }
+    const float m = lane_op<32>(most, MaxOp());
+    if (__builtin_amdgcn_ballot_w64(m * a.scale_log2e > m_run * a.scale_log2e + kWinSlack) != 0) {
+      const float m_new = fmaxf(m_run, m);
+      const float alpha = __builtin_amdgcn_exp2f((m_run - m_new) * a.scale_log2e);
+      l_run *= alpha;
+      m_run = m_new;
 #pragma unroll
-    for (int b = 0; b < RB; ++b) {
-      const float m = lane_op<32>(most[b], MaxOp());
-      if (__builtin_amdgcn_ballot_w64(m * a.scale_log2e > m_run[b] * a.scale_log2e + kWinSlack) != 0) {
-        const float m_new = fmaxf(m_run[b], m);
-        const float alpha = __builtin_amdgcn_exp2f((m_run[b] - m_new) * a.scale_log2e);
-        l_run[b] *= alpha;
-        m_run[b] = m_new;
+      for (int d = 0; d < DT; ++d)
 #pragma unroll
-        for (int d = 0; d < DT; ++d)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) oacc[b][d][r] *= alpha;
-      }
+        for (int r = 0; r < 16; ++r) oacc[d][r] *= alpha;
     }
   };
   // In an iteration a half's probabilities meet V while the scores of the half behind it are made, twice: so it reads halves
   // 2 i and 2 i + 1 of V and 2 i + 1 and 2 i + 2 of K, and K's tiles lie half a tile behind V's.  Both land in the iteration
   // before.  A barrier each.
-  floatx16 even[RB], odd[RB];
+  floatx16 even, odd;
   request(-32, of_k, k_lds1);
   request(0, of_v, v_lds0);
   request(32, of_k, k_lds0);
@@ -304,33 +283,29 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(RB == 2
   lds_barrier();
   const floatx16 none = {-INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY,
                          -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY};
-  auto scores = [&](floatx16 (&to)[RB]) __attribute__((always_inline)) {
-#pragma unroll
-    for (int st = 0; st < DSTEPS; ++st) {
-      const bf16x8 kf = read_k(k_lds1, 32, st);
-#pragma unroll
-      for (int b = 0; b < RB; ++b) to[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[b][st], st == 0 ? zero : to[b], 0, 0, 0);
-    }
-#pragma unroll
-    for (int b = 0; b < RB; ++b) {
-      most[b] = -INFINITY;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) most[b] = fmaxf(most[b], to[b][r]);
-    }
-  };
   // Half `half` from scores to output, and the scores of the next; where the wave's rows see neither, the next are scores of
   // nothing.  (Behind the last half they are of what the buffer holds, and all are masked.)
-  auto advance = [&](floatx16 (&cur)[RB], floatx16 (&nxt)[RB], int half, const uint16_t* k_buf, int k_from, uint16_t* v_buf,
+  auto advance = [&](floatx16& cur, floatx16& nxt, int half, const uint16_t* k_buf, int k_from, uint16_t* v_buf,
                      int v_from) __attribute__((always_inline)) {
     if (half < sink_halves || (half + 1 >= from_half && half < upto_half)) {
       step(cur, nxt, k_buf, k_from, v_buf, v_from);
       settle(nxt, half + 1);
     } else {
-#pragma unroll
-      for (int b = 0; b < RB; ++b) nxt[b] = none;
+      nxt = none;
     }
   };
-  scores(even);
+  {
+    bf16x8 op[DSTEPS];
+#pragma unroll
+    for (int st = 0; st < DSTEPS; ++st) op[st] = read_k(k_lds1, 32, st);
+    __builtin_amdgcn_sched_barrier(0);
+    even = zero;
+#pragma unroll
+    for (int st = 0; st < DSTEPS; ++st) even = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[st], qf[st], even, 0, 0, 0);
+    most = -INFINITY;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) most = fmaxf(most, even[r]);
+  }
   settle(even, 0);
   lds_barrier();  // (the first iteration's loads land where these scores' keys were)
   auto one_tile = [&](int half, uint16_t* k_now, uint16_t* k_then, uint16_t* v_now, uint16_t* v_then) __attribute__((always_inline)) {
@@ -350,74 +325,77 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(RB == 2
   if (idle) return;
 
   // ---- the quotient; lane holds O[row][32 d + 8 g + 4 hl + i] ----
+  // By way of LDS, where a wave's rows take the place of keys that all waves are done with (chunk c of row r at c ^ a swizzle), so
+  // that a store writes whole rows; 8 bytes of each of 32 rows at a time, the stores took a workgroup 2 us.
+  const float l = lane_op<32>(l_run, AddOp());
+  const float inv = l == 0.f ? 0.f : 1.f / l;  // (every score below fp32's range: 0)
+  uint16_t* mine = (wave & 2 ? v_lds0 : k_lds0) + (wave & 1) * kWinRows * HD;
+  auto swizzle = [](int row) { return CPR == 16 ? row & 15 : (row >> 1) & 7; };
+  float check = 0.f;
+  bf16x2 ones;
+  ones[0] = (__bf16)1.f;
+  ones[1] = (__bf16)1.f;
 #pragma unroll
-  for (int b = 0; b < RB; ++b) {
-    const int i = wave_q + b * block_q + row_q;
-    const float l = lane_op<32>(l_run[b], AddOp());
-    const float inv = l == 0.f ? 0.f : 1.f / l;  // (every score below fp32's range: 0)
-    bool nan = false;
+  for (int d = 0; d < DT; ++d)
 #pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        oacc[b][d][r] *= inv;
-        nan = nan || oacc[b][d][r] != oacc[b][d][r];
-      }
-    if (i < len) {
-      uint16_t* orow = in.o + (((size_t)start + i) * in.n_heads + row_head) * HD + hl * 4;
-#pragma unroll
-      for (int d = 0; d < DT; ++d)
-#pragma unroll
-        for (int g = 0; g < 4; ++g)
-          *reinterpret_cast<u32x2*>(orow + d * 32 + g * 8) =
-              u32x2{pack_bf16(oacc[b][d][4 * g], oacc[b][d][4 * g + 1]), pack_bf16(oacc[b][d][4 * g + 2], oacc[b][d][4 * g + 3])};
+    for (int g = 0; g < 4; ++g) {
+      const u32x2 w{pack_bf16(oacc[d][4 * g] * inv, oacc[d][4 * g + 1] * inv), pack_bf16(oacc[d][4 * g + 2] * inv, oacc[d][4 * g + 3] * inv)};
+      check = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w[0]), ones, check, false);
+      check = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w[1]), ones, check, false);
+      *reinterpret_cast<u32x2*>(mine + lq * HD + ((4 * d + g) ^ swizzle(lq)) * 8 + 4 * hl) = w;
     }
-    // A hidden key's V that is not finite has made NaN of the rows that share a tile with it (0 times it): rows with NaN are done
-    // again, key by key over what they see, 64 scores at a time.  NaN that they see stays.
-    uint64_t again = __builtin_amdgcn_ballot_w64(nan && i < len);
-    again = (again | again >> 32) & 0xffffffffu;
-    while (again) {
-      const int row = __builtin_ctzll(again);
-      again &= again - 1;
-      const int at = wave_q + b * block_q + (row >> a.pack_log2), head = (kv * n_sub + sub) * pack + (row & (pack - 1));
-      const uint16_t* qr = in.q + ((size_t)start + at) * in.q_stride + (size_t)head * HD;
-      const int begin = max(at - in.window + 1, 0), before = min(in.sinks, begin), n = at + 1 - begin + before;
-      constexpr int ND = HD / 64;
-      float m = kLowestScore, sum = 0.f, out[ND] = {};
-      for (int c0 = 0; c0 < n; c0 += 64) {
-        const int v = min(c0 + lane, n - 1);
-        const uint16_t* kr = kbase + (size_t)(v < before ? v : v - before + begin) * in.k_stride;
-        float dot = 0.f;
+  __builtin_amdgcn_wave_barrier();  // (a wave's LDS accesses keep their order; the compiler has to keep it too)
+  uint64_t again = __builtin_amdgcn_ballot_w64(check != check && query < len);
+  again = (again | again >> 32) & 0xffffffffu;
+#pragma unroll
+  for (int j = 0; j < kWinRows / RPL; ++j) {
+    const int row = j * RPL + ld_sub, at = wave_q + (row >> a.pack_log2), head = (kv * n_sub + sub) * pack + (row & (pack - 1));
+    const u32x4 w = ld16(mine + row * HD + (ld_c ^ swizzle(row)) * 8);
+    if (at < len && !((again >> row) & 1)) st16(in.o + (((size_t)start + at) * in.n_heads + head) * HD + ld_c * 8, w);
+  }
+  // A hidden key's V that is not finite has made NaN of the rows that share a tile with it (0 times it): rows with NaN are done
+  // again, key by key over what they see, 64 scores at a time.  NaN that they see stays.
+  while (again) {
+    const int row = __builtin_ctzll(again);
+    again &= again - 1;
+    const int at = wave_q + (row >> a.pack_log2), head = (kv * n_sub + sub) * pack + (row & (pack - 1));
+    const uint16_t* qr = in.q + ((size_t)start + at) * in.q_stride + (size_t)head * HD;
+    const int begin = max(at - in.window + 1, 0), before = min(in.sinks, begin), n = at + 1 - begin + before;
+    constexpr int ND = HD / 64;
+    float m = kLowestScore, sum = 0.f, out[ND] = {};
+    for (int c0 = 0; c0 < n; c0 += 64) {
+      const int v = min(c0 + lane, n - 1);
+      const uint16_t* kr = kbase + (size_t)(v < before ? v : v - before + begin) * in.k_stride;
+      float dot = 0.f;
 #pragma unroll 4
-        for (int d = 0; d < HD; d += 2) {
-          const uint32_t x = *reinterpret_cast<const uint32_t*>(qr + d), y = *reinterpret_cast<const uint32_t*>(kr + d);
-          dot = fmaf(bf16_lo(x), bf16_lo(y), dot);
-          dot = fmaf(bf16_hi(x), bf16_hi(y), dot);
-        }
-        dot = c0 + lane < n ? dot * a.scale_log2e : -INFINITY;
-        float most = dot;
-        most = lane_op<1>(most, MaxOp());
-        most = lane_op<2>(most, MaxOp());
-        most = lane_op<kMirror4>(most, MaxOp());
-        most = across_groups<8>(most, MaxOp());
-        const float m_new = fmaxf(m, most), alpha = __builtin_amdgcn_exp2f(m - m_new), p = __builtin_amdgcn_exp2f(dot - m_new);
-        m = m_new;
-        sum = sum * alpha + wave_sum(p);
-#pragma unroll
-        for (int j = 0; j < ND; ++j) out[j] *= alpha;
-        const int count = min(64, n - c0);
-        for (int j = 0; j < count; ++j) {
-          const float pj = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(p), j));
-          const int vj = c0 + j;
-          const uint16_t* vr = vbase + (size_t)(vj < before ? vj : vj - before + begin) * in.v_stride + ND * lane;
-#pragma unroll
-          for (int e = 0; e < ND; ++e) out[e] = fmaf(pj, __uint_as_float((uint32_t)vr[e] << 16), out[e]);
-        }
+      for (int d = 0; d < HD; d += 2) {
+        const uint32_t x = *reinterpret_cast<const uint32_t*>(qr + d), y = *reinterpret_cast<const uint32_t*>(kr + d);
+        dot = fmaf(bf16_lo(x), bf16_lo(y), dot);
+        dot = fmaf(bf16_hi(x), bf16_hi(y), dot);
       }
-      __bf16* to = reinterpret_cast<__bf16*>(in.o) + (((size_t)start + at) * in.n_heads + head) * HD + ND * lane;
+      dot = c0 + lane < n ? dot * a.scale_log2e : -INFINITY;
+      float most = dot;
+      most = lane_op<1>(most, MaxOp());
+      most = lane_op<2>(most, MaxOp());
+      most = lane_op<kMirror4>(most, MaxOp());
+      most = across_groups<8>(most, MaxOp());
+      const float m_new = fmaxf(m, most), alpha = __builtin_amdgcn_exp2f(m - m_new), p = __builtin_amdgcn_exp2f(dot - m_new);
+      m = m_new;
+      sum = sum * alpha + wave_sum(p);
 #pragma unroll
-      for (int e = 0; e < ND; ++e) to[e] = (__bf16)(sum == 0.f ? 0.f : out[e] / sum);
+      for (int j = 0; j < ND; ++j) out[j] *= alpha;
+      const int count = min(64, n - c0);
+      for (int j = 0; j < count; ++j) {
+        const float pj = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(p), j));
+        const int vj = c0 + j;
+        const uint16_t* vr = vbase + (size_t)(vj < before ? vj : vj - before + begin) * in.v_stride + ND * lane;
+#pragma unroll
+        for (int e = 0; e < ND; ++e) out[e] = fmaf(pj, __uint_as_float((uint32_t)vr[e] << 16), out[e]);
+      }
     }
+    __bf16* to = reinterpret_cast<__bf16*>(in.o) + (((size_t)start + at) * in.n_heads + head) * HD + ND * lane;
+#pragma unroll
+    for (int e = 0; e < ND; ++e) to[e] = (__bf16)(sum == 0.f ? 0.f : out[e] / sum);
   }
 }
 
@@ -429,25 +407,17 @@ static int pack_log2_of(int kv_group) {
 }
 
 struct WindowPlan {
-  int waves, row_blocks, pack_log2;
+  int pack_log2;
   long places, blocks;
 };
 static WindowPlan window_plan(const WindowRows& r) {
   WindowPlan p;
-  p.waves = 4;
-  p.row_blocks = 1;
   p.pack_log2 = pack_log2_of(r.n_heads / r.n_kv_heads);
-  p.places = (long)r.t / ((32 * p.row_blocks * p.waves) >> p.pack_log2) + r.B;
+  p.places = (long)r.t / ((kWinRows * kWinWaves) >> p.pack_log2) + r.B;
   p.blocks = p.places * (r.n_heads >> p.pack_log2);
   return p;
 }
 bool window_attention_fits(const WindowRows& r) { return window_plan(r).blocks <= 0x7fffffffL / 256 - 8; }
-
-template <int HD, int NW, int RB>
-static hipError_t launch_window(const WindowArgs& a, hipStream_t stream) {
-  hipLaunchKernelGGL((window_attention_kernel<HD, NW, RB>), dim3((unsigned)(8 * a.per_xcd)), dim3(64 * NW), 0, stream, a);
-  return hipGetLastError();
-}
 
 hipError_t launch_window_attention(const WindowRows& r, int head_dim, hipStream_t stream) {
   if (!window_attention_fits(r)) return hipErrorInvalidValue;
@@ -456,13 +426,19 @@ hipError_t launch_window_attention(const WindowRows& r, int head_dim, hipStream_
   a.r = r;
   a.kv_group = r.n_heads / r.n_kv_heads;
   a.pack_log2 = p.pack_log2;
-  a.head_blocks = r.n_heads >> p.pack_log2;
   a.places = (int)p.places;
   a.blocks = (int)p.blocks;
   a.per_xcd = (int)((p.blocks + 7) / 8);
   a.scale_log2e = 1.4426950408889634f / sqrtf((float)head_dim);
-  if (head_dim == 128) return launch_window<128, 4, 1>(a, stream);
-  if (head_dim == 64) return launch_window<64, 4, 1>(a, stream);
+  const dim3 grid((unsigned)(8 * a.per_xcd)), threads(64 * kWinWaves);
+  if (head_dim == 128) {
+    hipLaunchKernelGGL(window_attention_kernel<128>, grid, threads, 0, stream, a);
+    return hipGetLastError();
+  }
+  if (head_dim == 64) {
+    hipLaunchKernelGGL(window_attention_kernel<64>, grid, threads, 0, stream, a);
+    return hipGetLastError();
+  }
   return hipErrorInvalidValue;
 }
 
