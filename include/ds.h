@@ -367,7 +367,7 @@ ds_status ds_decode_step_shared(ds_ctx *ctx, const ds_layer_weights *w, const vo
  *   cu_rows     device [B+1] int32, starts at 0: sequence i has the new rows cu_rows[i] .. cu_rows[i+1]-1, any number of them, 0
  *               too; rows from cu_rows[B] on are left out.  NULL: one row each, t = B
  *   ctx_lens    device [B] int32: tokens before them; the j-th new row is token ctx_lens[i] + j, and its page must be in
- *               block_tables.  -1: a sequence that only pads the batch, of which nothing is read into or written to anything
+ *               block_tables.  -1: a sequence that only pads the batch; nothing is written for its rows
  *   positions   device [t] int32: a row's row of the table (outside it: the nearest in it); NULL: the token's number
  *   table       device fp32 [n_pos, rot]: rot / 2 cosines, then rot / 2 sines.  rot: a multiple of 16 up to s
  *   adjacent    0: features i and i + rot / 2 of a head are the pair i, else features 2 i and 2 i + 1; those from rot on stay
@@ -388,8 +388,10 @@ ds_status ds_kv_append_rotary(ds_ctx *ctx, const void *q, int32_t q_stride, cons
  * j < sinks (>= 0: first tokens that stay visible).  Rows of q, k and v start their strides (in elements, multiples of 8 up to
  * 2^24, at least a row's width) apart: k and q as ds_kv_append_rotary leaves them, v in the rows of the QKV product.  o is
  * [t, n, s].  Sequences may be empty (the debug validation, which is ds_prefill_attention's, takes none); rows from
- * cu_seqlens[B] on are left as they are.  What a query does not see does not count, whatever it holds.  Scores are fp32: a key
- * whose score is below its range weighs nothing (all of them: output 0).  A probability is rounded to bf16 before it meets V. */
+ * cu_seqlens[B] on are left as they are.  What a query does not see does not count, whatever it holds; a V that is not finite
+ * makes NaN of that feature where it is seen.  Scores are fp32: a key whose score is below its range weighs nothing (all of
+ * them: output 0), one above it makes the row NaN.  A probability is rounded to bf16 before it meets V.  Workgroups that find a
+ * V that is not finite, or scores beyond some 2^20, take several times as long. */
 ds_status ds_prefill_attention_window(ds_ctx *ctx, const void *q, int32_t q_stride, const void *k, int32_t k_stride,
                                       const void *v, int32_t v_stride, const int32_t *cu_seqlens, int32_t B, int32_t t,
                                       int32_t max_seqlen, int32_t window, int32_t sinks, void *o, void *stream);

@@ -325,12 +325,9 @@ __global__ __launch_bounds__(64 * kWinWaves) __attribute__((amdgpu_waves_per_eu(
   if (idle) return;
 
   // ---- the quotient; lane holds O[row][32 d + 8 g + 4 hl + i] ----
-  // By way of LDS, where a wave's rows take the place of keys that all waves are done with (chunk c of row r at c ^ a swizzle), so
-  // that a store writes whole rows; 8 bytes of each of 32 rows at a time, the stores took a workgroup 2 us.
   const float l = lane_op<32>(l_run, AddOp());
   const float inv = l == 0.f ? 0.f : 1.f / l;  // (every score below fp32's range: 0)
-  uint16_t* mine = (wave & 2 ? v_lds0 : k_lds0) + (wave & 1) * kWinRows * HD;
-  auto swizzle = [](int row) { return CPR == 16 ? row & 15 : (row >> 1) & 7; };
+  u32x2 out[DT][4];
   float check = 0.f;
   bf16x2 ones;
   ones[0] = (__bf16)1.f;
@@ -339,63 +336,95 @@ __global__ __launch_bounds__(64 * kWinWaves) __attribute__((amdgpu_waves_per_eu(
   for (int d = 0; d < DT; ++d)
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
-      const u32x2 w{pack_bf16(oacc[d][4 * g] * inv, oacc[d][4 * g + 1] * inv), pack_bf16(oacc[d][4 * g + 2] * inv, oacc[d][4 * g + 3] * inv)};
-      check = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w[0]), ones, check, false);
-      check = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w[1]), ones, check, false);
-      *reinterpret_cast<u32x2*>(mine + lq * HD + ((4 * d + g) ^ swizzle(lq)) * 8 + 4 * hl) = w;
+      out[d][g] = u32x2{pack_bf16(oacc[d][4 * g] * inv, oacc[d][4 * g + 1] * inv), pack_bf16(oacc[d][4 * g + 2] * inv, oacc[d][4 * g + 3] * inv)};
+      check = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, out[d][g][0]), ones, check, false);
+      check = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, out[d][g][1]), ones, check, false);
     }
+  // A hidden key's V that is not finite has made NaN of the rows that share its tile (0 times it), and scores so far from 0 that
+  // their multiple of the reference point is not exact to a sixteenth may have left the exponential's range.  Where a row of
+  // the wave is such a one, all its rows are done again, slowly.
+  if (__builtin_amdgcn_ballot_w64(query < len && (check != check || fabsf(m_run * a.scale_log2e) > 0x1p20f)) != 0) {
+    float m = kLowestScore, sum = 0.f;
+    floatx16 acc[DT], odd_ones[DT];  // of V's finite numbers by P; how many others a row sees
+#pragma unroll
+    for (int d = 0; d < DT; ++d) acc[d] = odd_ones[d] = zero;
+    auto row_of = [&](int v) __attribute__((always_inline)) {
+      v = min(v, total - 1);
+      return (size_t)(v >= first ? v - first + band : v);
+    };
+#pragma unroll 1
+    for (int v0 = 0; v0 < total; v0 += 32) {
+      floatx16 z = zero;
+#pragma unroll
+      for (int st = 0; st < DSTEPS; ++st)
+        z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16(ld16(kbase + row_of(v0 + lq) * in.k_stride + st * 16 + hl * 8)), qf[st], z, 0, 0, 0);
+      float most_now = -INFINITY;
+      u32x4 see[2];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int v = v0 + (r >> 2) * 8 + hl * 4 + (r & 3);
+        const bool seen = (v <= top) & ((v > top - in.window) | (v < in.sinks));
+        z[r] = seen ? z[r] * a.scale_log2e : -INFINITY;
+        most_now = fmaxf(most_now, z[r]);
+        const uint32_t one = seen ? 0x3f80u << (16 * (r & 1)) : 0u;
+        see[r / 8][r % 8 / 2] = r & 1 ? see[r / 8][r % 8 / 2] | one : one;
+      }
+      const float m_new = fmaxf(m, lane_op<32>(most_now, MaxOp())), alpha = __builtin_amdgcn_exp2f(m - m_new);
+      m = m_new;
+      sum *= alpha;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) acc[d] *= alpha;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        z[r] = __builtin_amdgcn_exp2f(z[r] - m);
+        sum += z[r];
+      }
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        u32x4 pw;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) pw[j] = pack_bf16(z[8 * x + 2 * j], z[8 * x + 2 * j + 1]);
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          u32x4 fine{0, 0, 0, 0}, others{0, 0, 0, 0};
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const uint32_t w = vbase[row_of(v0 + 16 * x + 8 * (e / 4) + 4 * hl + e % 4) * in.v_stride + 32 * d + lq];
+            const bool finite = (w & 0x7f80u) != 0x7f80u;
+            fine[e / 2] |= (finite ? w : 0u) << (16 * (e & 1));
+            others[e / 2] |= (finite ? 0u : 0x3f80u) << (16 * (e & 1));
+          }
+          acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16(fine), as_bf16(pw), acc[d], 0, 0, 0);
+          odd_ones[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16(others), as_bf16(see[x]), odd_ones[d], 0, 0, 0);
+        }
+      }
+    }
+    sum = lane_op<32>(sum, AddOp());
+    const float over = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        float o[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = odd_ones[d][4 * g + i] > 0.f ? __uint_as_float(0x7fc00000u) : acc[d][4 * g + i] * over;
+        out[d][g] = u32x2{pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3])};
+      }
+  }
+  // By way of LDS, where a wave's rows take the place of keys that all waves are done with (chunk c of row r at c ^ a swizzle), so
+  // that a store writes whole rows; 8 bytes of each of 32 rows at a time, the stores took a workgroup 2 us.
+  uint16_t* mine = (wave & 2 ? v_lds0 : k_lds0) + (wave & 1) * kWinRows * HD;
+  auto swizzle = [](int row) { return CPR == 16 ? row & 15 : (row >> 1) & 7; };
+#pragma unroll
+  for (int d = 0; d < DT; ++d)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) *reinterpret_cast<u32x2*>(mine + lq * HD + ((4 * d + g) ^ swizzle(lq)) * 8 + 4 * hl) = out[d][g];
   __builtin_amdgcn_wave_barrier();  // (a wave's LDS accesses keep their order; the compiler has to keep it too)
-  uint64_t again = __builtin_amdgcn_ballot_w64(check != check && query < len);
-  again = (again | again >> 32) & 0xffffffffu;
 #pragma unroll
   for (int j = 0; j < kWinRows / RPL; ++j) {
     const int row = j * RPL + ld_sub, at = wave_q + (row >> a.pack_log2), head = (kv * n_sub + sub) * pack + (row & (pack - 1));
     const u32x4 w = ld16(mine + row * HD + (ld_c ^ swizzle(row)) * 8);
-    if (at < len && !((again >> row) & 1)) st16(in.o + (((size_t)start + at) * in.n_heads + head) * HD + ld_c * 8, w);
-  }
-  // A hidden key's V that is not finite has made NaN of the rows that share a tile with it (0 times it): rows with NaN are done
-  // again, key by key over what they see, 64 scores at a time.  NaN that they see stays.
-  while (again) {
-    const int row = __builtin_ctzll(again);
-    again &= again - 1;
-    const int at = wave_q + (row >> a.pack_log2), head = (kv * n_sub + sub) * pack + (row & (pack - 1));
-    const uint16_t* qr = in.q + ((size_t)start + at) * in.q_stride + (size_t)head * HD;
-    const int begin = max(at - in.window + 1, 0), before = min(in.sinks, begin), n = at + 1 - begin + before;
-    constexpr int ND = HD / 64;
-    float m = kLowestScore, sum = 0.f, out[ND] = {};
-    for (int c0 = 0; c0 < n; c0 += 64) {
-      const int v = min(c0 + lane, n - 1);
-      const uint16_t* kr = kbase + (size_t)(v < before ? v : v - before + begin) * in.k_stride;
-      float dot = 0.f;
-#pragma unroll 4
-      for (int d = 0; d < HD; d += 2) {
-        const uint32_t x = *reinterpret_cast<const uint32_t*>(qr + d), y = *reinterpret_cast<const uint32_t*>(kr + d);
-        dot = fmaf(bf16_lo(x), bf16_lo(y), dot);
-        dot = fmaf(bf16_hi(x), bf16_hi(y), dot);
-      }
-      dot = c0 + lane < n ? dot * a.scale_log2e : -INFINITY;
-      float most = dot;
-      most = lane_op<1>(most, MaxOp());
-      most = lane_op<2>(most, MaxOp());
-      most = lane_op<kMirror4>(most, MaxOp());
-      most = across_groups<8>(most, MaxOp());
-      const float m_new = fmaxf(m, most), alpha = __builtin_amdgcn_exp2f(m - m_new), p = __builtin_amdgcn_exp2f(dot - m_new);
-      m = m_new;
-      sum = sum * alpha + wave_sum(p);
-#pragma unroll
-      for (int j = 0; j < ND; ++j) out[j] *= alpha;
-      const int count = min(64, n - c0);
-      for (int j = 0; j < count; ++j) {
-        const float pj = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(p), j));
-        const int vj = c0 + j;
-        const uint16_t* vr = vbase + (size_t)(vj < before ? vj : vj - before + begin) * in.v_stride + ND * lane;
-#pragma unroll
-        for (int e = 0; e < ND; ++e) out[e] = fmaf(pj, __uint_as_float((uint32_t)vr[e] << 16), out[e]);
-      }
-    }
-    __bf16* to = reinterpret_cast<__bf16*>(in.o) + (((size_t)start + at) * in.n_heads + head) * HD + ND * lane;
-#pragma unroll
-    for (int e = 0; e < ND; ++e) to[e] = (__bf16)(sum == 0.f ? 0.f : out[e] / sum);
+    if (at < len) st16(in.o + (((size_t)start + at) * in.n_heads + head) * HD + ld_c * 8, w);
   }
 }
 
@@ -424,6 +453,9 @@ hipError_t launch_window_attention(const WindowRows& r, int head_dim, hipStream_
   const WindowPlan p = window_plan(r);
   WindowArgs a{};
   a.r = r;
+  // (no sequence is longer: sums of them and of positions stay in 32 bits)
+  a.r.window = std::min(r.window, r.max_seqlen);
+  a.r.sinks = std::min(r.sinks, r.max_seqlen);
   a.kv_group = r.n_heads / r.n_kv_heads;
   a.pack_log2 = p.pack_log2;
   a.places = (int)p.places;

@@ -176,6 +176,38 @@ def test_scores_below_the_range_weigh_nothing(gpu):
     np.testing.assert_allclose(got[50:55], np.broadcast_to(v[50], (5, n, s)), rtol=2.0 ** -8)
 
 
+@pytest.mark.parametrize("size", [2.0 ** 12, 2.0 ** 30, 2.0 ** 60])
+def test_scores_far_from_zero(gpu, size):
+    """Keys that are alike, but one of two heads' that is a step of bf16 larger: all weigh the same, or the one has all the weight,
+    however far from 0 the scores are."""
+    n, s, l, window, sinks = 2, 64, 150, 40, 3
+    rng = np.random.default_rng(3)
+    for sign in (1, -1):
+        k = np.full((l, n, s), sign * size, np.float32)
+        k[100, 1] *= 1 + sign * 2.0 ** -7
+        bits = [synth.f32_to_bf16_bits(x.astype(np.float32)) for x in (np.ones((l, n, s)), k, rng.standard_normal((l, n, s)))]
+        c = Call(n, n, s, [l], 1, bits=bits).run(_ctx(n, n, s), window, sinks)
+        got, v = gu.to_f64(c.o), orc.from_bf16_bits(bits[2])
+        for i in (0, 50, 99, 100, 120, 139, 140, 149):
+            at = rwo.seen(i + 1, window, sinks)
+            want, mean = v[at].mean(0), np.abs(v[at]).mean(0)
+            if 100 <= i < 140:
+                want[1], mean[1] = v[100, 1], np.abs(v[100, 1])
+            # weights that are equal: their rounding to bf16 is too; sums in fp32, the quotient, the result's rounding
+            assert (np.abs(got[i] - want) <= 2.0 ** -8 * np.abs(want) * 1.01 + 2 * (2.0 ** -8 + 100 * 2.0 ** -23) * mean).all(), (size, i)
+
+
+def test_nothing_finite_at_all(gpu):
+    """NaN and infinities in all of V take longer and make NaN of all that is seen."""
+    n, n_kv, s, l = 16, 2, 128, 3000
+    rng = np.random.default_rng(4)
+    bits = [rows(rng, l, h, s) for h in (n, n_kv, n_kv)]
+    bits[2][:] = 0x7fc0
+    bits[2][::3] = 0x7f80
+    c = Call(n, n_kv, s, [l - 7, 7], 1, bits=bits).run(_ctx(n, n_kv, s), 500, 4)
+    assert torch.isnan(c.o.float()).all()
+
+
 def test_a_bound_below_a_length_drops_the_rest(gpu):
     n, s = 4, 64
     Call(n, n, s, [200, 90], 4).run(_ctx(n, n, s), 30, 4, bound=120).check(30, 4, lens=[120, 90])
