@@ -102,7 +102,7 @@ const char *ds_last_error(const ds_ctx *ctx);
  * ctx_lens[i] + 1 lies in [1, max_ctx] (kv_lens[i] in [0, max_kv_len]).  The calls for 8 bits and for shared prefixes
  * check the same, cu_groups (from 0 to B, no group above max_group_rows), the prefixes' lengths and pages, that no
  * two rows append to one page of 8 bits, and in ds_decode_step_shared that a row appends to no prefix's and no other
- * row's page, whatever the pages hold. */
+ * row's page, whatever the pages hold.  The calls for rotated positions and windows check theirs as each says below. */
 ds_status ds_set_validate(ds_ctx *ctx, int32_t on);
 
 /* Workspace (device bytes) for ds_prefill with up to max_tokens packed tokens.
@@ -387,8 +387,8 @@ ds_status ds_kv_append_rotary(ds_ctx *ctx, const void *q, int32_t q_stride, cons
 /* ds_prefill_attention through a window: the query of token i sees token j <= i of its sequence if i - j < window (>= 1) or
  * j < sinks (>= 0: first tokens that stay visible).  Rows of q, k and v start their strides (in elements, multiples of 8 up to
  * 2^24, at least a row's width) apart: k and q as ds_kv_append_rotary leaves them, v in the rows of the QKV product.  o is
- * [t, n, s].  Sequences may be empty (the debug validation, which is ds_prefill_attention's, takes none); rows from
- * cu_seqlens[B] on are left as they are.  What a query does not see does not count, whatever it holds; a V that is not finite
+ * [t, n, s].  Sequences may be empty, and rows from cu_seqlens[B] on are left as they are (the debug validation, which
+ * is ds_prefill_attention's, takes neither).  What a query does not see does not count, whatever it holds; a V that is not finite
  * makes NaN of that feature where it is seen.  Scores are fp32: a key whose score is below its range weighs nothing (all of
  * them: output 0), one above it makes the row NaN.  A probability is rounded to bf16 before it meets V.  Workgroups that find a
  * V that is not finite, or scores beyond some 2^20, take several times as long. */
@@ -399,7 +399,8 @@ ds_status ds_prefill_attention_window(ds_ctx *ctx, const void *q, int32_t q_stri
 /* ds_decode_attention over the last `window` (>= 1) tokens of each sequence and its first `sinks` (>= 0): with kv_lens[i] = L
  * the query, which is token L - 1's, sees token j if L - 1 - j < window or j < sinks.  Any kv_type, on its conventions
  * (roundings, scores beyond fp32's range, kv_lens[i] = 0: output 0).  What it does not see does not count, whatever it holds, and
- * entries of block_tables whose 16 tokens are all hidden are not read: they may be -1, their pages given back.
+ * entries of block_tables whose 16 tokens are all hidden are not read: they may be -1, their pages given back (the debug
+ * validation checks the others, and kv_lens).
  * Workspace: ds_decode_window_workspace_bytes(B, max_kv_len, window, sinks) (0: none), which serves smaller batches, lengths,
  * windows and sinks too. */
 size_t ds_decode_window_workspace_bytes(const ds_ctx *ctx, int32_t max_batch, int32_t max_ctx, int32_t window, int32_t sinks);

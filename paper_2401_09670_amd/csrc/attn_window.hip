@@ -336,14 +336,18 @@ __global__ __launch_bounds__(64 * kWinWaves) __attribute__((amdgpu_waves_per_eu(
   for (int d = 0; d < DT; ++d)
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
-      out[d][g] = u32x2{pack_bf16(oacc[d][4 * g] * inv, oacc[d][4 * g + 1] * inv), pack_bf16(oacc[d][4 * g + 2] * inv, oacc[d][4 * g + 3] * inv)};
-      check = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, out[d][g][0]), ones, check, false);
-      check = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, out[d][g][1]), ones, check, false);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {  // (a bit cast of a vector's element would be one of its first)
+        const uint32_t w = pack_bf16(oacc[d][4 * g + 2 * i] * inv, oacc[d][4 * g + 2 * i + 1] * inv);
+        out[d][g][i] = w;
+        check = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w), ones, check, false);
+      }
     }
-  // A hidden key's V that is not finite has made NaN of the rows that share its tile (0 times it), and scores so far from 0 that
-  // their multiple of the reference point is not exact to a sixteenth may have left the exponential's range.  Where a row of
-  // the wave is such a one, all its rows are done again, slowly.
-  if (__builtin_amdgcn_ballot_w64(query < len && (check != check || fabsf(m_run * a.scale_log2e) > 0x1p20f)) != 0) {
+  // A hidden key's V that is not finite has made NaN of the rows that share its tile (0 times it), one that is seen NaN or an
+  // infinity, by the size of its probability; and scores so far from 0 that their multiple of the reference point is not exact
+  // to a sixteenth may have left the exponential's range.  Where a row of the wave is such a one, all its rows are done again,
+  // slowly.
+  if (__builtin_amdgcn_ballot_w64(query < len && (!(fabsf(check) < INFINITY) || fabsf(m_run * a.scale_log2e) > 0x1p20f)) != 0) {
     float m = kLowestScore, sum = 0.f;
     floatx16 acc[DT], odd_ones[DT];  // of V's finite numbers by P; how many others a row sees
 #pragma unroll

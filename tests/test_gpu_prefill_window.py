@@ -208,6 +208,41 @@ def test_nothing_finite_at_all(gpu):
     assert torch.isnan(c.o.float()).all()
 
 
+@pytest.mark.parametrize("s", [64, 128])
+def test_a_hidden_nan_of_any_feature(gpu, s):
+    """One feature of one token's V: nothing of the rows that do not see it changes, whichever feature it is."""
+    n, n_kv, l, window, at = 2, 1, 70, 10, 30
+    rng = np.random.default_rng(8)
+    bits = [rows(rng, l, h, s) for h in (n, n_kv, n_kv)]
+    ctx = _ctx(n, n_kv, s)
+    clean = gu.to_f64(Call(n, n_kv, s, [l], 1, bits=bits).run(ctx, window, 1).o)
+    i = np.arange(l)
+    sees = (i >= at) & (i < at + window)
+    for f in range(s):
+        spoilt = [bits[0], bits[1], bits[2].copy()]
+        spoilt[2][at, 0, f] = 0x7fc0
+        got = gu.to_f64(Call(n, n_kv, s, [l], 1, bits=spoilt).run(ctx, window, 1).o)
+        assert np.isnan(got[sees][:, :, f]).all(), f
+        got[sees, :, f] = clean[sees, :, f]
+        # Done again or not, a result is off by its rounding and its probabilities' (attend): 3 * 2^-8 of the largest V and the
+        # little that scores and sums lose; and there are two.
+        assert (np.abs(got - clean) <= 2.0 ** -5 * np.abs(gu.to_f64(gu.to_dev(bits[2]))).max()).all(), f
+
+
+@pytest.mark.parametrize("s", [64, 128])
+def test_an_infinity_that_all_see(gpu, s):
+    """Of V: NaN of the feature in every row that sees it, whether or not another row of the wave does not."""
+    n, n_kv, l = 4, 2, 140
+    rng = np.random.default_rng(6)
+    bits = [rows(rng, l, h, s) for h in (n, n_kv, n_kv)]
+    bits[2][0, 0, 3], bits[2][0, 1, s - 1] = 0x7f80, 0xff80
+    for window, sinks in ((200, 0), (5, 1)):
+        got = gu.to_f64(Call(n, n_kv, s, [l], 1, bits=bits).run(_ctx(n, n_kv, s), window, sinks).o)
+        hit = np.zeros((l, n, s), bool)
+        hit[:, :2, 3] = hit[:, 2:, s - 1] = True
+        assert np.isnan(got[hit]).all() and np.isfinite(got[~hit]).all()
+
+
 def test_a_bound_below_a_length_drops_the_rest(gpu):
     n, s = 4, 64
     Call(n, n, s, [200, 90], 4).run(_ctx(n, n, s), 30, 4, bound=120).check(30, 4, lens=[120, 90])
