@@ -24,13 +24,17 @@
 //    and into LDS once.  What a tile takes in LDS accesses and softmax bounds it, not its bytes.
 // Where a (row, head) has more than one state, they are written out in fp32 and a second launch merges them in order.  Short
 // prefixes are no part of their own: every row's workgroup takes its prefix and then its own pages, and there are no states.
+// Through a window a row's own pages are those that its last and its first tokens are in, and tiles that hold one of their ends
+// are masked; nothing else changes.
 //
 // Measured, the launches alone under a trace, medians of several processes (a 1 GiB read reaches 5.9 TB/s here): 40 heads, e4m3,
 // 64 sequences of 545 tokens 67 to 70 us = 5.2 to 5.5 TB/s; int8, 128 of 16 to 2048 104 to 122 us = 4.8 to 5.6 (without a trace,
 // from pass to pass and with the append, 109 to 110); 64 heads on 8, e4m3, 48 of 1024 to 4096 60 us = 4.9 (the pieces are
 // unequal) and 4.8 for the states; int8, one of 65538 30 to 31 us = 4.4 and 4.7.  Shared: 64 rows of 40 heads behind 2048 bf16
 // tokens, 16 to 256 of their own, 40 to 42 us = 5.1 TB/s and 5; 7, 40 and 1 rows of 64 heads on 8 behind some 7000 e4m3 tokens
-// 35 to 36 us and 4.9, together 0.28 PFLOP/s (wide tiles).  The least call is 5 us.
+// 35 to 36 us and 4.9, together 0.28 PFLOP/s (wide tiles).  The least call is 5 us.  Windows: 64 sequences of 40 heads, bf16, 1024
+// tokens and 4 first ones 210 us = 6.4 TB/s; 128 of 64 heads on 8, e4m3, up to 512 and 4 23 us = 4.3; one, bf16, 8192 and 16 11.5 us =
+// 2.9 (256 workgroups that start) and 3.9.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
