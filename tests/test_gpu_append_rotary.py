@@ -222,6 +222,36 @@ def test_captured_and_replayed(gpu, kind):
         c.check()
 
 
+@pytest.mark.parametrize("kind", ["bf16", "e4m3", "int8"])
+@pytest.mark.parametrize("one", [False, True])
+def test_rows_and_pages_behind_4_gib(gpu, kind, one):
+    """Rows and pages that lie further behind their start than 32 bits reach."""
+    n, n_kv, s = 8, 2, 128
+    new, before = ([1] * 40, list(range(5, 45))) if one else ([30, 0, 11], [7, 3, 0])
+    ctx = _ctx(n, n_kv, s)
+    near, c = (Call(n, n_kv, s, kind, new, before, s, False, 30, one=one) for _ in range(2))
+    near.run(ctx).check()
+    c.stride = 1 << 26                                         # 40 rows are 5 GiB
+    flat = torch.empty(c.t * c.stride, dtype=torch.bfloat16, device="cuda")
+    flat.view(c.t, c.stride)[:, :c.qkv.shape[1]] = c.qkv
+    c.q, c.k, c.v = flat, flat[n * s:], flat[(n + n_kv) * s:]
+    far = (5 << 30) // c.pages[0][0].nbytes
+
+    def behind(x):
+        big = torch.empty((far + c.nb,) + tuple(x.shape[1:]), dtype=x.dtype, device="cuda")
+        big[far:] = x
+        return big
+
+    c.pages = tuple(None if x is None else behind(x) for x in c.pages)
+    c.bt = gu.i32_dev(np.where(c.tables < 0, -1, c.tables + far))
+    c.nb += far
+    c.run(ctx)
+    torch.cuda.synchronize()
+    assert torch.equal(c.q_out, near.q_out) and torch.equal(c.k_out, near.k_out)
+    for x, y in zip(c.pages, near.pages):
+        assert x is None or torch.equal(x[far:].view(torch.uint8), y.view(torch.uint8))
+
+
 def test_validation(gpu):
     n, n_kv, s = 4, 2, 64
     ctx = _ctx(n, n_kv, s)

@@ -138,3 +138,67 @@ def test_a_piece_behind_its_beginning(gpu):
         end = cut + 1 + i
         want, pav, size, keys = rwo.attend_window(gu.to_f64(q_out[cut + i]), kk[:end], vv[:end], window, sinks)
         assert not close(gu.to_f64(o[i]), want, pav, size, s, keys)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+def test_two_streams_at_once(gpu, kind):
+    """Two contexts, each with its own stream and workspace, and a graph of each replayed beside the other's eager calls."""
+    n, n_kv, s, window, sinks, B, l = 16, 2, 128, 700, 5, 3, 900
+    kind, rng, stride = KINDS[kind], np.random.default_rng(5), (n + 2 * n_kv) * s
+    table = torch.from_numpy(rwo.angle_table(l + 1, s)).cuda()
+    cu = gu.i32_dev(synth.cu_seqlens([l] * B))
+
+    class Side:
+        def __init__(self):
+            self.ctx = binding.Context(n * s, n, s, 64, n_kv_heads=n_kv)
+            self.stream = torch.cuda.Stream()
+            bt, self.nb = synth.make_block_tables([l + 1] * B, 16, 7)
+            self.bt, self.width = gu.i32_dev(bt), bt.shape[1]
+            self.pages = _pages(kind, self.nb, n_kv, s)
+            self.flat, self.one = (gu.to_dev(np.concatenate([rows(rng, t, h, s) for h in (n, n_kv, n_kv)], 1).reshape(-1))
+                                   for t in (B * l, B))
+            self.q, self.k, self.o = (torch.empty(B * l, h, s, dtype=torch.bfloat16, device="cuda") for h in (n, n_kv, n))
+            self.q1, self.o1 = (torch.empty(B, n, s, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+            self.ws = gu.workspace(self.ctx.ds_decode_window_workspace_bytes(B, l + 1, window, sinks))
+            self.lens = [gu.i32_dev([x] * B) for x in (0, l, l + 1)]
+
+        def run(self):
+            f, g, at = self.flat, self.one, ((n + n_kv) * s)
+            self.ctx.ds_kv_append_rotary(f, stride, f[n * s:], f[at:], stride, cu, B, B * l, self.lens[0], None, table, l + 1, s,
+                                         False, self.bt, self.width, *self.pages, self.nb, kind, self.q, self.k)
+            self.ctx.ds_prefill_attention_window(self.q, n * s, self.k, n_kv * s, f[at:], stride, cu, B, B * l, l, window, sinks,
+                                                 self.o)
+            self.ctx.ds_kv_append_rotary(g, stride, g[n * s:], g[at:], stride, None, B, B, self.lens[1], None, table, l + 1, s,
+                                         False, self.bt, self.width, *self.pages, self.nb, kind, self.q1)
+            self.ctx.ds_decode_attention_window(self.q1, self.lens[2], self.bt, B, self.width, l + 1, window, sinks, *self.pages,
+                                                self.nb, kind, self.o1, self.ws)
+
+        def results(self):
+            return [x.clone() for x in (self.q, self.k, self.o, self.q1, self.o1)]
+
+    sides = [Side(), Side()]
+    torch.cuda.synchronize()
+    alone = []
+    for x in sides:
+        with torch.cuda.stream(x.stream):
+            x.run()
+        torch.cuda.synchronize()
+        alone.append(x.results())
+    graphs = []
+    for x in sides:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=x.stream):
+            x.run()
+        graphs.append(graph)
+    for turn in range(4):
+        for x in sides:
+            for y in (x.q, x.k, x.o, x.q1, x.o1):
+                y.zero_()
+        torch.cuda.synchronize()
+        for i in (0, 1):
+            with torch.cuda.stream(sides[i].stream):
+                for _ in range(3):
+                    graphs[i].replay() if turn % 2 == i else sides[i].run()
+        torch.cuda.synchronize()
+        for x, want in zip(sides, alone):
+            assert all(torch.equal(a, b) for a, b in zip(x.results(), want)), turn
