@@ -14,7 +14,7 @@
 //
 // 4 s operations a (query head, visible pair) bound it, and what the softmax takes beside them.  From call to call (a product of
 // 8192^3 reaches 1364 TFLOP/s here, a copy 5.1 TB/s): 64 heads on 8, one prompt of 16383 tokens, window 2048, 64 first ones 1066 us
-// = 995 TFLOP/s; two of 8192, window 1024, 581 us = 887; 40 heads, 12 prompts of 16 to 2048, window 256, 4 first ones, 95 us, of
+// = 995 TFLOP/s; two of 8192, window 1024, 581 us = 887; 40 heads, 12 prompts of 16 to 2048, window 256, 4 first ones, 93 us, of
 // whose work the bytes are 54 and the operations 21.  Two prompts of 32 tokens of 4 heads of 64: 4.8 us, 3.8 of which any call
 // takes.  The large ones run into the chip's power: with zeros for data the first takes a sixth less.  Windows of 256 tokens are 6
 // tiles of a workgroup, at both ends of which there is nothing to overlap with, and a wave goes over some 320 keys for the 256
@@ -90,7 +90,12 @@ __global__ __launch_bounds__(64 * kWinWaves) __attribute__((amdgpu_waves_per_eu(
   // the list of keys
   const int q_end = min(q0 + queries, len);
   const int band = max(q0 - in.window + 1, 0);
-  const int first = min(in.sinks, band);        // number `first` is key `band`
+  // Number `first` is key `band`.  Where a wave has 32 queries and it takes no further tile, the band begins with a half tile: a
+  // wave then goes over a half less (40 heads, 12 prompts, window 256, 4 first tokens 90.7 -> 88.3 us; with a tile more, one prompt
+  // of 500, window 100, 13.2 -> 14.0).
+  const int first_whole = min((in.sinks + 31) & ~31, band), first_least = min(in.sinks, band);
+  const bool whole = a.pack_log2 == 0 && (q_end - band + first_whole + 63) / 64 == (q_end - band + first_least + 63) / 64;
+  const int first = whole ? first_whole : first_least;
   const int total = q_end - band + first;
   const int n_halves = (total + 31) / 32;
 
