@@ -165,7 +165,9 @@ __global__ __launch_bounds__(64 * kWinWaves) __attribute__((amdgpu_waves_per_eu(
   const int tail_half = (least_top + 1) >> 5, clear_half = (most_low + 31) >> 5, seen_sinks = in.sinks >> 5;
 
   floatx16 oacc[DT];
-  float m_run = kLowestScore, l_run = 0.f;
+  // The reference point is kept as the number that is taken off exponents, its product with the scale once rounded, and moves by
+  // what these numbers differ by: scores that are equal then weigh the same before and behind a move, however far from 0 they are.
+  float mb_run = kLowestScore * a.scale_log2e, l_run = 0.f;
 #pragma unroll
   for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -208,7 +210,7 @@ __global__ __launch_bounds__(64 * kWinWaves) __attribute__((amdgpu_waves_per_eu(
     constexpr int kPairSlots = DSTEPS + DT;    // all of them are there before the slots of the last 16 keys
     bf16x8 op[kOps];
     u32x4 pw[2];  // column operands of 16 keys each
-    const float mb = m_run * a.scale_log2e;
+    const float mb = mb_run;
     float sum = 0.f, top_of = -INFINITY;
     auto read = [&](int f) __attribute__((always_inline)) {
       op[f] = f < DSTEPS ? read_k(k_buf, k_from, f) : read_v(v_buf, v_from, (f - DSTEPS) / DT, (f - DSTEPS) % DT);
@@ -278,12 +280,12 @@ __global__ __launch_bounds__(64 * kWinWaves) __attribute__((amdgpu_waves_per_eu(
         most = fmaxf(most, nxt[r]);
       }
     }
-    const float m = lane_op<32>(most, MaxOp());
-    if (__builtin_amdgcn_ballot_w64(m * a.scale_log2e > m_run * a.scale_log2e + kWinSlack) != 0) {
-      const float m_new = fmaxf(m_run, m);
-      const float alpha = __builtin_amdgcn_exp2f((m_run - m_new) * a.scale_log2e);
+    const float mb = lane_op<32>(most, MaxOp()) * a.scale_log2e;
+    if (__builtin_amdgcn_ballot_w64(mb > mb_run + kWinSlack) != 0) {
+      const float mb_new = fmaxf(mb_run, mb);
+      const float alpha = __builtin_amdgcn_exp2f(mb_run - mb_new);
       l_run *= alpha;
-      m_run = m_new;
+      mb_run = mb_new;
 #pragma unroll
       for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -359,10 +361,10 @@ __global__ __launch_bounds__(64 * kWinWaves) __attribute__((amdgpu_waves_per_eu(
       }
     }
   // A hidden key's V that is not finite has made NaN of the rows that share its tile (0 times it), one that is seen NaN or an
-  // infinity, by the size of its probability; and scores so far from 0 that their multiple of the reference point is not exact
+  // infinity, by the size of its probability; and scores so far from 0 that the reference point is not their maximum's exponent
   // to a sixteenth may have left the exponential's range.  Where a row of the wave is such a one, all its rows are done again,
   // slowly.
-  if (__builtin_amdgcn_ballot_w64(query < len && (!(fabsf(check) < INFINITY) || fabsf(m_run * a.scale_log2e) > 0x1p20f)) != 0) {
+  if (__builtin_amdgcn_ballot_w64(query < len && (!(fabsf(check) < INFINITY) || fabsf(mb_run) > 0x1p20f)) != 0) {
     float m = kLowestScore, sum = 0.f;
     floatx16 acc[DT], odd_ones[DT];  // of V's finite numbers by P; how many others a row sees
 #pragma unroll

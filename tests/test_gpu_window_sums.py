@@ -11,6 +11,9 @@ from tests.test_gpu_prefill_window import Call, _ctx
 
 pytestmark = pytest.mark.gpu
 
+# head size, sign of a, a, b of most keys and of one
+FAR = [(64, 1, 2448, 18, 70), (64, -1, 2448, 122, 174), (128, 1, 2448, 50, 150), (128, -1, 2448, 148, 248)]
+
 
 def _alike(rng, l, n_kv, s):
     """V of which every token is the same: bits [l, n_kv, s], nothing near 0."""
@@ -75,3 +78,35 @@ def test_flat_scores_that_are_no_bf16_numbers(gpu):
         assert want.min() > 1 and want.max() < 2 - 2.0 ** -8
         bound = 2.0 ** -8 + 2.0 ** -8 * 1.01 * away + (2.0 ** -21 + 400 * 2.0 ** -23) * 2
         assert (np.abs(got[:, h] - want) <= bound).all(), (h, (np.abs(got[:, h] - want) / bound).max())
+
+
+# Rows' scores are 2048 a + b or 2048 a + b / 2, exact in fp32, times log2(e) / sqrt(s) within 2^19 and 2^20: there a reference point is
+# off by up to 2^-5 in the exponent, and from b = lower to b = upper by as much the other way.
+@pytest.mark.parametrize("s,sign,a,lower,upper", FAR)
+def test_equal_scores_on_either_side_of_another_reference_point(gpu, s, sign, a, lower, upper):
+    """Keys of one score before and behind a key that moves the reference point weigh the same, in rows that it moves by more than the
+    slack and in rows that it moves because another row of the wave is one of those."""
+    n, l = 2, 64
+    rng = np.random.default_rng(9)
+    q, k = np.zeros((l, n, s), np.float32), np.zeros((l, n, s), np.float32)
+    q[:, :, 0], q[::2, :, 1], q[1::2, :, 1] = 2048, 0.5, 1
+    k[:, :, 0], k[:, :, 1] = sign * a, lower
+    k[32, :, 1] = upper
+    v = np.where(np.arange(l)[:, None, None] < 32, 1.5, -1.5) + 2.0 ** -5 * rng.standard_normal((l, n, s))
+    v[32] *= 2.0 ** -8
+    bits = [synth.f32_to_bf16_bits(x.astype(np.float32)) for x in (q, k, v)]
+    qd, kd, vd = (orc.from_bf16_bits(b).astype(np.float64) for b in bits)
+    assert (qd == q).all() and (kd == k).all()
+    got = gu.to_f64(Call(n, n, s, [l], 1, bits=bits).run(_ctx(n, n, s), l, 0).o)
+    for h in range(n):
+        z = qd[:, h] @ kd[:, h].T
+        z = (z - sign * 2048.0 * a) / np.sqrt(s)         # (what all of a row's scores have in common, taken off exactly)
+        p = np.where(np.arange(l) <= np.arange(l)[:, None], np.exp(z - z.max(1, keepdims=True)), 0)
+        p /= p.sum(1, keepdims=True)
+        want = p @ vd[:, h]
+        # The result's rounding; the probabilities' (2^-8 each), whose sum is that of the rounded ones; exponents of at most 24, their
+        # scale and the exponentials in fp32, sums of 128 terms
+        away = (p[:, :, None] * np.abs(vd[None, :, h] - want[:, None])).sum(1)
+        bound = 2.0 ** -8 * np.abs(want) + 2.0 ** -8 * 1.01 * away + (2.0 ** -18 + 128 * 2.0 ** -23) * (p @ np.abs(vd[:, h]))
+        worst = (np.abs(got[:, h] - want) / bound).max(1)
+        assert (worst <= 1).all(), (h, worst.max(), worst.argmax())
