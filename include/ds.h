@@ -387,8 +387,8 @@ ds_status ds_kv_append_rotary(ds_ctx *ctx, const void *q, int32_t q_stride, cons
 /* ds_prefill_attention through a window: the query of token i sees token j <= i of its sequence if i - j < window (>= 1) or
  * j < sinks (>= 0: first tokens that stay visible).  Rows of q, k and v start their strides (in elements, multiples of 8 up to
  * 2^24, at least a row's width) apart: k and q as ds_kv_append_rotary leaves them, v in the rows of the QKV product.  o is
- * [t, n, s].  Sequences may be empty, and rows from cu_seqlens[B] on are left as they are (the debug validation, which
- * is ds_prefill_attention's, takes neither).  What a query does not see does not count, whatever it holds; a V that is not finite
+ * [t, n, s].  Sequences may be empty, and rows from cu_seqlens[B] on are left as they are (the debug validation refuses those, as
+ * ds_prefill_attention's does).  What a query does not see does not count, whatever it holds; a V that is not finite
  * makes NaN of that feature where it is seen.  Scores are fp32: a key whose score is below its range weighs nothing (all of
  * them: output 0), one above it makes the row NaN.  A probability is rounded to bf16 before it meets V.  Workgroups that find a
  * V that is not finite, or scores beyond some 2^20, take several times as long. */

@@ -390,15 +390,16 @@ ds_status fetch_i32(ds_ctx* ctx, const int32_t* dev, size_t n, hipStream_t s, st
   return DS_OK;
 }
 
-// cu_seqlens [B+1]: starts at 0, ends at t, every length in [1, max_seqlen]
+// cu_seqlens [B+1]: starts at 0, ends at t, every length in [least, max_seqlen]
 ds_status validate_cu(ds_ctx* ctx, const char* who, const int32_t* cu_dev, int B, int t, int max_seqlen,
-                      hipStream_t s, std::vector<int32_t>& cu) {
+                      hipStream_t s, std::vector<int32_t>& cu, int least = 1) {
   ds_status st = fetch_i32(ctx, cu_dev, (size_t)B + 1, s, cu);
   if (st != DS_OK) return st;
   if (cu[0] != 0) return fail(ctx, DS_ERR_BOUNDS, "%s: cu_seqlens[0] = %d, must be 0", who, cu[0]);
   for (int i = 0; i < B; ++i) {
     const long len = (long)cu[i + 1] - cu[i];
-    if (len < 1) return fail(ctx, DS_ERR_BOUNDS, "%s: cu_seqlens not increasing at sequence %d", who, i);
+    if (len < least)
+      return fail(ctx, DS_ERR_BOUNDS, "%s: cu_seqlens %s at sequence %d", who, least > 0 ? "not increasing" : "decreases", i);
     if (len > max_seqlen)
       return fail(ctx, DS_ERR_BOUNDS, "%s: sequence %d has %ld tokens > max_seqlen %d", who, i, len, max_seqlen);
   }
@@ -1506,7 +1507,7 @@ ds_status ds_prefill_attention_window(ds_ctx* ctx, const void* q, int32_t q_stri
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (ctx->validate) {
     std::vector<int32_t> cu;
-    if (ds_status st = validate_cu(ctx, who, cu_seqlens, B, t, max_seqlen, s, cu)) return st;
+    if (ds_status st = validate_cu(ctx, who, cu_seqlens, B, t, max_seqlen, s, cu, 0)) return st;
   }
   DS_LAUNCH(ctx, s, DS_K_PREFILL_ATTN, ds::launch_window_attention(rows, c.head_dim, s));
   return DS_OK;
