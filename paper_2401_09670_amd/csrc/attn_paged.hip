@@ -122,7 +122,7 @@ struct Seen {
   int low;  // tokens of that page that are hidden
 };
 __device__ __forceinline__ Seen seen_of(int len, int window, int sinks) {
-  const int hidden = max(len - window, 0);  // tokens before the window
+  const int hidden = max(len, window) - window;  // tokens before the window (in 32 bits whatever the two are)
   Seen v{0, 0, 0, 0};
   if (sinks < hidden) {
     v.sink_pages = (sinks + kKvPage - 1) / kKvPage;
