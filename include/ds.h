@@ -390,7 +390,8 @@ ds_status ds_kv_append_rotary(ds_ctx *ctx, const void *q, int32_t q_stride, cons
  * [t, n, s].  Sequences may be empty, and rows from cu_seqlens[B] on are left as they are (the debug validation refuses those, as
  * ds_prefill_attention's does).  What a query does not see does not count, whatever it holds; a V that is not finite
  * makes NaN of that feature where it is seen.  Scores are fp32: a key whose score is below its range weighs nothing (all of
- * them: output 0), one above it makes the row NaN.  A probability is rounded to bf16 before it meets V.  Workgroups that find a
+ * them: output 0), one above it makes the row NaN.  A probability is rounded to bf16 (2^-8 of it at most) before it meets V, and
+ * the sum is that of the rounded ones: a V that is the same wherever it is seen comes back as it is.  Workgroups that find a
  * V that is not finite, or scores beyond some 2^20, take several times as long. */
 ds_status ds_prefill_attention_window(ds_ctx *ctx, const void *q, int32_t q_stride, const void *k, int32_t k_stride,
                                       const void *v, int32_t v_stride, const int32_t *cu_seqlens, int32_t B, int32_t t,
@@ -398,7 +399,9 @@ ds_status ds_prefill_attention_window(ds_ctx *ctx, const void *q, int32_t q_stri
 
 /* ds_decode_attention over the last `window` (>= 1) tokens of each sequence and its first `sinks` (>= 0): with kv_lens[i] = L
  * the query, which is token L - 1's, sees token j if L - 1 - j < window or j < sinks.  Any kv_type, on its conventions
- * (roundings, scores beyond fp32's range, kv_lens[i] = 0: output 0).  What it does not see does not count, whatever it holds, and
+ * (roundings, scores beyond fp32's range, kv_lens[i] = 0: output 0; a V that is not finite, which a prompt's attention turns into
+ * NaN of the feature, may come out infinite here on bf16 pages and is NaN of the row on pages of 8 bits, as without a
+ * window).  What it does not see does not count, whatever it holds, and
  * entries of block_tables whose 16 tokens are all hidden are not read: they may be -1, their pages given back (the debug
  * validation checks the others, and kv_lens).
  * Workspace: ds_decode_window_workspace_bytes(B, max_kv_len, window, sinks) (0: none), which serves smaller batches, lengths,

@@ -13,12 +13,13 @@
 // transposing LDS read.
 //
 // 4 s operations a (query head, visible pair) bound it, and what the softmax takes beside them.  From call to call (a product of
-// 8192^3 reaches 1364 TFLOP/s here, a copy 5.1 TB/s): 64 heads on 8, one prompt of 16383 tokens, window 2048, 64 first ones 1066 us
-// = 995 TFLOP/s; two of 8192, window 1024, 581 us = 887; 40 heads, 12 prompts of 16 to 2048, window 256, 4 first ones, 93 us, of
-// whose work the bytes are 54 and the operations 21.  Two prompts of 32 tokens of 4 heads of 64: 4.8 us, 3.8 of which any call
-// takes.  The large ones run into the chip's power: with zeros for data the first takes a sixth less.  Windows of 256 tokens are 6
-// tiles of a workgroup, at both ends of which there is nothing to overlap with, and a wave goes over some 320 keys for the 256
-// that each of its rows sees.
+// 8192^3 reaches 1364 TFLOP/s here, a copy 5.1 TB/s), over three sets of tensors in turn and on several cards: 64 heads on 8, one
+// prompt of 16383 tokens, window 2048, 64 first ones 1074 to 1096 us = 968 to 988 TFLOP/s; two of 8192, window 1024, 587 to 601 us =
+// 857 to 878; 40 heads, 12 prompts of 16 to 2048, window 256, 4 first ones, 93 us, of whose work the bytes are 54 and the operations
+// 21.  Two prompts of 32 tokens of 4 heads of 64: 4.8 us, 3.8 of which any call takes.  The large ones run into the chip's power:
+// with zeros for data the first takes a sixth less.  A workgroup of the third has 128 + 255 keys and a half tile of first ones: 7 tiles,
+// at both ends of which there is nothing to overlap with.  A wave goes over 10 of their 13 halves, 320 keys for the 256 that each of
+// its rows sees, and waits at the barriers of the others.
 #include <algorithm>
 #include <type_traits>
 
@@ -91,8 +92,8 @@ __global__ __launch_bounds__(64 * kWinWaves) __attribute__((amdgpu_waves_per_eu(
   const int q_end = min(q0 + queries, len);
   const int band = max(q0 - in.window + 1, 0);
   // Number `first` is key `band`.  Where a wave has 32 queries and it takes no further tile, the band begins with a half tile: a
-  // wave then goes over a half less (40 heads, 12 prompts, window 256, 4 first tokens 90.7 -> 88.3 us; with a tile more, one prompt
-  // of 500, window 100, 13.2 -> 14.0).
+  // wave then goes over a half less (40 heads, 12 prompts, window 256, 4 first tokens, three sets of tensors in turn 95.3 -> 93.0 us,
+  // one set 90.9 -> 88.6; with a tile more, one prompt of 500, window 100, one set, 13.2 -> 14.0).
   const int first_whole = min((in.sinks + 31) & ~31, band), first_least = min(in.sinks, band);
   const bool whole = a.pack_log2 == 0 && (q_end - band + first_whole + 63) / 64 == (q_end - band + first_least + 63) / 64;
   const int first = whole ? first_whole : first_least;

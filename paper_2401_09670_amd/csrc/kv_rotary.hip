@@ -52,10 +52,12 @@ __device__ __forceinline__ void load_words(uint32_t (&w)[N], const uint16_t* p) 
     w[1] = v[1];
   }
 }
-// Rows into the pages go past the caches, and the turned rows where there are more of them than the last-level cache keeps for
-// whoever reads them next.  (us, none past, all past, by this rule: 20000 rows of 64 heads, 320 MB of Q, 159, 144 and 141;
-// 6800 of 40, 139 MB of Q and K and as much into bf16 pages, 97, 91 and 80, and with the attention of 8000 of 40 behind it
-// 248, 251 and 239; one row of 64 sequences of 40 and its attention 115.8, 113.1 and 113.6.)
+// Rows into the pages go past the caches (V of 8 bits apart where sequences have rows of any number: its pieces, half of what
+// such a cache takes, are stored as usual), and the turned rows where there are more of them than the last-level cache keeps
+// for whoever reads them next.  (us, nothing past, all past, by this rule: 20000 rows of 64 heads, 320 MB of Q, 155, 141 and 141;
+// 6800 of 40, 139 MB of Q and K and as much into bf16 pages, two sets of tensors in turn 95, 87 and 78, three sets 95, 88 and 91,
+// and 8000 of 40 with the attention behind them 237, 234 and 230; one row of 64 sequences of 40 and its attention 115.3, 113.5
+// and 113.5.)
 template <int N>
 __device__ __forceinline__ void store_past(void* p, const uint32_t (&w)[N]) {
   if constexpr (N == 4) __builtin_nontemporal_store(u32x4{w[0], w[1], w[2], w[3]}, reinterpret_cast<u32x4*>(p));
@@ -300,8 +302,8 @@ __global__ __launch_bounds__(kRotThreads) void kv_append_rotary_kernel(const Rot
 
 constexpr double kKeptBytes = 200e6;  // what is left of the last-level cache beside what is read
 
-// Heads of a wave, where that leaves two waves a SIMD or more; else 1.  (8: the 6800 rows above 80 instead of 78 us, the 20000 157
-// instead of 153.)
+// Heads of a wave, where that leaves two waves a SIMD or more; else 1.  (8: the 6800 rows above, three sets of tensors in turn, 94.3
+// instead of 91.9 us, the 20000 144.4 instead of 141.2.)
 constexpr int kHeads = 4;
 
 struct RotaryPlan {
