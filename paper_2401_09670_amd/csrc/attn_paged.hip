@@ -34,7 +34,7 @@
 // tokens, 16 to 256 of their own, 40 to 42 us = 5.1 TB/s and 5; 7, 40 and 1 rows of 64 heads on 8 behind some 7000 e4m3 tokens
 // 35 to 36 us and 4.9, together 0.28 PFLOP/s (wide tiles).  The least call is 5 us.  Windows: 64 sequences of 40 heads, bf16, 1024
 // tokens and 4 first ones 210 to 215 us = 6.3 to 6.4 TB/s; 128 of 64 heads on 8, e4m3, up to 512 and 4 22 to 23 us = 4.3 to
-// 4.5; one, bf16, 8192 and 16 10.6 to 11.6 us = 2.9 to 3.2 (512 workgroups that start) and 3.7 to 3.9 for the states.
+// 4.5; one, bf16, 8192 and 16 11 to 12 us = 2.9 to 3.2 (512 workgroups that start) and 3.7 to 3.9 for the states.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>

@@ -14,8 +14,8 @@
 //
 // 4 s operations a (query head, visible pair) bound it, and what the softmax takes beside them.  From call to call (a product of
 // 8192^3 reaches 1364 TFLOP/s here, a copy 5.1 TB/s), over three sets of tensors in turn and on several cards: 64 heads on 8, one
-// prompt of 16383 tokens, window 2048, 64 first ones 1067 to 1096 us = 968 to 994 TFLOP/s; two of 8192, window 1024, 584 to 601 us =
-// 857 to 883; 40 heads, 12 prompts of 16 to 2048, window 256, 4 first ones, 92 to 93 us, of whose work the bytes are 54 and the
+// prompt of 16383 tokens, window 2048, 64 first ones 1.07 to 1.10 ms = 965 to 994 TFLOP/s; two of 8192, window 1024, 0.58 to 0.60 ms
+// = 855 to 883; 40 heads, 12 prompts of 16 to 2048, window 256, 4 first ones, 92 to 93 us, of whose work the bytes are 54 and the
 // operations 21.  Two prompts of 32 tokens of 4 heads of 64: 4.8 us, 3.8 of which any call takes.  The large ones run into the chip's power:
 // with zeros for data the first takes a sixth less.  A workgroup of the third has 128 + 255 keys and a half tile of first ones: 7 tiles,
 // at both ends of which there is nothing to overlap with.  A wave goes over 10 of their 13 halves, 320 keys for the 256 that each of

@@ -4,7 +4,7 @@
 // fp32, products and sums rounded one by one (no fused multiply-add: the result is the definition's bit by bit, whichever of a
 // pair a lane computes), then to bf16 once; a cache of 8 bits holds that bf16 row rounded again (kv_quant.h).
 // Bytes bound it: every row is read once and written once or (K) twice, the table's rows come out of the caches.  12 prompts, 6800
-// rows of 40 heads, into bf16 pages 84 to 91 us = 5.3 to 5.8 TB/s by card over three sets of tensors in turn, 80 over two; pieces of
+// rows of 40 heads, into bf16 pages 84 to 92 us = 5.3 to 5.8 TB/s by card over three sets of tensors in turn, 80 over two; pieces of
 // 20000 rows of 64 heads on 8 into int8 pages 136 to 141 us = 5.9 to 6.2 (a copy reaches 5.1).  One row of 64 sequences of 64 heads on 8: 3.8 us on the GPU, 5.2
 // from call to call, which is the host.
 //
