@@ -1,7 +1,6 @@
 """Attention of prompts through a window divides by the sum of the very probabilities that it multiplies V with."""
 import numpy as np
 import pytest
-import torch
 
 from oracle import ds_oracle as orc
 from paper_2401_09670_amd import synth
